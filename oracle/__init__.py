@@ -20,6 +20,8 @@ e4m3             Exact OCP E4M3FN encoder / decoder and the overflow predicate.
 fp8_consumer     Stage 3 of the geometry-aware forward pass up to the E4M3
                  logits: S = Q K^T / sqrt(d_h), S / scale, codes, max |S~| and
                  the overflow count per head.
+fp8_blocks       8-bit matrices with a scale for each block of 128.
+rotary           Rotary positions as complex rotations.
 
 Every function here is pinned by the ``-m "not gpu"`` tests against values
 the paper prints, closed forms or textbook routines; none is "parity

@@ -1,0 +1,390 @@
+// Products of 8-bit matrices with a scale for each block of 128 (spectral_matmul_fp8):
+//   C[i][j] = sum_b sA[b][i] sB[b][j] sum_{c in b} A[i][c] B[j][c].
+// A block's inner sum starts from zero on the matrix cores; the vector ALUs add
+// it to C with the blocks' scales, in float32.
+//
+// Which matrix instruction depends on C's type.  The 8-bit one (16x16x128, the
+// depth of a block) adds the products of 8 neighbouring columns at the exponent of the
+// largest, dropping what lies 14 bits below it: measured, 1 + 2^-13 is kept
+// and 1 + 2^-14 is not, while different eights are added in float32.  On normal values a
+// block's sum is off by 1.5e-5 of itself: nothing in a C of bf16 (2^-8), nor beside
+// the codes' own rounding (2^-4), but more than a float32 C stands for.  A
+// float32 C takes the codes as float16, which holds both formats exactly, and the float16
+// instruction, whose products are exact and summed in float32 (1e-8 of the sum), at half the rate.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "entry_util.h"
+#include "fp8_device.h"
+#include "quantize_fp8.h"
+
+namespace {
+
+using namespace sn_dev;
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct MatArgs {
+  const uint8_t* a;
+  const uint8_t* b;
+  const float* sa;
+  const float* sb;
+  void* c;
+  int64_t m, n, k;
+  int64_t ld_a, ld_b, ld_c;
+  int64_t sa_block, sa_row, sb_block, sb_row;
+  int32_t a_shift, b_shift;  // log2 of the rows that share a scale (0 or 7)
+  int32_t tiles_m, tiles_n;
+  int32_t vec;  // C takes 4 elements in one store
+};
+
+// One 16 x 16 block of the inner sums over 128 columns: rows from x (format
+// FX: 0 E4M3, 1 E5M2), columns from y.  A lane gives 32 bytes of row lane % 16 of
+// each; any 32 columns, the same ones in x and y.
+template <int FX, int FY>
+__device__ __forceinline__ f32x4 block_product(const i32x8& x, const i32x8& y) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, f32x4{0.f, 0.f, 0.f, 0.f}, FX, FY, 0, 0, 0, 0);
+}
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Eight codes as float16, exactly (NaN codes as NaN).
+template <int F>
+__device__ __forceinline__ f16x8 widen(uint32_t w0, uint32_t w1) {
+  f16x2 h[4];
+  if constexpr (F == 0) {
+    h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.f, false);
+    h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.f, true);
+    h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.f, false);
+    h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.f, true);
+  } else {
+    // E5M2 is the upper byte of a float16
+    h[0] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0u, w0, 0x010c000cu));
+    h[1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0u, w0, 0x030c020cu));
+    h[2] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0u, w1, 0x010c000cu));
+    h[3] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0u, w1, 0x030c020cu));
+  }
+  return f16x8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+}
+
+__device__ __forceinline__ i32x8 join(const u32x4& lo, const u32x4& hi) {
+  return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// Zeroes the bytes of a 16-byte chunk from byte n on.
+__device__ __forceinline__ void keep_chunk(u32x4& q, int n) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) q[e] = keep_bytes(q[e], n - 4 * e);
+}
+
+// Bytes from a matrix row to the end of the last row of its tile, for the range check of loads:
+// the rows there are, up to the 16-byte chunk that holds column k - 1.
+__device__ __forceinline__ uint32_t range_bytes(int64_t row, int64_t rows, int tile, int64_t ld, int64_t k) {
+  if (row >= rows) return 0;
+  const int64_t last = (rows - row < tile ? rows - row : tile) - 1;
+  return (uint32_t)(last * ld + ((k + 15) & ~int64_t(15)));
+}
+
+template <typename TC>
+__device__ __forceinline__ void store4(TC* p, const f32x4& v, int n, bool vec) {
+  if constexpr (sizeof(TC) == 4) {
+    if (vec && n >= 4) {
+      *reinterpret_cast<f32x4*>(p) = v;
+      return;
+    }
+  } else {
+    if (vec && n >= 4) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+      return;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e < n) p[e] = (TC)v[e];
+}
+
+// Tiles of 128 x 128 by 4 waves of 64 x 64.  Blocks of 128 columns come through two LDS
+// stages of 32 KB, the next requested before the current one is multiplied.
+// The products are formed transposed (rows from B): a lane holds four
+// neighbouring columns of one row of C, with one scale of A.
+constexpr int kT = 128;
+
+template <int FA, int FB, bool ROWS_B, typename TC>
+__global__ void __launch_bounds__(256) matmul_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t stage[2][2 * kT * 128];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int per_xcd = gridDim.x / 8;
+  const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
+  const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
+
+  const int64_t am = bm * kT + 32 * wv, bnr = bn * kT + 32 * wv;  // rows this wave stages
+  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, 32, a.ld_a, a.k));
+  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.b + bnr * a.ld_b, range_bytes(bnr, a.n, 32, a.ld_b, a.k));
+  auto issue = [&](int kb) {
+    uint8_t* dst = stage[kb & 1] + 4096 * wv;
+    stage_issue<32, 0>(ra, dst, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane);
+    stage_issue<32, 0>(rb, dst + kT * 128, 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane);
+  };
+
+  const int wm = wv >> 1, wn = wv & 1;
+  const int64_t m0 = bm * kT + 64 * wm, n0 = bn * kT + 64 * wn;
+  // scales of this lane's rows; rows past the last read the last one's, their results are dropped
+  const float* pa[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) pa[i] = a.sa + (min(m0 + 16 * i + s, a.m - 1) >> a.a_shift) * a.sa_row;
+  const float* pb[ROWS_B ? 16 : 1];
+  if constexpr (ROWS_B) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) pb[j] = a.sb + min(n0 + 16 * (j >> 2) + 4 * q + (j & 3), a.n - 1) * a.sb_row;
+  } else {
+    pb[0] = a.sb + (min(n0, a.n - 1) >> 7) * a.sb_row;
+  }
+
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int n_kb = (int)((a.k + 127) / 128);
+  if (n_kb > 0) issue(0);
+#pragma unroll 1
+  for (int kb = 0; kb < n_kb; ++kb) {
+    float sa[4], sb[ROWS_B ? 16 : 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sa[i] = pa[i][kb * a.sa_block];
+#pragma unroll
+    for (int j = 0; j < (ROWS_B ? 16 : 1); ++j) sb[j] = pb[j][kb * a.sb_block];
+    __builtin_amdgcn_s_waitcnt(0);  // this wave's part of block kb is in LDS
+    __syncthreads();                // every part, and block kb - 1 fully read
+    if (kb + 1 < n_kb) issue(kb + 1);
+    const uint8_t* ta = stage[kb & 1];
+    const uint8_t* tb = ta + kT * 128;
+    u32x4 fa[4][2], fb[4][2];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        fa[r][h] = stage_chunk(ta, 64 * wm + 16 * r + s, 4 * h + q);
+        fb[r][h] = stage_chunk(tb, 64 * wn + 16 * r + s, 4 * h + q);
+      }
+    if (kb + 1 == n_kb) {  // columns from k on are whatever the rows hold there
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          keep_chunk(fa[r][h], keep);
+          keep_chunk(fb[r][h], keep);
+        }
+      }
+    }
+    f32x4 part[4][4];
+    if constexpr (sizeof(TC) == 2) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          part[i][j] = block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1]));
+    } else {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        f16x8 ha[4], hb[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          ha[r] = widen<FA>(fa[r][h >> 1][2 * (h & 1)], fa[r][h >> 1][2 * (h & 1) + 1]);
+          hb[r] = widen<FB>(fb[r][h >> 1][2 * (h & 1)], fb[r][h >> 1][2 * (h & 1) + 1]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                hb[j], ha[i], h == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[i][j], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i][j][e] = fmaf(part[i][j][e], sa[i] * sb[ROWS_B ? 4 * j + e : 0], acc[i][j][e]);
+  }
+
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t m = m0 + 16 * i + s;
+    if (m >= a.m) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t n = n0 + 16 * j + 4 * q;
+      if (n < a.n)
+        store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4), a.vec != 0);
+    }
+  }
+}
+
+template <int FA, int FB, bool ROWS_B>
+void launch2(const MatArgs& a, bool bf16, hipStream_t st) {
+  const dim3 grid((uint32_t)(((a.tiles_m * a.tiles_n + 7) / 8) * 8));
+  if (bf16)
+    matmul_kernel<FA, FB, ROWS_B, __bf16><<<grid, 256, 0, st>>>(a);
+  else
+    matmul_kernel<FA, FB, ROWS_B, float><<<grid, 256, 0, st>>>(a);
+}
+
+template <int FA, int FB>
+void launch1(const MatArgs& a, bool bf16, hipStream_t st) {
+  a.b_shift ? launch2<FA, FB, false>(a, bf16, st) : launch2<FA, FB, true>(a, bf16, st);
+}
+
+void launch(const MatArgs& a, int fa, int fb, bool bf16, hipStream_t st) {
+  if (fa)
+    fb ? launch1<1, 1>(a, bf16, st) : launch1<1, 0>(a, bf16, st);
+  else
+    fb ? launch1<0, 1>(a, bf16, st) : launch1<0, 0>(a, bf16, st);
+}
+
+// ------------------------------------------------------------------ host side
+
+using sn::aligned;
+using sn::refuse;
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct MatPlan {
+  bool plain_a;
+  int64_t ld_codes;  // of a plain A's codes
+  int64_t off_scale, bytes;
+};
+
+// Checks the description and fills in its defaults.
+int resolve(sn_matmul& p, MatPlan& pl) {
+  const bool plain = p.a_type == SN_F32 || p.a_type == SN_BF16;
+  if (!plain && p.a_type != SN_E4M3 && p.a_type != SN_E5M2)
+    return refuse(SN_EDTYPE, "a_type must be SN_E4M3, SN_E5M2, SN_F32 or SN_BF16");
+  if (p.b_type != SN_E4M3 && p.b_type != SN_E5M2) return refuse(SN_EDTYPE, "b_type must be SN_E4M3 or SN_E5M2");
+  if (p.c_type != SN_F32 && p.c_type != SN_BF16) return refuse(SN_EDTYPE, "c_type must be SN_F32 or SN_BF16");
+  if (p.m < 0 || p.n < 0 || p.k < 0) return refuse(SN_EINVAL, "m, n and k must be >= 0");
+  if ((p.a_block_rows != 1 && p.a_block_rows != 128) || (p.b_block_rows != 1 && p.b_block_rows != 128))
+    return refuse(SN_EINVAL, "a_block_rows and b_block_rows must be 1 or 128");
+  if (plain && p.a_block_rows != 1) return refuse(SN_EINVAL, "a plain A is quantised by rows: a_block_rows must be 1");
+  constexpr int64_t kMost = int64_t(1) << 40, kMostLd = int64_t(1) << 22;
+  if (p.m > kMost || p.n > kMost || p.k > kMostLd || p.ld_a > kMost || p.ld_b > kMost || p.ld_c > kMost)
+    return refuse(SN_EINVAL, "m, n or a row stride is too large (k and code rows stay below 2^22)");
+  if (p.ld_a == 0) p.ld_a = plain ? p.k : round_up(p.k, 16);
+  if (p.ld_b == 0) p.ld_b = round_up(p.k, 16);
+  if (p.ld_c == 0) p.ld_c = p.n;
+  if (p.ld_a < p.k || p.ld_b < p.k || p.ld_c < p.n)
+    return refuse(SN_EINVAL, "ld_a and ld_b must be >= k, ld_c >= n");
+  if ((!plain && (p.ld_a % 16 || p.ld_a >= kMostLd)) || p.ld_b % 16 || p.ld_b >= kMostLd || p.k > kMostLd - 128)
+    return refuse(SN_EINVAL, "code rows must be multiples of 16 bytes, below 2^22");
+  if (p.sa_block == 0 && p.sa_row == 0) {
+    p.sa_row = 1;
+    p.sa_block = (p.m + p.a_block_rows - 1) / p.a_block_rows;
+  }
+  if (p.sb_block == 0 && p.sb_row == 0) {
+    p.sb_row = 1;
+    p.sb_block = (p.n + p.b_block_rows - 1) / p.b_block_rows;
+  }
+  if (p.sa_block < 0 || p.sa_row < 0 || p.sb_block < 0 || p.sb_row < 0 || p.sa_block > kMost || p.sa_row > kMost ||
+      p.sb_block > kMost || p.sb_row > kMost)
+    return refuse(SN_EINVAL, "scale strides must be >= 0 and below 2^40");
+  if (((p.m + kT - 1) / kT) * ((p.n + kT - 1) / kT) >= (int64_t(1) << 30))
+    return refuse(SN_EINVAL, "m x n must stay below 2^30 tiles of 128 x 128");
+  if (plain && ((p.m + 127) / 128) * ((p.k + 127) / 128) >= (int64_t(1) << 31))
+    return refuse(SN_EINVAL, "a plain A must stay below 2^31 tiles of 128 x 128");
+  pl = MatPlan{};
+  pl.plain_a = plain;
+  if (plain && p.m > 0 && p.k > 0) {
+    pl.ld_codes = round_up(p.k, 16);
+    pl.off_scale = round_up(p.m * pl.ld_codes, 256);
+    pl.bytes = pl.off_scale + round_up(p.m * ((p.k + 127) / 128) * 4, 256);
+  }
+  return SN_OK;
+}
+
+}  // namespace
+
+extern "C" SN_API int spectral_matmul_fp8_workspace_bytes(const sn_matmul* desc, int64_t* bytes) {
+  if (!desc || !bytes) return refuse(SN_ENULL, "p and bytes must not be NULL");
+  sn_matmul p = *desc;
+  MatPlan pl;
+  if (int rc = resolve(p, pl)) return rc;
+  *bytes = pl.bytes;
+  return SN_OK;
+}
+
+extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, const float* sa, const void* b,
+                                          const float* sb, void* c, void* workspace, int64_t workspace_bytes,
+                                          void* hip_stream) {
+  if (!desc) return refuse(SN_ENULL, "p must not be NULL");
+  sn_matmul p = *desc;
+  MatPlan pl;
+  if (int rc = resolve(p, pl)) return rc;
+  if (p.m == 0 || p.n == 0) return SN_OK;
+  if (!c || (p.k > 0 && (!a || !b || !sb || (!pl.plain_a && !sa))))
+    return refuse(SN_ENULL, "a, sa (of codes), b, sb and c must not be NULL");
+  if (pl.plain_a ? !aligned(a, p.a_type == SN_F32 ? 4 : 2) : !aligned(a, 16) || !aligned(sa, 4))
+    return refuse(SN_EINVAL, "codes must be 16-byte aligned, a plain A and scales aligned to their type");
+  if (!aligned(b, 16) || !aligned(sb, 4) || !aligned(c, p.c_type == SN_F32 ? 4 : 2))
+    return refuse(SN_EINVAL, "codes must be 16-byte aligned, scales and C aligned to their type");
+  if (pl.bytes > 0) {
+    if (!workspace) return refuse(SN_ENULL, "workspace must not be NULL");
+    if (workspace_bytes < pl.bytes) return refuse(SN_EINVAL, "workspace too small (spectral_matmul_fp8_workspace_bytes)");
+    if (!aligned(workspace, 256)) return refuse(SN_EINVAL, "workspace must be 256-byte aligned");
+  }
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (int rc = sn::check_stream(st)) return rc;
+
+  MatArgs g{};
+  g.a = static_cast<const uint8_t*>(a);
+  g.b = static_cast<const uint8_t*>(b);
+  g.sa = sa;
+  g.sb = sb;
+  g.c = c;
+  g.m = p.m;
+  g.n = p.n;
+  g.k = p.k;
+  g.ld_a = p.ld_a;
+  g.ld_b = p.ld_b;
+  g.ld_c = p.ld_c;
+  g.sa_block = p.sa_block;
+  g.sa_row = p.sa_row;
+  g.sb_block = p.sb_block;
+  g.sb_row = p.sb_row;
+  g.a_shift = p.a_block_rows == 128 ? 7 : 0;
+  g.b_shift = p.b_block_rows == 128 ? 7 : 0;
+  const int cs = p.c_type == SN_F32 ? 4 : 2;
+  g.vec = p.ld_c % 4 == 0 && aligned(c, 4 * cs);
+  g.tiles_m = (int32_t)((p.m + kT - 1) / kT);
+  g.tiles_n = (int32_t)((p.n + kT - 1) / kT);
+  if (pl.plain_a && p.k > 0) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    sn::QuantArgs qa{};
+    qa.x = a;
+    qa.rows = p.m;
+    qa.cols = p.k;
+    qa.ld_x = p.ld_a;
+    qa.row_codes = ws;
+    qa.ld_row = pl.ld_codes;
+    qa.row_scale = reinterpret_cast<float*>(ws + pl.off_scale);
+    sn::launch_quantize(qa, p.a_type == SN_BF16, false, false, st);
+    if (int rc = sn::launched("quantise")) return rc;
+    g.a = ws;
+    g.ld_a = pl.ld_codes;
+    g.sa = qa.row_scale;
+    g.sa_block = p.m;
+    g.sa_row = 1;
+  }
+  launch(g, p.a_type == SN_E5M2, p.b_type == SN_E5M2, p.c_type == SN_BF16, st);
+  return sn::launched("product");
+}

@@ -25,6 +25,7 @@
 
 #include "kernels.h"
 #include "logits_fp8.h"
+#include "rotary.h"
 #include "spectral.h"
 
 namespace {
@@ -1217,10 +1218,11 @@ SN_API int spectral_logits_workspace_bytes(const sn_shape* shape, int32_t seq_le
   return SN_OK;
 }
 
-SN_API int spectral_logits_fp8(sn_ctx* c, const void* const* x_layers, int64_t ld_x, int32_t seq_len,
-                               const void* const* wq_layers, const void* const* wk_layers, const float* scale,
-                               void* workspace, int64_t workspace_bytes, uint8_t* codes, float* max_abs,
-                               int32_t* n_over) {
+// rotary: the frequencies by which Q and K are turned between the projections and the logits, or nullptr
+static int run_logits(sn_ctx* c, const void* const* x_layers, int64_t ld_x, int32_t seq_len,
+                      const void* const* wq_layers, const void* const* wk_layers, const float* scale,
+                      const RotaryTable* rotary, const int64_t* positions, void* workspace, int64_t workspace_bytes,
+                      uint8_t* codes, float* max_abs, int32_t* n_over) {
   if (!c) return fail(SN_ENULL, "ctx must not be NULL");
   if (!x_layers || !wq_layers || !wk_layers || !scale || !workspace || !max_abs || !n_over)
     return fail(SN_ENULL, "x_layers, wq_layers, wk_layers, scale, workspace, max_abs and n_over must not be NULL");
@@ -1300,6 +1302,36 @@ SN_API int spectral_logits_fp8(sn_ctx* c, const void* const* x_layers, int64_t l
   rc = timed(c, KIND_LOGITS, [&] { sn_launch_zero_stats(max_abs, n_over, L * sh.n_q_heads, c->stream); });
   if (rc != SN_OK) return rc;
   if ((rc = timed(c, KIND_PROJ, [&] { sn_launch_proj(p, c->stream); })) != SN_OK) return rc;
+  if (rotary) {
+    int r2 = SN_OK;
+    rc = timed(c, KIND_PROJ, [&] {
+      r2 = launch_rotary_planes(*rotary, L, seq_len, positions, sh.n_q_heads, sh.n_kv_heads, p.qh, p.ql, p.kh, p.kl,
+                                c->stream);
+    });
+    if (rc != SN_OK || r2 != SN_OK) return rc != SN_OK ? rc : r2;
+  }
   return timed(c, KIND_LOGITS, [&] { sn_launch_logits(g, dh, c->stream); });
+}
+
+SN_API int spectral_logits_fp8(sn_ctx* c, const void* const* x_layers, int64_t ld_x, int32_t seq_len,
+                               const void* const* wq_layers, const void* const* wk_layers, const float* scale,
+                               void* workspace, int64_t workspace_bytes, uint8_t* codes, float* max_abs,
+                               int32_t* n_over) {
+  return run_logits(c, x_layers, ld_x, seq_len, wq_layers, wk_layers, scale, nullptr, nullptr, workspace,
+                    workspace_bytes, codes, max_abs, n_over);
+}
+
+SN_API int spectral_logits_fp8_rotary(sn_ctx* c, const void* const* x_layers, int64_t ld_x, int32_t seq_len,
+                                      const void* const* wq_layers, const void* const* wk_layers,
+                                      const float* scale, const sn_rotary* rotary, const int64_t* positions,
+                                      void* workspace, int64_t workspace_bytes, uint8_t* codes, float* max_abs,
+                                      int32_t* n_over) {
+  if (!c) return fail(SN_ENULL, "ctx must not be NULL");
+  RotaryTable table{};
+  if (int rc = rotary_table(rotary, table)) return rc;
+  if (rotary->head_dim != c->shape.head_dim) return fail(SN_EINVAL, "the rotary plan has another head_dim");
+  if (reinterpret_cast<uintptr_t>(positions) & 7) return fail(SN_EINVAL, "positions must be 8-byte aligned");
+  return run_logits(c, x_layers, ld_x, seq_len, wq_layers, wk_layers, scale, &table, positions, workspace,
+                    workspace_bytes, codes, max_abs, n_over);
 }
 }  // extern "C"

@@ -1,0 +1,179 @@
+"""8-bit matrices with a scale for each block of 128, and their products.
+
+``quantize_fp8``, ``matmul_fp8`` and ``LinearFp8`` check torch tensors and pass
+them to spectral_quantize_fp8 and spectral_matmul_fp8 (include/spectral.h) on
+the current stream of the tensors' device; all arithmetic runs in the HIP kernels.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .spectral import (SN_BF16, SN_E4M3, SN_E5M2, SN_F32, sn_matmul, spectral_matmul_fp8,
+                       spectral_matmul_fp8_workspace_bytes, spectral_quantize_fp8)
+
+BLOCK = 128
+_FORMATS = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
+_CODES = {torch.float8_e4m3fn: SN_E4M3, torch.float8_e5m2: SN_E5M2, torch.float32: SN_F32, torch.bfloat16: SN_BF16}
+
+
+def _blocks(n: int) -> int:
+    return -(-n // BLOCK)
+
+
+def _on(device):
+    """Makes a tensor's device the current one for a call."""
+    return torch.cuda.device(device)
+
+
+class Fp8Matrix:
+    """A matrix [rows, cols] in 8 bits: ``codes`` [rows, >= cols rounded up to 16] (torch.float8_e4m3fn or float8_e5m2,
+    rows contiguous and 16-byte aligned, columns past ``cols`` not used) and ``scale`` float32 [ceil(cols / 128), rows] (a scale per row and 128 columns) or
+    [ceil(cols / 128), ceil(rows / 128)] (per 128 x 128 tile), any strides:
+    element (r, c) is codes[r, c] * scale[c // 128, r or r // 128]."""
+
+    __slots__ = ("codes", "scale", "rows", "cols", "block_rows")
+
+    def __init__(self, codes: torch.Tensor, scale: torch.Tensor, cols: int | None = None):
+        if codes.dim() != 2 or codes.dtype not in (torch.float8_e4m3fn, torch.float8_e5m2) or not codes.is_cuda:
+            raise ValueError("codes must be a two-dimensional float8 CUDA tensor")
+        self.rows = codes.shape[0]
+        self.cols = codes.shape[1] if cols is None else int(cols)
+        if not 0 <= self.cols <= codes.shape[1]:
+            raise ValueError(f"cols must be in [0, {codes.shape[1]}]")
+        if codes.shape[1] < -(-self.cols // 16) * 16:
+            raise ValueError("code rows must hold their columns rounded up to 16")
+        if self.cols and (codes.stride(1) != 1 or (self.rows > 1 and (codes.stride(0) % 16
+                          or codes.stride(0) < codes.shape[1])) or codes.data_ptr() % 16):
+            raise ValueError("code rows must be contiguous and 16-byte aligned")
+        if scale.dtype != torch.float32 or scale.dim() != 2 or scale.device != codes.device:
+            raise ValueError("scale must be a two-dimensional float32 tensor on the codes' device")
+        kb, mb = _blocks(self.cols), _blocks(self.rows)
+        if tuple(scale.shape) == (kb, self.rows):
+            self.block_rows = 1
+        elif tuple(scale.shape) == (kb, mb):
+            self.block_rows = BLOCK
+        else:
+            raise ValueError(f"scale must be [{kb}, {self.rows}] or [{kb}, {mb}], got {tuple(scale.shape)}")
+        # strides of two zeros say "dense" to the library
+        self.codes, self.scale = codes, scale if any(scale.stride()) else scale.contiguous()
+
+    @property
+    def values(self) -> torch.Tensor:
+        """The codes [rows, cols] without the columns that fill up their rows."""
+        return self.codes[:, :self.cols]
+
+    @property
+    def ld(self) -> int:
+        return self.codes.stride(0) if self.rows > 1 and self.cols else -(-self.cols // 16) * 16
+
+
+def _plain(x: torch.Tensor, name: str) -> int:
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda or x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 CUDA tensor")
+    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        raise ValueError(f"{name} must be row-major")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: bool = False,
+                 fmt: str = "e4m3") -> tuple[Fp8Matrix | None, Fp8Matrix | None]:
+    """x [R, C] (float32 or bfloat16, row-major) to 8 bits.  Returns (the matrix, its transpose); ``rows`` and ``cols``
+    say which of the two are formed, from one reading of x.  ``tile``: a scale per 128 x 128 tile instead of per row
+    (of the transpose: per column) and 128 elements."""
+    ld = _plain(x, "x")
+    if fmt not in _FORMATS:
+        raise ValueError("fmt must be 'e4m3' or 'e5m2'")
+    if not (rows or cols):
+        raise ValueError("rows and cols are both false")
+    r, c = x.shape
+    dev, dtype = x.device, _FORMATS[fmt]
+
+    def room(n, k):  # n code rows of k columns
+        return (torch.empty(n, -(-k // 16) * 16, dtype=dtype, device=dev),
+                torch.empty(_blocks(k), _blocks(n) if tile else n, dtype=torch.float32, device=dev))
+
+    a = room(r, c) if rows else (None, None)
+    b = room(c, r) if cols else (None, None)
+    if r and c:
+        with _on(dev):
+            spectral_quantize_fp8(x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype], int(tile),
+                                  a[0].data_ptr() if rows else 0, a[0].stride(0) if rows else 0,
+                                  a[1].data_ptr() if rows else 0, b[0].data_ptr() if cols else 0,
+                                  b[0].stride(0) if cols else 0, b[1].data_ptr() if cols else 0,
+                                  torch.cuda.current_stream(dev).cuda_stream)
+    return (Fp8Matrix(*a, cols=c) if rows else None), (Fp8Matrix(*b, cols=r) if cols else None)
+
+
+def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """a b^T: a [M, K] an Fp8Matrix, or a float32 or bfloat16 tensor that is quantised by rows to E4M3 on the way; b
+    [N, K] an Fp8Matrix.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8, for callers that
+    keep it (matmul_fp8_workspace_bytes); calls that can run at the same time need their own."""
+    if not isinstance(b, Fp8Matrix):
+        raise ValueError("b must be an Fp8Matrix")
+    plain = not isinstance(a, Fp8Matrix)
+    if plain:
+        ld_a, (m, k), a_type, a_rows, dev = _plain(a, "a"), a.shape, _CODES[a.dtype], 1, a.device
+    else:
+        ld_a, m, k, a_type, a_rows, dev = a.ld, a.rows, a.cols, _CODES[a.codes.dtype], a.block_rows, a.codes.device
+    n = b.rows
+    if b.cols != k:
+        raise ValueError(f"a has {k} columns and b {b.cols}")
+    if b.codes.device != dev:
+        raise ValueError("a and b are on different devices")
+    if out is None:
+        if out_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
+        out = torch.empty(m, n, dtype=out_dtype, device=dev)
+    elif tuple(out.shape) != (m, n) or out.device != dev or out.dtype not in (torch.float32, torch.bfloat16) \
+            or (n > 1 and out.stride(1) != 1) or (m > 1 and out.stride(0) < n):
+        raise ValueError(f"out must be a row-major float32 or bfloat16 tensor [{m}, {n}] on {dev}")
+    if m == 0 or n == 0:
+        return out
+    p = sn_matmul(m, n, k, a_type, _CODES[b.codes.dtype], _CODES[out.dtype], a_rows, b.block_rows, ld_a, b.ld,
+                  out.stride(0) if m > 1 else n, 0 if plain else a.scale.stride(0), 0 if plain else a.scale.stride(1),
+                  b.scale.stride(0), b.scale.stride(1))
+    need = spectral_matmul_fp8_workspace_bytes(p)
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif need and (workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+    with _on(dev):
+        spectral_matmul_fp8(p, (a if plain else a.codes).data_ptr(), 0 if plain else a.scale.data_ptr(),
+                            b.codes.data_ptr(), b.scale.data_ptr(), out.data_ptr(), workspace.data_ptr() if need else 0,
+                            need, torch.cuda.current_stream(dev).cuda_stream)
+    return out
+
+
+class LinearFp8:
+    """y = x W^T with both sides in 8 bits, and its gradients.  The weight [N, K] (float32 or bfloat16) is quantised by
+    tiles, and so is its transpose for dx; ``set_weight`` does so again after an update.  ``backward=False`` (serving)
+    leaves the transpose out.  Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the
+    format of dy."""
+
+    def __init__(self, weight: torch.Tensor, grad_fmt: str = "e4m3", backward: bool = True):
+        if grad_fmt not in _FORMATS:
+            raise ValueError("grad_fmt must be 'e4m3' or 'e5m2'")
+        self.grad_fmt, self._back = grad_fmt, bool(backward)
+        self.set_weight(weight)
+
+    def set_weight(self, weight: torch.Tensor) -> None:
+        self.weight, self.weight_t = quantize_fp8(weight, tile=True, cols=self._back)
+
+    def forward(self, x: torch.Tensor, keep: bool = False, out_dtype: torch.dtype = torch.bfloat16):
+        """x [M, K] -> y [M, N].  With ``keep``: (y, what backward needs of x)."""
+        if not keep:
+            return matmul_fp8(x, self.weight, out_dtype)
+        rows, cols = quantize_fp8(x, cols=True)
+        return matmul_fp8(rows, self.weight, out_dtype), cols
+
+    def backward(self, dy: torch.Tensor, kept: Fp8Matrix, dx_dtype: torch.dtype = torch.bfloat16,
+                 dw_dtype: torch.dtype = torch.float32) -> tuple[torch.Tensor, torch.Tensor]:
+        """dy [M, N] and forward's ``kept`` -> (dx [M, K], dW [N, K])."""
+        if self.weight_t is None:
+            raise ValueError("the layer was made with backward=False")
+        rows, cols = quantize_fp8(dy, cols=True, fmt=self.grad_fmt)
+        return matmul_fp8(rows, self.weight_t, dx_dtype), matmul_fp8(cols, kept, dw_dtype)

@@ -1,0 +1,63 @@
+"""Rotary positions of queries and keys (spectral_rotary, include/spectral.h) for torch tensors."""
+
+from __future__ import annotations
+
+import torch
+
+from .spectral import (SN_BF16, SN_F32, sn_heads, sn_rotary, spectral_rotary, spectral_rotary_frequencies)
+
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "index": 3, "turns": 4}
+_DTYPES = {torch.float32: SN_F32, torch.bfloat16: SN_BF16}
+
+
+class Rotary:
+    """The plan of one model: pairs of the first ``rot_dim`` elements of a head ("half": i and i + rot_dim / 2;
+    "interleaved": 2 i and 2 i + 1) turn by position times base^(-2 i / rot_dim).  ``scaling`` stretches the positions
+    beyond the length ``trained``: "linear", "base", "index" and "turns" as SN_ROTARY_* in include/spectral.h."""
+
+    def __init__(self, head_dim: int, rot_dim: int | None = None, layout: str = "half", base: float = 10000.0,
+                 scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 32.0, trained: int = 0):
+        if layout not in _LAYOUTS:
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        if scaling not in _SCALINGS:
+            raise ValueError(f"scaling must be one of {', '.join(_SCALINGS)}")
+        self.plan = sn_rotary(head_dim, head_dim if rot_dim is None else rot_dim, _LAYOUTS[layout], _SCALINGS[scaling],
+                              base, factor, low, high, trained)
+        spectral_rotary_frequencies(self.plan)  # refuses a bad plan here
+
+    def frequencies(self) -> tuple[list[float], float]:
+        """(angle per position of each pair in radians, amplitude)."""
+        return spectral_rotary_frequencies(self.plan)
+
+    def apply(self, q: torch.Tensor, k: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+              start: int = 0, inverse: bool = False, out=None):
+        """q, k: float32 or bfloat16 [tokens, heads, head_dim], any token and head strides.  positions: int64 [tokens],
+        or None: token t is at start + t; rows of tokens at negative positions (padding) are left as out holds them.
+        inverse turns back: the gradient.  out: a tensor (with k: a pair) like q (and k), which may be the inputs
+        themselves; new tensors if None.  Returns the turned q, or (q, k)."""
+        xs = (q,) if k is None else (q, k)
+        if out is None:
+            outs = tuple(torch.empty_like(x, memory_format=torch.contiguous_format) for x in xs)
+        else:
+            outs = (out,) if k is None else tuple(out)
+            if len(outs) != len(xs):
+                raise ValueError("out must hold one tensor for q and one for k")
+        n, d, dev = q.shape[0] if q.dim() == 3 else -1, self.plan.head_dim, q.device
+        heads = (sn_heads * len(xs))()
+        for i, (x, o) in enumerate(zip(xs, outs)):
+            if x.dim() != 3 or x.shape[0] != n or x.shape[2] != d or x.dtype not in _DTYPES or x.dtype != q.dtype \
+                    or not x.is_cuda or x.device != dev or x.stride(2) != 1:
+                raise ValueError(f"q and k must be [tokens, heads, {d}] float32 or bfloat16 CUDA tensors of one type, "
+                                 "with contiguous heads")
+            if o.shape != x.shape or o.dtype != x.dtype or o.device != dev or o.stride(2) != 1:
+                raise ValueError("out must have the shape, type and device of its input, with contiguous heads")
+            heads[i] = sn_heads(x.data_ptr(), o.data_ptr(), x.shape[1], x.stride(0), x.stride(1), o.stride(0),
+                                o.stride(1))
+        if positions is not None and (positions.dtype != torch.int64 or tuple(positions.shape) != (n,)
+                                      or positions.device != dev or not positions.is_contiguous()):
+            raise ValueError(f"positions must be a contiguous int64 tensor [{n}] on {dev}")
+        with torch.cuda.device(dev):
+            spectral_rotary(self.plan, _DTYPES[q.dtype], n, positions.data_ptr() if positions is not None else 0,
+                            int(start), int(inverse), heads, len(xs), torch.cuda.current_stream(dev).cuda_stream)
+        return outs[0] if k is None else outs

@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libspectral.so")
 
 SN_OK, SN_EINVAL, SN_ENULL, SN_EDTYPE, SN_EHIP, SN_ESTATE = 0, -1, -2, -3, -4, -5
-SN_F32, SN_BF16 = 0, 1
+SN_F32, SN_BF16, SN_E4M3, SN_E5M2 = 0, 1, 2, 3
 SN_FLAG_VALU_K_SWEEP = 1
 SN_FLAG_GRAM = 2
 SN_FLAG_LAYER = 4
@@ -42,6 +42,12 @@ EXPORTED = (
     "spectral_slack_ratio",
     "spectral_logits_workspace_bytes",
     "spectral_logits_fp8",
+    "spectral_logits_fp8_rotary",
+    "spectral_quantize_fp8",
+    "spectral_matmul_fp8_workspace_bytes",
+    "spectral_matmul_fp8",
+    "spectral_rotary_frequencies",
+    "spectral_rotary",
 )
 
 
@@ -66,6 +72,52 @@ class sn_params(ctypes.Structure):
         ("q_strips", ctypes.c_int32),
         ("k_strips", ctypes.c_int32),
         ("flags", ctypes.c_int32),
+    ]
+
+
+class sn_matmul(ctypes.Structure):
+    _fields_ = [
+        ("m", ctypes.c_int64),
+        ("n", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("a_type", ctypes.c_int32),
+        ("b_type", ctypes.c_int32),
+        ("c_type", ctypes.c_int32),
+        ("a_block_rows", ctypes.c_int32),
+        ("b_block_rows", ctypes.c_int32),
+        ("ld_a", ctypes.c_int64),
+        ("ld_b", ctypes.c_int64),
+        ("ld_c", ctypes.c_int64),
+        ("sa_block", ctypes.c_int64),
+        ("sa_row", ctypes.c_int64),
+        ("sb_block", ctypes.c_int64),
+        ("sb_row", ctypes.c_int64),
+    ]
+
+
+class sn_rotary(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("scaling", ctypes.c_int32),
+        ("base", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("low", ctypes.c_double),
+        ("high", ctypes.c_double),
+        ("trained", ctypes.c_int64),
+    ]
+
+
+class sn_heads(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("heads", ctypes.c_int64),
+        ("x_token", ctypes.c_int64),
+        ("x_head", ctypes.c_int64),
+        ("out_token", ctypes.c_int64),
+        ("out_head", ctypes.c_int64),
     ]
 
 
@@ -123,6 +175,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.spectral_logits_fp8.argtypes = [vp, ctypes.POINTER(vp), i64, i32, ctypes.POINTER(vp), ctypes.POINTER(vp), vp,
                                         vp, i64, vp, vp, vp]
     lib.spectral_logits_fp8.restype = ctypes.c_int
+    lib.spectral_logits_fp8_rotary.argtypes = [vp, ctypes.POINTER(vp), i64, i32, ctypes.POINTER(vp),
+                                               ctypes.POINTER(vp), vp, ctypes.POINTER(sn_rotary), vp, vp, i64, vp, vp, vp]
+    lib.spectral_logits_fp8_rotary.restype = ctypes.c_int
+    lib.spectral_quantize_fp8.argtypes = [vp, i64, i64, i64, i32, i32, i32, vp, i64, vp, vp, i64, vp, vp]
+    lib.spectral_quantize_fp8.restype = ctypes.c_int
+    lib.spectral_matmul_fp8_workspace_bytes.argtypes = [ctypes.POINTER(sn_matmul), ctypes.POINTER(i64)]
+    lib.spectral_matmul_fp8_workspace_bytes.restype = ctypes.c_int
+    lib.spectral_matmul_fp8.argtypes = [ctypes.POINTER(sn_matmul), vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.spectral_matmul_fp8.restype = ctypes.c_int
+    lib.spectral_rotary_frequencies.argtypes = [ctypes.POINTER(sn_rotary), dp, dp]
+    lib.spectral_rotary_frequencies.restype = ctypes.c_int
+    lib.spectral_rotary.argtypes = [ctypes.POINTER(sn_rotary), i32, i64, vp, i64, i32, ctypes.POINTER(sn_heads), i32, vp]
+    lib.spectral_rotary.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -249,6 +314,56 @@ def spectral_logits_fp8(ctx: int, x_ptrs: Sequence[int], ld_x: int, seq_len: int
                                               ctypes.c_void_p(scale), ctypes.c_void_p(workspace),
                                               int(workspace_bytes), ctypes.c_void_p(codes or None),
                                               ctypes.c_void_p(max_abs), ctypes.c_void_p(n_over)))
+
+
+def spectral_logits_fp8_rotary(ctx: int, x_ptrs: Sequence[int], ld_x: int, seq_len: int, wq_ptrs: Sequence[int],
+                               wk_ptrs: Sequence[int], scale: int, rotary: sn_rotary, positions: int, workspace: int,
+                               workspace_bytes: int, codes: int, max_abs: int, n_over: int) -> None:
+    n = len(wq_ptrs)
+    xs = (ctypes.c_void_p * n)(*x_ptrs)
+    wq = (ctypes.c_void_p * n)(*wq_ptrs)
+    wk = (ctypes.c_void_p * n)(*wk_ptrs)
+    _check(load_library().spectral_logits_fp8_rotary(
+        ctypes.c_void_p(ctx), xs, int(ld_x), int(seq_len), wq, wk, ctypes.c_void_p(scale), ctypes.byref(rotary),
+        ctypes.c_void_p(positions or None), ctypes.c_void_p(workspace), int(workspace_bytes),
+        ctypes.c_void_p(codes or None), ctypes.c_void_p(max_abs), ctypes.c_void_p(n_over)))
+
+
+# ------------------------------- 8-bit matrices and rotary positions, context-free
+
+
+def spectral_quantize_fp8(x: int, rows: int, cols: int, ld_x: int, dtype: int, fmt: int, tiles: int, row_codes: int,
+                          ld_row: int, row_scale: int, col_codes: int, ld_col: int, col_scale: int,
+                          stream: int = 0) -> None:
+    _check(load_library().spectral_quantize_fp8(x or None, rows, cols, ld_x, dtype, fmt, tiles, row_codes or None,
+                                                ld_row, row_scale or None, col_codes or None, ld_col,
+                                                col_scale or None, stream or None))
+
+
+def spectral_matmul_fp8_workspace_bytes(p: sn_matmul) -> int:
+    out = ctypes.c_int64(0)
+    _check(load_library().spectral_matmul_fp8_workspace_bytes(ctypes.byref(p), ctypes.byref(out)))
+    return out.value
+
+
+def spectral_matmul_fp8(p: sn_matmul, a: int, sa: int, b: int, sb: int, c: int, workspace: int, workspace_bytes: int,
+                        stream: int = 0) -> None:
+    _check(load_library().spectral_matmul_fp8(ctypes.byref(p), a or None, sa or None, b or None, sb or None, c or None,
+                                              workspace or None, workspace_bytes, stream or None))
+
+
+def spectral_rotary_frequencies(p: sn_rotary) -> tuple[list[float], float]:
+    """(angle per position of each pair in radians, amplitude) of a plan."""
+    freq, amp = (ctypes.c_double * 128)(), ctypes.c_double()
+    _check(load_library().spectral_rotary_frequencies(ctypes.byref(p), freq, ctypes.byref(amp)))
+    return list(freq[:p.rot_dim // 2]), amp.value
+
+
+def spectral_rotary(p: sn_rotary, dtype: int, n_tokens: int, positions: int, first: int, inverse: int, heads,
+                    n_heads: int, stream: int = 0) -> None:
+    """heads: a ctypes array of n_heads sn_heads."""
+    _check(load_library().spectral_rotary(ctypes.byref(p), dtype, n_tokens, positions or None, first, inverse, heads,
+                                          n_heads, stream or None))
 
 
 # ------------------------------------------- consumer-side calibration
@@ -435,9 +550,11 @@ class Spectral:
                             sigma.data_ptr(), scale.data_ptr())
         return sigma, scale
 
-    def logits_fp8(self, x, wq, wk, scale, want_codes: bool = False, workspace=None):
+    def logits_fp8(self, x, wq, wk, scale, want_codes: bool = False, workspace=None, rotary=None, positions=None):
         """FP8 E4M3 logit consumer.  x: bf16 [L, seq, d] tensor (or list of
         [seq, >= d] row-major layers); scale: float32 [L] on the device.
+        rotary: a Rotary plan that turns queries and keys by their positions
+        (int64 [seq], the row numbers if None; rows at negative ones stay).
         Returns (max_abs [L, n_q], n_over [L, n_q], codes [L, n_q, seq, seq]
         uint8 or None)."""
         import torch
@@ -457,6 +574,9 @@ class Spectral:
         if scale.dtype != torch.float32 or tuple(scale.shape) != (L,) or not scale.is_cuda:
             raise ValueError(f"scale must be a float32 CUDA tensor of shape ({L},)")
         dev = scale.device
+        if positions is not None and (rotary is None or positions.dtype != torch.int64 or tuple(positions.shape) != (seq,)
+                                      or positions.device != dev or not positions.is_contiguous()):
+            raise ValueError(f"positions go with rotary and must be a contiguous int64 tensor [{seq}] on {dev}")
         need = spectral_logits_workspace_bytes(self.shape, seq)
         if workspace is None or workspace.numel() < need:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
@@ -467,9 +587,14 @@ class Spectral:
         if stream != self._stream:
             spectral_set_stream(self.ctx, stream)
             self._stream = stream
-        spectral_logits_fp8(self.ctx, [t.data_ptr() for t in layers], ld_x, seq, wq_p, wk_p, scale.data_ptr(),
-                            workspace.data_ptr(), workspace.numel(), codes.data_ptr() if want_codes else 0,
-                            max_abs.data_ptr(), n_over.data_ptr())
+        outs = (workspace.data_ptr(), workspace.numel(), codes.data_ptr() if want_codes else 0, max_abs.data_ptr(),
+                n_over.data_ptr())
+        x_p = [t.data_ptr() for t in layers]
+        if rotary is None:
+            spectral_logits_fp8(self.ctx, x_p, ld_x, seq, wq_p, wk_p, scale.data_ptr(), *outs)
+        else:
+            spectral_logits_fp8_rotary(self.ctx, x_p, ld_x, seq, wq_p, wk_p, scale.data_ptr(), rotary.plan,
+                                       positions.data_ptr() if positions is not None else 0, *outs)
         return max_abs, n_over, codes
 
     def profile(self, enable: bool = True):
