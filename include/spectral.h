@@ -287,8 +287,7 @@ SN_API int spectral_logits_fp8(sn_ctx* ctx, const void* const* x_layers, int64_t
  * x / scale is exact and a code is x / scale rounded once, to nearest even.  A
  * block that holds an infinity or a NaN gets scale and codes NaN.
  *   x          device [rows][ld_x] (ld_x = 0: cols) of dtype SN_F32 or
- *              SN_BF16; any alignment of the type, fastest where rows are
- *              16-byte aligned.
+ *              SN_BF16, any alignment of the type.
  *   format     SN_E4M3 or SN_E5M2.
  *   tiles      0: a scale per row and 128 columns (in the transpose: per
  *              column of x and 128 rows); 1: per 128 x 128 tile.
@@ -392,8 +391,7 @@ typedef struct {
 SN_API int spectral_rotary_frequencies(const sn_rotary* p, double* freq, double* amplitude);
 
 /* One tensor of heads: element e of head h of token t is at
- * t * token + h * head + e (strides in elements, any alignment of the type,
- * fastest where every head is 16-byte aligned). */
+ * t * token + h * head + e (strides in elements, any alignment of the type). */
 typedef struct {
   const void* x;
   void* out;                     /* may be x itself, with the same strides; must not overlap it otherwise */

@@ -24,6 +24,48 @@ __device__ __forceinline__ void block_scale(uint32_t amax_bits, int top, float& 
   inverse = __uint_as_float(bad ? 0x7fc00000u : (uint32_t)(127 - e) << 23);
 }
 
+// Wide loads and stores at any alignment of the element, which global memory instructions of this
+// target take (an address that is not a multiple of 16 costs the second line it touches).
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+// Eight neighbouring values of a row as they are stored.
+template <typename T>
+struct Eight {
+  static constexpr int W = sizeof(T) / 2;  // 16-byte words
+  u32x4 w[W];
+  __device__ __forceinline__ float value(int e) const {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t x = w[0][e >> 1];
+      return __uint_as_float(e & 1 ? x & 0xffff0000u : x << 16);
+    } else {
+      return __uint_as_float(w[e >> 2][e & 3]);
+    }
+  }
+  __device__ __forceinline__ uint32_t magnitude(int e) const { return __float_as_uint(value(e)) & 0x7fffffffu; }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j] = u32x4{0, 0, 0, 0};
+  }
+  // Columns c .. c + 7 of a row of n; zeros from n on.
+  __device__ __forceinline__ void load(const T* p, int c, int n) {
+    if (c + 8 <= n) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[j] = *reinterpret_cast<const u32x4_any*>(reinterpret_cast<const char*>(p) + 16 * j);
+      return;
+    }
+    clear();
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+      if (c + e < n) {
+        if constexpr (sizeof(T) == 2)
+          w[0][e >> 1] |= (uint32_t)__builtin_bit_cast(uint16_t, p[e]) << (16 * (e & 1));
+        else
+          w[e >> 2][e & 3] = __float_as_uint(p[e]);
+      }
+  }
+};
+
 constexpr int format_top(bool e5m2) { return e5m2 ? 15 : 8; }
 
 // Four codes of four values, lowest byte first, rounded to nearest even.

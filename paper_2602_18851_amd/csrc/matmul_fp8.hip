@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "entry_util.h"
 #include "fp8_device.h"
@@ -38,7 +39,7 @@ struct MatArgs {
   int64_t sa_block, sa_row, sb_block, sb_row;
   int32_t a_shift, b_shift;  // log2 of the rows that share a scale (0 or 7)
   int32_t tiles_m, tiles_n;
-  int32_t vec;  // C takes 4 elements in one store
+  int32_t fa, fb, c_bf16;    // formats (1: E5M2) and C's type, for the kernels that take any
 };
 
 // One 16 x 16 block of the inner sums over 128 columns: rows from x (format
@@ -89,22 +90,17 @@ __device__ __forceinline__ uint32_t range_bytes(int64_t row, int64_t rows, int t
   return (uint32_t)(last * ld + ((k + 15) & ~int64_t(15)));
 }
 
+// Four neighbouring elements of C, of which n are there.
 template <typename TC>
-__device__ __forceinline__ void store4(TC* p, const f32x4& v, int n, bool vec) {
-  if constexpr (sizeof(TC) == 4) {
-    if (vec && n >= 4) {
-      *reinterpret_cast<f32x4*>(p) = v;
-      return;
-    }
-  } else {
-    if (vec && n >= 4) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-      return;
-    }
+__device__ __forceinline__ void store4(TC* p, const f32x4& v, int n) {
+  typedef TC vec __attribute__((ext_vector_type(4)));
+  typedef vec vec_any __attribute__((aligned(sizeof(TC))));
+  if (n >= 4) {
+    *reinterpret_cast<vec_any*>(p) = vec{(TC)v[0], (TC)v[1], (TC)v[2], (TC)v[3]};
+    return;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
+  for (int e = 0; e < 3; ++e)
     if (e < n) p[e] = (TC)v[e];
 }
 
@@ -227,8 +223,212 @@ __global__ void __launch_bounds__(256) matmul_kernel(MatArgs a) {
     for (int j = 0; j < 4; ++j) {
       const int64_t n = n0 + 16 * j + 4 * q;
       if (n < a.n)
-        store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4), a.vec != 0);
+        store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
     }
+  }
+}
+
+// Few rows of A: every byte of B is used once or a few times, so B's rate from memory
+// bounds the call, and B goes straight to registers.  A workgroup takes 16 TN rows of B
+// against all rows of A (16 TM), its 8 waves every eighth block of columns each;
+// their sums meet in LDS and are added in a fixed order.  A wave requests
+// AHEAD blocks before it multiplies them; four waves a SIMD keep memory busy meanwhile.
+// The matrix cores are idle enough for the float16 instruction, so every block's sum is
+// exact to float32 here whatever C's type.  A plain A (PLAIN 1: bf16, 2: float32) that
+// fits LDS is quantised by every workgroup for itself, which saves a launch.
+constexpr int kFewWaves = 8;
+constexpr int64_t kPlainBytes = 48 << 10;  // LDS for the codes and scales of a plain A
+
+struct Chunks {
+  u32x4 c[2];  // 32 codes of one row: columns 16 q .. 16 q + 15 of each half of a block
+};
+
+// Reads columns c .. c + 15 and c + 64 .. c + 79 of a row.
+__device__ __forceinline__ Chunks load_chunks(const uint8_t* row, int c) {
+  return Chunks{{*reinterpret_cast<const u32x4*>(row + c), *reinterpret_cast<const u32x4*>(row + c + 64)}};
+}
+
+// The same where the row has k codes: columns from k on are zeros.
+__device__ __forceinline__ Chunks load_last(const uint8_t* row, int c, int k) {
+  Chunks r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    r.c[h] = u32x4{0, 0, 0, 0};
+    if (c + 64 * h < k) {
+      r.c[h] = *reinterpret_cast<const u32x4*>(row + c + 64 * h);
+      keep_chunk(r.c[h], k - c - 64 * h);
+    }
+  }
+  return r;
+}
+
+// Codes 8 h .. 8 h + 7 of them as float16.
+template <int F>
+__device__ __forceinline__ f16x8 widen(const Chunks& r, int h) {
+  return widen<F>(r.c[h >> 1][2 * (h & 1)], r.c[h >> 1][2 * (h & 1) + 1]);
+}
+
+// Quantises the rows of a plain A into LDS, as the quantiser does: 16 lanes take a block, 8 values each.
+template <typename T>
+__device__ __forceinline__ void stage_plain(const MatArgs& a, uint8_t* codes, int n_kb) {
+  const int k = (int)a.k, m = (int)a.m;
+  float* scale = reinterpret_cast<float*>(codes + m * n_kb * 128);
+  const int l = threadIdx.x & 15;
+#pragma unroll 2
+  for (int b = threadIdx.x >> 4; b < m * n_kb; b += 4 * kFewWaves) {
+    const int r = b / n_kb, kb = b % n_kb, c = 128 * kb + 8 * l;
+    Eight<T> x;
+    x.load(reinterpret_cast<const T*>(a.a) + r * a.ld_a + c, c, k);
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, x.magnitude(e));
+    float sc, inv;
+    block_scale(max16(top), format_top(false), sc, inv);
+    uint2 w = make_uint2(encode4<false>(x.value(0) * inv, x.value(1) * inv, x.value(2) * inv, x.value(3) * inv),
+                         encode4<false>(x.value(4) * inv, x.value(5) * inv, x.value(6) * inv, x.value(7) * inv));
+    // zeros past the last column, also of a block that is not finite
+    if (c + 8 > k) w = make_uint2(keep_bytes(w.x, k - c), keep_bytes(w.y, k - c - 4));
+    *reinterpret_cast<uint2*>(codes + 128 * b + 8 * l) = w;
+    if (l == 0) scale[b] = sc;
+  }
+}
+
+template <int TM, int TN, int PLAIN, int FA, int FB>
+__global__ void __launch_bounds__(64 * kFewWaves, TM * TN == 1 ? 4 : 2) few_rows_kernel(MatArgs a) {
+  static_assert(PLAIN == 0 || TM <= 2, "a plain A has 32 rows at most");
+  constexpr int AHEAD = PLAIN ? 4 : 2;
+  __shared__ f32x4 sums[kFewWaves][TM * TN][64];
+  extern __shared__ __attribute__((aligned(16))) uint8_t plain_codes[];  // PLAIN: [m][n_kb][128], then scales [m][n_kb]
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int k = (int)a.k, n_kb = (k + 127) / 128, n_full = k / 128;
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * TN;
+  using T = typename std::conditional<PLAIN == 1, __bf16, float>::type;
+  const float* plain_scale = reinterpret_cast<const float*>(plain_codes + (PLAIN ? a.m * n_kb * 128 : 0));
+
+  // rows past the last read the last one's, their results are dropped
+  const uint8_t* pa[TM];
+  const float* ps[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t m = min((int64_t)(16 * i + s), a.m - 1);
+    pa[i] = PLAIN ? plain_codes + m * n_kb * 128 : a.a + m * a.ld_a;
+    ps[i] = PLAIN ? plain_scale + m * n_kb : a.sa + (m >> a.a_shift) * a.sa_row;
+  }
+  const uint8_t* pb[TN];
+  const float* pt[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int64_t n = min(n0 + 16 * j + s, a.n - 1);
+    pb[j] = a.b + n * a.ld_b;
+    pt[j] = a.sb + (n >> a.b_shift) * a.sb_row;
+  }
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  struct Side {
+    Chunks b[TN], a[TM];
+    float sb[TN], sa[TM];
+  };
+  auto load = [&](Side& t, int kb, auto last) {
+    constexpr bool LAST = decltype(last)::value;  // the block that column k ends in
+    const int c = 128 * kb + 16 * q;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      t.b[j] = LAST ? load_last(pb[j], c, k) : load_chunks(pb[j], c);
+      t.sb[j] = pt[j][kb * a.sb_block];
+    }
+    if constexpr (PLAIN == 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        t.a[i] = LAST ? load_last(pa[i], c, k) : load_chunks(pa[i], c);
+        t.sa[i] = ps[i][kb * a.sa_block];
+      }
+    }
+  };
+  auto multiply = [&](Side& t, int kb) {
+    __builtin_amdgcn_sched_barrier(0);  // one block's codes as float16 at a time
+    if constexpr (PLAIN != 0) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        t.a[i] = load_chunks(pa[i], 128 * kb + 16 * q);
+        t.sa[i] = ps[i][kb];
+      }
+    }
+    f32x4 part[TM][TN];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      f16x8 ha[TM], hb[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ha[i] = widen<FA>(t.a[i], h);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) hb[j] = widen<FB>(t.b[j], h);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              hb[j], ha[i], h == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float sb = __shfl(t.sb[j], 4 * q + e);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j][e] = fmaf(part[i][j][e], t.sa[i] * sb, acc[i][j][e]);
+      }
+  };
+  // this wave's full blocks wv, wv + 8, ..: `count` of them, in groups of AHEAD
+  const int count = n_full > wv ? (n_full - wv + kFewWaves - 1) / kFewWaves : 0, groups = count / AHEAD;
+  if constexpr (PLAIN != 0) {
+    stage_plain<T>(a, plain_codes, n_kb);
+    __syncthreads();
+  }
+  int kb = wv;
+#pragma unroll 1
+  for (int g = 0; g < groups; ++g, kb += kFewWaves * AHEAD) {
+    Side t[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) load(t[u], kb + kFewWaves * u, std::false_type{});
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) multiply(t[u], kb + kFewWaves * u);
+  }
+  // what is left: fewer than AHEAD full blocks and, for one wave, the ragged one
+#pragma unroll 1
+  for (; kb < n_full; kb += kFewWaves) {
+    Side t;
+    load(t, kb, std::false_type{});
+    multiply(t, kb);
+  }
+  if (kb < n_kb) {
+    Side t;
+    load(t, kb, std::true_type{});
+    multiply(t, kb);
+  }
+
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sums[wv][i * TN + j][lane] = acc[i][j];
+  __syncthreads();
+#pragma unroll 1
+  for (int t = wv; t < TM * TN; t += kFewWaves) {
+    f32x4 r = sums[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) r += sums[w][t][lane];
+    const int64_t m = 16 * (t / TN) + s, n = n0 + 16 * (t % TN) + 4 * q;
+    if (m >= a.m || n >= a.n) continue;
+    const int left = (int)min(a.n - n, (int64_t)4);
+    if (a.c_bf16)
+      store4(static_cast<__bf16*>(a.c) + m * a.ld_c + n, r, left);
+    else
+      store4(static_cast<float*>(a.c) + m * a.ld_c + n, r, left);
   }
 }
 
@@ -260,8 +460,38 @@ using sn::refuse;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// Rows of A up to which the kernel for few rows runs.
+constexpr int64_t kFewRows = 64;
+
+// LDS that the codes and scales of a plain A take.
+int64_t plain_bytes(int64_t m, int64_t k) { return m * ((k + 127) / 128) * (128 + 4); }
+
+template <int FA, int FB>
+void launch_few(const MatArgs& a, int plain, hipStream_t st) {
+  const int t = (int)((a.m + 15) / 16);
+  const dim3 one((uint32_t)((a.n + 15) / 16)), two((uint32_t)((a.n + 31) / 32));
+  constexpr int W = 64 * kFewWaves;
+  if constexpr (FA == 0) {
+    const size_t lds = (size_t)plain_bytes(a.m, a.k);
+    if (plain == 1)
+      return t == 1 ? few_rows_kernel<1, 1, 1, FA, FB><<<one, W, lds, st>>>(a)
+                    : few_rows_kernel<2, 1, 1, FA, FB><<<one, W, lds, st>>>(a);
+    if (plain == 2)
+      return t == 1 ? few_rows_kernel<1, 1, 2, FA, FB><<<one, W, lds, st>>>(a)
+                    : few_rows_kernel<2, 1, 2, FA, FB><<<one, W, lds, st>>>(a);
+  }
+  switch (t) {
+    case 1: return few_rows_kernel<1, 1, 0, FA, FB><<<one, W, 0, st>>>(a);
+    case 2: return few_rows_kernel<2, 1, 0, FA, FB><<<one, W, 0, st>>>(a);
+    case 3: return few_rows_kernel<3, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
+    default: return few_rows_kernel<4, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
+  }
+}
+
 struct MatPlan {
   bool plain_a;
+  bool few;   // the kernel for few rows
+  bool fuse;  // ... which quantises a plain A itself
   int64_t ld_codes;  // of a plain A's codes
   int64_t off_scale, bytes;
 };
@@ -304,7 +534,9 @@ int resolve(sn_matmul& p, MatPlan& pl) {
     return refuse(SN_EINVAL, "a plain A must stay below 2^31 tiles of 128 x 128");
   pl = MatPlan{};
   pl.plain_a = plain;
-  if (plain && p.m > 0 && p.k > 0) {
+  pl.few = p.m <= kFewRows;
+  pl.fuse = plain && p.m <= 32 && plain_bytes(p.m, p.k) <= kPlainBytes;
+  if (plain && !pl.fuse && p.m > 0 && p.k > 0) {
     pl.ld_codes = round_up(p.k, 16);
     pl.off_scale = round_up(p.m * pl.ld_codes, 256);
     pl.bytes = pl.off_scale + round_up(p.m * ((p.k + 127) / 128) * 4, 256);
@@ -363,11 +595,12 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
   g.sb_row = p.sb_row;
   g.a_shift = p.a_block_rows == 128 ? 7 : 0;
   g.b_shift = p.b_block_rows == 128 ? 7 : 0;
-  const int cs = p.c_type == SN_F32 ? 4 : 2;
-  g.vec = p.ld_c % 4 == 0 && aligned(c, 4 * cs);
   g.tiles_m = (int32_t)((p.m + kT - 1) / kT);
   g.tiles_n = (int32_t)((p.n + kT - 1) / kT);
-  if (pl.plain_a && p.k > 0) {
+  g.fa = p.a_type == SN_E5M2;
+  g.fb = p.b_type == SN_E5M2;
+  g.c_bf16 = p.c_type == SN_BF16;
+  if (pl.plain_a && !pl.fuse && p.k > 0) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     sn::QuantArgs qa{};
     qa.x = a;
@@ -385,6 +618,13 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
     g.sa_block = p.m;
     g.sa_row = 1;
   }
-  launch(g, p.a_type == SN_E5M2, p.b_type == SN_E5M2, p.c_type == SN_BF16, st);
+  if (pl.few) {
+    const int plain = !pl.fuse ? 0 : p.a_type == SN_BF16 ? 1 : 2;
+    if (g.fa)
+      g.fb ? launch_few<1, 1>(g, plain, st) : launch_few<1, 0>(g, plain, st);
+    else
+      g.fb ? launch_few<0, 1>(g, plain, st) : launch_few<0, 0>(g, plain, st);
+  } else
+    launch(g, g.fa, g.fb, g.c_bf16, st);
   return sn::launched("product");
 }

@@ -18,7 +18,6 @@ struct QuantArgs {
   int64_t ld_col;
   float* col_scale;  // [ceil(rows / 128)][cols or column tiles]
   int32_t tiles_c;   // column tiles
-  int32_t vec;       // rows of x are 16-byte aligned
 };
 
 // Queues the kernel (rows, cols >= 1; arguments checked by the caller).

@@ -27,7 +27,7 @@ using sn::QuantArgs;
 // In LDS a column's 16 slots of 8 bytes are permuted by the column group, so
 // that the 16 lanes of a row group write to different banks.
 template <typename T, bool E5M2, bool TILES, bool ROW, bool COL>
-__global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
+__global__ void __launch_bounds__(256, 4) quantize_kernel(QuantArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t tcodes[COL ? 128 * 128 : 16];
   __shared__ uint32_t wave_max[4][128];
   __shared__ __attribute__((aligned(16))) float col_inv[128];
@@ -38,36 +38,18 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
   const int nc = (int)(a.cols - c0 < 128 ? a.cols - c0 : 128);
   const int rl = 8 * rg, cl = 8 * cg;
 
-  float v[8][8];
+  Eight<T> v[8];
   const T* src = static_cast<const T*>(a.x) + r0 * a.ld_x + c0;
-  const bool whole = a.vec && cl + 8 <= nc;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const T* p = src + (rl + i) * a.ld_x + cl;
-    if (whole && rl + i < nr) {
-      if constexpr (sizeof(T) == 2) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[i][2 * e] = __uint_as_float(w[e] << 16);
-          v[i][2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-        }
-      } else {
-        const f32x4 w0 = *reinterpret_cast<const f32x4*>(p), w1 = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[i][e] = w0[e];
-          v[i][4 + e] = w1[e];
-        }
-      }
+    if (rl + i < nr) {
+      v[i].load(src + (rl + i) * a.ld_x + cl, cl, nc);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = rl + i < nr && cl + e < nc ? (float)p[e] : 0.f;
+      v[i].clear();
     }
   }
 
   // maxima of the bits of |x|: an infinity, and a NaN above it, stay
-  auto bits = [](float x) { return __float_as_uint(x) & 0x7fffffffu; };
   constexpr int TOP = format_top(E5M2);
   float rinv[8];  // factor of each of this thread's rows
   if constexpr (TILES) {
@@ -75,7 +57,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, bits(v[i][e]));
+      for (int e = 0; e < 8; ++e) m = max(m, v[i].magnitude(e));
     m = max16(m);
     m = max(m, (uint32_t)__shfl_xor((int)m, 16));
     m = max(m, (uint32_t)__shfl_xor((int)m, 32));
@@ -96,7 +78,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
     for (int i = 0; i < 8; ++i) {
       uint32_t m = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, bits(v[i][e]));
+      for (int e = 0; e < 8; ++e) m = max(m, v[i].magnitude(e));
       float s;
       block_scale(max16(m), TOP, s, rinv[i]);
       if (cg == i && rl + i < nr) a.row_scale[tc * a.rows + r0 + rl + i] = s;
@@ -108,21 +90,22 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       uint2 w = make_uint2(
-          encode4<E5M2>(v[i][0] * rinv[i], v[i][1] * rinv[i], v[i][2] * rinv[i], v[i][3] * rinv[i]),
-          encode4<E5M2>(v[i][4] * rinv[i], v[i][5] * rinv[i], v[i][6] * rinv[i], v[i][7] * rinv[i]));
+          encode4<E5M2>(v[i].value(0) * rinv[i], v[i].value(1) * rinv[i], v[i].value(2) * rinv[i], v[i].value(3) * rinv[i]),
+          encode4<E5M2>(v[i].value(4) * rinv[i], v[i].value(5) * rinv[i], v[i].value(6) * rinv[i], v[i].value(7) * rinv[i]));
       if (cl + 8 > nc) w = make_uint2(keep_bytes(w.x, nc - cl), keep_bytes(w.y, nc - cl - 4));
       if (rl + i < nr && cl < room) *reinterpret_cast<uint2*>(a.row_codes + (r0 + rl + i) * a.ld_row + c0 + cl) = w;
     }
   }
 
   if constexpr (COL) {
+    __builtin_amdgcn_sched_barrier(0);  // the codes by rows first: fewer registers, more waves
     if constexpr (!TILES) {
       uint32_t m[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         m[e] = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m[e] = max(m[e], bits(v[i][e]));
+        for (int i = 0; i < 8; ++i) m[e] = max(m[e], v[i].magnitude(e));
         m[e] = max(m[e], (uint32_t)__shfl_xor((int)m[e], 16));
         m[e] = max(m[e], (uint32_t)__shfl_xor((int)m[e], 32));
       }
@@ -143,7 +126,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantArgs a) {
     for (int e = 0; e < 8; ++e) {
       float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = v[i][e] * (TILES ? rinv[i] : col_inv[cl + e]);
+      for (int i = 0; i < 8; ++i) f[i] = v[i].value(e) * (TILES ? rinv[i] : col_inv[cl + e]);
       uint2 w = make_uint2(encode4<E5M2>(f[0], f[1], f[2], f[3]), encode4<E5M2>(f[4], f[5], f[6], f[7]));
       if (rl + 8 > nr) w = make_uint2(keep_bytes(w.x, nr - rl), keep_bytes(w.y, nr - rl - 4));
       *reinterpret_cast<uint2*>(tcodes + 128 * (cl + e) + 8 * (rg ^ cg)) = w;
@@ -186,9 +169,7 @@ void launch1(const QuantArgs& a, bool e5m2, bool tiles, hipStream_t st) {
 namespace sn {
 
 void launch_quantize(QuantArgs a, bool bf16, bool e5m2, bool tiles, hipStream_t st) {
-  const int es = bf16 ? 2 : 4;
   a.tiles_c = (int32_t)((a.cols + 127) / 128);
-  a.vec = aligned(a.x, 16) && (a.ld_x * es) % 16 == 0;
   bf16 ? launch1<__bf16>(a, e5m2, tiles, st) : launch1<float>(a, e5m2, tiles, st);
 }
 

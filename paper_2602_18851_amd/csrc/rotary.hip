@@ -30,7 +30,8 @@ struct Plain {
   __device__ __forceinline__ void load(int64_t at, float (&f)[V]) const {
     if constexpr (V * sizeof(T) >= 4) {
       typedef T vec __attribute__((ext_vector_type(V)));
-      const vec w = *reinterpret_cast<const vec*>(x + at);
+      typedef vec vec_any __attribute__((aligned(sizeof(T))));  // wide accesses need no more
+      const vec w = *reinterpret_cast<const vec_any*>(x + at);
 #pragma unroll
       for (int e = 0; e < V; ++e) f[e] = (float)w[e];
     } else {
@@ -42,10 +43,11 @@ struct Plain {
   __device__ __forceinline__ void store(int64_t at, const float (&f)[V]) const {
     if constexpr (V * sizeof(T) >= 4) {
       typedef T vec __attribute__((ext_vector_type(V)));
+      typedef vec vec_any __attribute__((aligned(sizeof(T))));
       vec w;
 #pragma unroll
       for (int e = 0; e < V; ++e) w[e] = (T)f[e];
-      *reinterpret_cast<vec*>(out + at) = w;
+      *reinterpret_cast<vec_any*>(out + at) = w;
     } else {
 #pragma unroll
       for (int e = 0; e < V; ++e) out[at + e] = (T)f[e];
@@ -182,18 +184,31 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
   }
 }
 
-template <typename IO, int V>
-void launch_layout(RotaryArgs<IO> a, hipStream_t st) {
+template <typename IO, int V, bool INTERLEAVED>
+void launch_pairs(RotaryArgs<IO> a, hipStream_t st) {
   const int64_t heads = (int64_t)a.t[0].heads + (a.n_tensors > 1 ? a.t[1].heads : 0);
   const int64_t per_token = std::max<int64_t>(1, heads * (a.table.pairs / V));  // items
   a.tokens_per_group = (int32_t)std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 4 * kThreads / per_token));
   const int64_t groups = (a.n_tokens + a.tokens_per_group - 1) / a.tokens_per_group;
   a.splits = groups >= 512 ? 1 : (int32_t)std::min<int64_t>((per_token + kThreads - 1) / kThreads, 64);
-  const dim3 grid((uint32_t)(groups * a.splits));
-  if (a.table.interleaved)
-    rotary_kernel<IO, V, true><<<grid, kThreads, 0, st>>>(a);
-  else
-    rotary_kernel<IO, V, false><<<grid, kThreads, 0, st>>>(a);
+  rotary_kernel<IO, V, INTERLEAVED><<<dim3((uint32_t)(groups * a.splits)), kThreads, 0, st>>>(a);
+}
+
+// Pairs a thread takes: as many as make 16-byte accesses (W elements, half as many
+// neighbouring pairs), where rot_dim and the rest of the head are multiples of that, else
+// half as many, else one.
+template <typename IO, int W>
+void launch_layout(const RotaryArgs<IO>& a, hipStream_t st) {
+  const int rest = a.table.head_dim - 2 * a.table.pairs;
+  auto fits = [&](int v) { return a.table.pairs % v == 0 && rest % v == 0; };
+  if (a.table.interleaved) {
+    if (fits(W / 2)) return launch_pairs<IO, W / 2, true>(a, st);
+    if (fits(W / 4)) return launch_pairs<IO, W / 4, true>(a, st);
+    return launch_pairs<IO, 1, true>(a, st);
+  }
+  if (fits(W)) return launch_pairs<IO, W, false>(a, st);
+  if (fits(W / 2)) return launch_pairs<IO, W / 2, false>(a, st);
+  launch_pairs<IO, 1, false>(a, st);
 }
 
 }  // namespace
@@ -262,11 +277,7 @@ int launch_rotary_planes(const RotaryTable& t, int64_t layers, int64_t seq, cons
     h.x_head = h.out_head = t.head_dim;
     h.x_token = h.out_token = heads[w] * t.head_dim;
   }
-  // planes and heads (multiples of 16 elements) are 16-byte aligned
-  if (t.pairs % 8 == 0)
-    launch_layout<Planes, 8>(a, st);
-  else
-    launch_layout<Planes, 1>(a, st);
+  launch_layout<Planes, 8>(a, st);
   return launched("rotary");
 }
 
@@ -295,9 +306,6 @@ int run_rotary(const RotaryTable& table, int64_t n_tokens, const int64_t* positi
   a.n_tokens = a.period = n_tokens;
   a.sign = inverse ? -1.f : 1.f;
   a.n_tensors = n_heads;
-  constexpr int W = 16 / (int)sizeof(T);  // elements of 16 bytes
-  const int rest = table.head_dim - 2 * table.pairs;
-  bool wide = true;
   for (int w = 0; w < n_heads; ++w) {
     const sn_heads& s = heads[w];
     HeadsArg<Plain<T>>& h = a.t[w];
@@ -308,14 +316,8 @@ int run_rotary(const RotaryTable& table, int64_t n_tokens, const int64_t* positi
     h.x_head = s.x_head;
     h.out_token = s.out_token;
     h.out_head = s.out_head;
-    wide = wide && aligned(s.x, 16) && aligned(s.out, 16) &&
-           ((s.x_token | s.x_head | s.out_token | s.out_head) % W) == 0;
   }
-  // 16-byte accesses where every chunk of a half (of a pair sequence) is whole and aligned
-  if (wide && table.pairs % W == 0 && rest % W == 0)
-    launch_layout<Plain<T>, W>(a, st);
-  else
-    launch_layout<Plain<T>, 1>(a, st);
+  launch_layout<Plain<T>, 16 / (int)sizeof(T)>(a, st);
   return launched("rotary");
 }
 
