@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 
 #include "device_util.h"
 #include "entry_util.h"
@@ -215,7 +216,30 @@ void launch_layout(const RotaryArgs<IO>& a, hipStream_t st) {
 
 namespace sn {
 
+namespace {
+// The table of this thread's last good plan: a program turns every layer by one plan, and forming 64
+// powers takes as long as the launch.
+struct Formed {
+  sn_rotary plan;
+  RotaryTable table;
+  bool any;
+};
+thread_local Formed t_formed{};
+int form_table(const sn_rotary* p, RotaryTable& t);
+}  // namespace
+
 int rotary_table(const sn_rotary* p, RotaryTable& t) {
+  if (p && t_formed.any && std::memcmp(&t_formed.plan, p, sizeof *p) == 0) {
+    t = t_formed.table;
+    return SN_OK;
+  }
+  const int rc = form_table(p, t);
+  if (rc == SN_OK) t_formed = Formed{*p, t, true};
+  return rc;
+}
+
+namespace {
+int form_table(const sn_rotary* p, RotaryTable& t) {
   if (!p) return refuse(SN_ENULL, "the rotary plan must not be NULL");
   if (p->head_dim < 2 || p->head_dim > 1024) return refuse(SN_EINVAL, "head_dim must be in [2, 1024]");
   if (p->rot_dim < 2 || p->rot_dim % 2 || p->rot_dim > p->head_dim || p->rot_dim > 2 * kMaxPairs)
@@ -257,6 +281,7 @@ int rotary_table(const sn_rotary* p, RotaryTable& t) {
   }
   return SN_OK;
 }
+}  // namespace
 
 int launch_rotary_planes(const RotaryTable& t, int64_t layers, int64_t seq, const int64_t* positions, int64_t q_heads,
                          int64_t k_heads, uint16_t* qh, uint16_t* ql, uint16_t* kh, uint16_t* kl, hipStream_t st) {
@@ -345,6 +370,7 @@ extern "C" SN_API int spectral_rotary(const sn_rotary* p, int32_t dtype, int64_t
       return refuse(SN_EINVAL, "strides must be in [0, 2^40]");
     if (n_tokens > 0 && h.heads > 0 && (!h.x || !h.out)) return refuse(SN_ENULL, "x and out must not be NULL");
     if (!aligned(h.x, es) || !aligned(h.out, es)) return refuse(SN_EINVAL, "x and out must be aligned to their type");
+    if (n_tokens == 0 || h.heads == 0) continue;
     const bool heads_apart = h.heads <= 1 || h.out_head >= p->head_dim;
     const bool tokens_apart = n_tokens <= 1 || h.out_token >= p->head_dim;
     const bool nested = n_tokens <= 1 || h.heads <= 1 || h.out_token / h.heads >= h.out_head ||

@@ -7,10 +7,11 @@ the current stream of the tensors' device; all arithmetic runs in the HIP kernel
 
 from __future__ import annotations
 
-import ctypes
+import functools
 
 import torch
 
+from .launch import on_stream_of
 from .spectral import (SN_BF16, SN_E4M3, SN_E5M2, SN_F32, sn_matmul, spectral_matmul_fp8,
                        spectral_matmul_fp8_workspace_bytes, spectral_quantize_fp8)
 
@@ -19,63 +20,67 @@ _FORMATS = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 _CODES = {torch.float8_e4m3fn: SN_E4M3, torch.float8_e5m2: SN_E5M2, torch.float32: SN_F32, torch.bfloat16: SN_BF16}
 
 
-def _blocks(n: int) -> int:
-    return -(-n // BLOCK)
+_FLOAT8 = (torch.float8_e4m3fn, torch.float8_e5m2)
+_PLAIN = (torch.float32, torch.bfloat16)
 
 
-def _on(device):
-    """Makes a tensor's device the current one for a call."""
-    return torch.cuda.device(device)
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(m, n, k, a_type, b_type, c_type, a_rows, b_rows) -> int:
+    return spectral_matmul_fp8_workspace_bytes(sn_matmul(m, n, k, a_type, b_type, c_type, a_rows, b_rows))
 
 
 class Fp8Matrix:
     """A matrix [rows, cols] in 8 bits: ``codes`` [rows, >= cols rounded up to 16] (torch.float8_e4m3fn or float8_e5m2,
-    rows contiguous and 16-byte aligned, columns past ``cols`` not used) and ``scale`` float32 [ceil(cols / 128), rows] (a scale per row and 128 columns) or
-    [ceil(cols / 128), ceil(rows / 128)] (per 128 x 128 tile), any strides:
+    rows contiguous and 16-byte aligned, columns past ``cols`` not used) and ``scale`` float32 [ceil(cols / 128), rows] (a
+    scale per row and 128 columns) or [ceil(cols / 128), ceil(rows / 128)] (per 128 x 128 tile), any strides:
     element (r, c) is codes[r, c] * scale[c // 128, r or r // 128]."""
 
-    __slots__ = ("codes", "scale", "rows", "cols", "block_rows")
+    __slots__ = ("codes", "scale", "rows", "cols", "block_rows", "ld")
 
     def __init__(self, codes: torch.Tensor, scale: torch.Tensor, cols: int | None = None):
-        if codes.dim() != 2 or codes.dtype not in (torch.float8_e4m3fn, torch.float8_e5m2) or not codes.is_cuda:
+        if codes.dtype not in _FLOAT8 or codes.dim() != 2 or not codes.is_cuda:
             raise ValueError("codes must be a two-dimensional float8 CUDA tensor")
-        self.rows = codes.shape[0]
-        self.cols = codes.shape[1] if cols is None else int(cols)
-        if not 0 <= self.cols <= codes.shape[1]:
-            raise ValueError(f"cols must be in [0, {codes.shape[1]}]")
-        if codes.shape[1] < -(-self.cols // 16) * 16:
+        rows, width = codes.shape
+        if cols is None:
+            cols = width
+        if not 0 <= cols <= width:
+            raise ValueError(f"cols must be in [0, {width}]")
+        full = (cols + 15) // 16 * 16
+        if width < full:
             raise ValueError("code rows must hold their columns rounded up to 16")
-        if self.cols and (codes.stride(1) != 1 or (self.rows > 1 and (codes.stride(0) % 16
-                          or codes.stride(0) < codes.shape[1])) or codes.data_ptr() % 16):
+        step, one = codes.stride()
+        self.ld = step if rows > 1 and cols else full
+        if cols and (one != 1 or self.ld % 16 or self.ld < full or codes.data_ptr() % 16):
             raise ValueError("code rows must be contiguous and 16-byte aligned")
-        if scale.dtype != torch.float32 or scale.dim() != 2 or scale.device != codes.device:
-            raise ValueError("scale must be a two-dimensional float32 tensor on the codes' device")
-        kb, mb = _blocks(self.cols), _blocks(self.rows)
-        if tuple(scale.shape) == (kb, self.rows):
+        if scale.dtype != torch.float32 or scale.device != codes.device:
+            raise ValueError("scale must be a float32 tensor on the codes' device")
+        shape = tuple(scale.shape)
+        kb = (cols + 127) // 128
+        if shape == (kb, rows):
             self.block_rows = 1
-        elif tuple(scale.shape) == (kb, mb):
+        elif shape == (kb, (rows + 127) // 128):
             self.block_rows = BLOCK
         else:
-            raise ValueError(f"scale must be [{kb}, {self.rows}] or [{kb}, {mb}], got {tuple(scale.shape)}")
+            raise ValueError(f"scale must be [{kb}, {rows}] or [{kb}, {(rows + 127) // 128}], got {shape}")
         # strides of two zeros say "dense" to the library
         self.codes, self.scale = codes, scale if any(scale.stride()) else scale.contiguous()
+        self.rows, self.cols = rows, cols
 
     @property
     def values(self) -> torch.Tensor:
         """The codes [rows, cols] without the columns that fill up their rows."""
         return self.codes[:, :self.cols]
 
-    @property
-    def ld(self) -> int:
-        return self.codes.stride(0) if self.rows > 1 and self.cols else -(-self.cols // 16) * 16
-
 
 def _plain(x: torch.Tensor, name: str) -> int:
-    if not isinstance(x, torch.Tensor) or x.dim() != 2 or not x.is_cuda or x.dtype not in (torch.float32, torch.bfloat16):
+    """The row stride of a plain matrix."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN or x.dim() != 2 or not x.is_cuda:
         raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 CUDA tensor")
-    if x.shape[1] > 1 and x.stride(1) != 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+    rows, cols = x.shape
+    step, one = x.stride()
+    if (cols > 1 and one != 1) or (rows > 1 and step < cols):
         raise ValueError(f"{name} must be row-major")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    return step if rows > 1 else cols
 
 
 def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: bool = False,
@@ -92,59 +97,66 @@ def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: b
     dev, dtype = x.device, _FORMATS[fmt]
 
     def room(n, k):  # n code rows of k columns
-        return (torch.empty(n, -(-k // 16) * 16, dtype=dtype, device=dev),
-                torch.empty(_blocks(k), _blocks(n) if tile else n, dtype=torch.float32, device=dev))
+        codes = torch.empty((n, (k + 15) // 16 * 16), dtype=dtype, device=dev)
+        return codes, torch.empty(((k + 127) // 128, (n + 127) // 128 if tile else n), dtype=torch.float32, device=dev)
 
-    a = room(r, c) if rows else (None, None)
-    b = room(c, r) if cols else (None, None)
+    a = room(r, c) if rows else None
+    b = room(c, r) if cols else None
     if r and c:
-        with _on(dev):
-            spectral_quantize_fp8(x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype], int(tile),
-                                  a[0].data_ptr() if rows else 0, a[0].stride(0) if rows else 0,
-                                  a[1].data_ptr() if rows else 0, b[0].data_ptr() if cols else 0,
-                                  b[0].stride(0) if cols else 0, b[1].data_ptr() if cols else 0,
-                                  torch.cuda.current_stream(dev).cuda_stream)
+        ra = (a[0].data_ptr(), a[0].shape[1], a[1].data_ptr()) if rows else (0, 0, 0)
+        cb = (b[0].data_ptr(), b[0].shape[1], b[1].data_ptr()) if cols else (0, 0, 0)
+        on_stream_of(dev, spectral_quantize_fp8, x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype],
+                     1 if tile else 0, *ra, *cb)
     return (Fp8Matrix(*a, cols=c) if rows else None), (Fp8Matrix(*b, cols=r) if cols else None)
 
 
 def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:
     """a b^T: a [M, K] an Fp8Matrix, or a float32 or bfloat16 tensor that is quantised by rows to E4M3 on the way; b
-    [N, K] an Fp8Matrix.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8, for callers that
-    keep it (matmul_fp8_workspace_bytes); calls that can run at the same time need their own."""
+    [N, K] an Fp8Matrix.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8 scratch for callers
+    that keep it (a new tensor where it is too small); calls that can run at the same time need their own."""
     if not isinstance(b, Fp8Matrix):
         raise ValueError("b must be an Fp8Matrix")
     plain = not isinstance(a, Fp8Matrix)
     if plain:
-        ld_a, (m, k), a_type, a_rows, dev = _plain(a, "a"), a.shape, _CODES[a.dtype], 1, a.device
+        ld_a = _plain(a, "a")
+        codes, sa, sa_block, sa_row, a_rows = a, 0, 0, 0, 1
+        m, k = a.shape
     else:
-        ld_a, m, k, a_type, a_rows, dev = a.ld, a.rows, a.cols, _CODES[a.codes.dtype], a.block_rows, a.codes.device
-    n = b.rows
+        ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a.scale.data_ptr(), a.block_rows, a.rows, a.cols
+        sa_block, sa_row = a.scale.stride()
+    n, dev = b.rows, codes.device
     if b.cols != k:
         raise ValueError(f"a has {k} columns and b {b.cols}")
     if b.codes.device != dev:
         raise ValueError("a and b are on different devices")
     if out is None:
-        if out_dtype not in (torch.float32, torch.bfloat16):
+        if out_dtype not in _PLAIN:
             raise ValueError("out_dtype must be torch.float32 or torch.bfloat16")
-        out = torch.empty(m, n, dtype=out_dtype, device=dev)
-    elif tuple(out.shape) != (m, n) or out.device != dev or out.dtype not in (torch.float32, torch.bfloat16) \
-            or (n > 1 and out.stride(1) != 1) or (m > 1 and out.stride(0) < n):
-        raise ValueError(f"out must be a row-major float32 or bfloat16 tensor [{m}, {n}] on {dev}")
+        out = torch.empty((m, n), dtype=out_dtype, device=dev)
+        ld_c = n
+    else:
+        if tuple(out.shape) != (m, n) or out.device != dev or out.dtype not in _PLAIN:
+            raise ValueError(f"out must be a float32 or bfloat16 tensor [{m}, {n}] on {dev}")
+        ld_c, one = out.stride()
+        if (n > 1 and one != 1) or (m > 1 and ld_c < n):
+            raise ValueError("out must be row-major")
+        if m <= 1:
+            ld_c = n
     if m == 0 or n == 0:
         return out
-    p = sn_matmul(m, n, k, a_type, _CODES[b.codes.dtype], _CODES[out.dtype], a_rows, b.block_rows, ld_a, b.ld,
-                  out.stride(0) if m > 1 else n, 0 if plain else a.scale.stride(0), 0 if plain else a.scale.stride(1),
-                  b.scale.stride(0), b.scale.stride(1))
-    need = spectral_matmul_fp8_workspace_bytes(p)
-    if need and (workspace is None or workspace.numel() < need):
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    elif need and (workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous()):
-        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
-    with _on(dev):
-        spectral_matmul_fp8(p, (a if plain else a.codes).data_ptr(), 0 if plain else a.scale.data_ptr(),
-                            b.codes.data_ptr(), b.scale.data_ptr(), out.data_ptr(), workspace.data_ptr() if need else 0,
-                            need, torch.cuda.current_stream(dev).cuda_stream)
+    kinds = (m, n, k, _CODES[codes.dtype], _CODES[b.codes.dtype], _CODES[out.dtype], a_rows, b.block_rows)
+    need = _workspace_bytes(*kinds)
+    ws = 0
+    if need:
+        if workspace is None or workspace.numel() < need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
+        ws = workspace.data_ptr()
+    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *b.scale.stride())
+    on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b.scale.data_ptr(),
+                 out.data_ptr(), ws, need)
     return out
 
 

@@ -1,0 +1,16 @@
+"""Calls on the current torch stream of a tensor's device."""
+
+from __future__ import annotations
+
+import torch
+from torch._C import _cuda_getCurrentRawStream as _raw_stream  # the handle without a Stream object around it
+
+
+def on_stream_of(device: torch.device, call, *args) -> None:
+    """call(*args, stream) with the device as the current one."""
+    index = device.index
+    if torch.cuda.current_device() == index:
+        call(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            call(*args, _raw_stream(index))

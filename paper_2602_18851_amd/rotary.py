@@ -2,9 +2,12 @@
 
 from __future__ import annotations
 
+import ctypes
+
 import torch
 
-from .spectral import (SN_BF16, SN_F32, sn_heads, sn_rotary, spectral_rotary, spectral_rotary_frequencies)
+from .launch import on_stream_of
+from .spectral import SN_BF16, SN_F32, sn_rotary, spectral_rotary, spectral_rotary_frequencies
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "index": 3, "turns": 4}
@@ -38,26 +41,35 @@ class Rotary:
         themselves; new tensors if None.  Returns the turned q, or (q, k)."""
         xs = (q,) if k is None else (q, k)
         if out is None:
-            outs = tuple(torch.empty_like(x, memory_format=torch.contiguous_format) for x in xs)
+            outs = None
         else:
             outs = (out,) if k is None else tuple(out)
             if len(outs) != len(xs):
                 raise ValueError("out must hold one tensor for q and one for k")
-        n, d, dev = q.shape[0] if q.dim() == 3 else -1, self.plan.head_dim, q.device
-        heads = (sn_heads * len(xs))()
-        for i, (x, o) in enumerate(zip(xs, outs)):
-            if x.dim() != 3 or x.shape[0] != n or x.shape[2] != d or x.dtype not in _DTYPES or x.dtype != q.dtype \
-                    or not x.is_cuda or x.device != dev or x.stride(2) != 1:
-                raise ValueError(f"q and k must be [tokens, heads, {d}] float32 or bfloat16 CUDA tensors of one type, "
-                                 "with contiguous heads")
-            if o.shape != x.shape or o.dtype != x.dtype or o.device != dev or o.stride(2) != 1:
-                raise ValueError("out must have the shape, type and device of its input, with contiguous heads")
-            heads[i] = sn_heads(x.data_ptr(), o.data_ptr(), x.shape[1], x.stride(0), x.stride(1), o.stride(0),
-                                o.stride(1))
+        d, dev, dtype = self.plan.head_dim, q.device, q.dtype
+        n = q.shape[0] if q.dim() == 3 else -1
+        made, fields = [], []
+        for i, x in enumerate(xs):
+            shape = x.shape
+            if len(shape) != 3 or shape[0] != n or shape[2] != d or x.dtype != dtype or dtype not in _DTYPES \
+                    or not x.is_cuda or x.device != dev:
+                raise ValueError(f"q and k must be [tokens, heads, {d}] float32 or bfloat16 CUDA tensors of one type")
+            xt, xh, xe = x.stride()
+            if outs is None:
+                o = torch.empty(shape, dtype=dtype, device=dev)
+                ot, oh, oe = shape[1] * d, d, 1
+            else:
+                o = outs[i]
+                if o.shape != shape or o.dtype != dtype or o.device != dev:
+                    raise ValueError("out must have the shape, type and device of its input")
+                ot, oh, oe = o.stride()
+            if xe != 1 or oe != 1:
+                raise ValueError("heads must be contiguous")
+            made.append(o)
+            fields += (x.data_ptr(), o.data_ptr(), shape[1], xt, xh, ot, oh)
         if positions is not None and (positions.dtype != torch.int64 or tuple(positions.shape) != (n,)
                                       or positions.device != dev or not positions.is_contiguous()):
             raise ValueError(f"positions must be a contiguous int64 tensor [{n}] on {dev}")
-        with torch.cuda.device(dev):
-            spectral_rotary(self.plan, _DTYPES[q.dtype], n, positions.data_ptr() if positions is not None else 0,
-                            int(start), int(inverse), heads, len(xs), torch.cuda.current_stream(dev).cuda_stream)
-        return outs[0] if k is None else outs
+        on_stream_of(dev, spectral_rotary, self.plan, _DTYPES[dtype], n, 0 if positions is None else positions.data_ptr(),
+                     start, 1 if inverse else 0, (ctypes.c_int64 * len(fields))(*fields), len(xs))
+        return made[0] if k is None else tuple(made)

@@ -186,7 +186,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.spectral_matmul_fp8.restype = ctypes.c_int
     lib.spectral_rotary_frequencies.argtypes = [ctypes.POINTER(sn_rotary), dp, dp]
     lib.spectral_rotary_frequencies.restype = ctypes.c_int
-    lib.spectral_rotary.argtypes = [ctypes.POINTER(sn_rotary), i32, i64, vp, i64, i32, ctypes.POINTER(sn_heads), i32, vp]
+    lib.spectral_rotary.argtypes = [ctypes.POINTER(sn_rotary), i32, i64, vp, i64, i32, vp, i32, vp]
     lib.spectral_rotary.restype = ctypes.c_int
     _lib = lib
     return lib
@@ -361,7 +361,7 @@ def spectral_rotary_frequencies(p: sn_rotary) -> tuple[list[float], float]:
 
 def spectral_rotary(p: sn_rotary, dtype: int, n_tokens: int, positions: int, first: int, inverse: int, heads,
                     n_heads: int, stream: int = 0) -> None:
-    """heads: a ctypes array of n_heads sn_heads."""
+    """heads: a ctypes array of n_heads sn_heads, or of their seven 64-bit fields in order."""
     _check(load_library().spectral_rotary(ctypes.byref(p), dtype, n_tokens, positions or None, first, inverse, heads,
                                           n_heads, stream or None))
 

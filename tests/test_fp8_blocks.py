@@ -158,9 +158,9 @@ def test_bad_products_are_refused(lib, code, kw):  # noqa: F811
     (sp.SN_ENULL, dict(a=0)), (sp.SN_ENULL, dict(sa=0)), (sp.SN_ENULL, dict(b=0)), (sp.SN_ENULL, dict(sb=0)),
     (sp.SN_ENULL, dict(c=0)), (sp.SN_EINVAL, dict(a=24)), (sp.SN_EINVAL, dict(b=8)), (sp.SN_EINVAL, dict(sa=18)),
     (sp.SN_EINVAL, dict(sb=2)), (sp.SN_EINVAL, dict(c=17)),
-    (sp.SN_ENULL, dict(p=dict(a_type=sp.SN_BF16), workspace=0)),
-    (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16), nbytes=16)), (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16), workspace=128)),
-    (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16), a=17))])
+    (sp.SN_ENULL, dict(p=dict(a_type=sp.SN_BF16, m=100), workspace=0)),
+    (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16, m=100), nbytes=16)), (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16, m=100), workspace=128)),
+    (sp.SN_EINVAL, dict(p=dict(a_type=sp.SN_BF16, m=100), a=17))])
 def test_bad_product_arguments_are_refused(lib, code, kw):  # noqa: F811
     a = dict(p={}, a=16, sa=16, b=16, sb=16, c=16, workspace=256, nbytes=1 << 30)
     a.update(kw)
