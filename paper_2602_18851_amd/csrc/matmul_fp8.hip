@@ -39,6 +39,7 @@ struct MatArgs {
   int64_t sa_block, sa_row, sb_block, sb_row;
   int32_t a_shift, b_shift;  // log2 of the rows that share a scale (0 or 7)
   int32_t tiles_m, tiles_n;
+  int32_t big;
   int32_t fa, fb, c_bf16;    // formats (1: E5M2) and C's type, for the kernels that take any
 };
 
@@ -224,6 +225,229 @@ __global__ void __launch_bounds__(256) matmul_kernel(MatArgs a) {
       const int64_t n = n0 + 16 * j + 4 * q;
       if (n < a.n)
         store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
+    }
+  }
+}
+
+// Large products: tiles of 256 x 256 by 8 waves of 128 x 64, two per SIMD. A step is
+// a block of 128 columns, two stages of 64 KB in LDS.  A stage is four half
+// tiles of 128 rows (A0, A1; B0, B1); a wave takes 64 rows of each A half and 32 of each
+// B half, so a step falls into four phases of one quadrant (64 x 32, 8 products of 16 x 16 x 128):
+//   phase           0        1        2        3
+//   reads           A0, s    B1       A1       B0 of step k + 1
+//   multiplies      A0 B0    A0 B1    A1 B1    A1 B0
+//   requests        B0       s, A0    B1       A1        (of step k + 2)
+// (s: the scales of the block, one of each row of A and B.)  A phase is a memory part
+// and a product part with a bare barrier after each, and waves 4-7 run half a phase
+// behind waves 0-3, so on every SIMD one wave multiplies while the other reads.
+// Nothing is read or refilled too early:
+//   - data of phase P were requested in phase P - 7; before the barrier that ends the memory part of phase
+//     P - 1 every wave waits until only what it requested after them is outstanding: six
+//     half tiles of two loads and the scales among them, 13 or 14;
+//   - a memory part ends with its reads complete, a barrier before any wave
+//     requests into their place.
+// Requests past the last step read nothing (an empty range; scales: the last block again)
+// and keep the count.
+constexpr int kBT = 256;
+constexpr int kBHalf = 128 * 128;
+constexpr int kBStage = 4 * kBHalf;
+
+__device__ __forceinline__ void big_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+// At most N vector-memory operations outstanding and every LDS read complete.
+template <int N>
+__device__ __forceinline__ void big_wait() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+}
+
+template <int FA, int FB, bool ROWS_B, typename TC>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) big_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t stage[2 * kBStage];
+  __shared__ float scales[2][2 * kBT];  // of the tile's rows of A, then of B
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int per_xcd = gridDim.x / 8;
+  const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
+  const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
+
+  // this wave stages rows 16 wv .. + 15 of every half tile.  Row r of B half h is row 64 (r / 32) + 32 h + r mod 32
+  // of the tile, so that a wave's 64 are one range.
+  const uint8_t* base[4];
+  uint32_t len[4];
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int64_t row = h < 2 ? bm * kBT + 128 * h + 16 * wv : bn * kBT + 64 * (wv >> 1) + 32 * (h & 1) + 16 * (wv & 1);
+    base[h] = h < 2 ? a.a + row * a.ld_a : a.b + row * a.ld_b;
+    len[h] = range_bytes(row, h < 2 ? a.m : a.n, 16, h < 2 ? a.ld_a : a.ld_b, a.k);
+  }
+  const uint32_t rb[2] = {(uint32_t)a.ld_a, (uint32_t)a.ld_b};
+  const int n_k = (int)((a.k + 127) / 128), n_full = (int)(a.k / 128);
+  const int sr = lane >> 3, p = lane & 7;
+  uint32_t voff[2][2];  // operand, row group of 8
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      voff[o][j] = (uint32_t)sr * rb[o] + 16u * (uint32_t)(p ^ stage_swz(16 * wv + 8 * j + sr));
+  auto issue = [&](int h, int k) {  // this wave's part of half tile h of step k
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base[h], k < n_k ? len[h] : 0u);
+    uint8_t* dst = stage + (k & 1) * kBStage + h * kBHalf + 2048 * wv;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + 1024 * j), 16, voff[h >> 1][j],
+                                               8u * j * rb[h >> 1] + 128u * (uint32_t)k, 0, 0);
+  };
+  // waves 0-3 stage the scales of 64 rows of A each, waves 4-7 of B; rows past the last take the last one's
+  const bool sc_a = wv < 4;
+  const int64_t sc_row0 = sc_a ? bm * kBT : bn * kBT, sc_rows = sc_a ? a.m : a.n, sc_step = sc_a ? a.sa_row : a.sb_row;
+  const int sc_shift = sc_a ? a.a_shift : a.b_shift;
+  const int64_t sc_at = min(sc_row0 + 64 * (wv & 3) + lane, sc_rows - 1) >> sc_shift;
+  const float* sc_base = (sc_a ? a.sa : a.sb) + (sc_row0 >> sc_shift) * sc_step;
+  const uint32_t sc_off = (uint32_t)((sc_at - (sc_row0 >> sc_shift)) * sc_step * 4);
+  const int64_t sc_block = sc_a ? a.sa_block : a.sb_block;
+  auto issue_scales = [&](int k) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(uni(sc_base + (k < n_k ? k : n_k - 1) * sc_block), 0x7fffffffu);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(scales[k & 1] + 64 * wv), 4, sc_off, 0, 0, 0);
+  };
+  enum { A0 = 0, A1 = 1, B0 = 2, B1 = 3 };
+
+  const int wm = wv >> 2, wn = wv & 3;  // 64 rows of each A half from 64 wm, 32 of each B half from 32 wn
+  f32x4 acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 fa[4][2], fb0[2][2], fb1[2][2], fbn[2][2];  // [16 rows][half of the block's columns]
+  float sa[8];                    // scale of row 128 (i / 4) + 64 wm + 16 (i % 4) + s, times B's where that is one
+  f32x4 sb[ROWS_B ? 4 : 1];       // scales of rows 64 wn + 16 j + 4 q .. + 3 of B
+  auto read_a = [&](int h, int k) {
+    const uint8_t* src = stage + (k & 1) * kBStage + h * kBHalf;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) fa[r][c] = stage_chunk(src, 64 * wm + 16 * r + s, 4 * c + q);
+  };
+  auto read_b = [&](u32x4 (&f)[2][2], int h, int k) {
+    const uint8_t* src = stage + (k & 1) * kBStage + h * kBHalf;
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) f[r][c] = stage_chunk(src, 32 * wn + 16 * r + s, 4 * c + q);
+  };
+  auto read_scales = [&](int k) {
+    const float* src = scales[k & 1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sa[i] = src[128 * (i >> 2) + 64 * wm + 16 * (i & 3) + s];
+    if constexpr (ROWS_B) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sb[j] = *reinterpret_cast<const f32x4*>(src + kBT + 64 * wn + 16 * j + 4 * q);
+    } else {
+      const float b = src[kBT + 64 * wn];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sa[i] *= b;
+    }
+  };
+  // zeroes columns >= k of operands of the ragged step
+  auto mask = [&](auto& f) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int keep = (int)(a.k - (int64_t)n_full * 128) - 16 * (4 * c + q);
+#pragma unroll
+      for (auto& x : f) keep_chunk(x[c], keep);
+    }
+  };
+  auto products = [&](int i0, int j0, const u32x4 (&fb)[2][2]) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const f32x4 part = block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1]));
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i0 + i][j0 + j][e] = fmaf(part[e], ROWS_B ? sa[i0 + i] * sb[j0 + j][e] : sa[i0 + i], acc[i0 + i][j0 + j][e]);
+      }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  auto step = [&](int k, auto ragged_tag) {
+    constexpr bool RAGGED = decltype(ragged_tag)::value;
+    // phase 0
+    read_a(A0, k);
+    read_scales(k);
+    issue(B0, k + 2);
+    big_wait<13>();
+    big_barrier();
+    if constexpr (RAGGED) {
+      mask(fa);
+      mask(fb0);
+    }
+    products(0, 0, fb0);
+    big_barrier();
+    // phase 1
+    read_b(fb1, B1, k);
+    issue_scales(k + 2);
+    issue(A0, k + 2);
+    big_wait<14>();
+    big_barrier();
+    if constexpr (RAGGED) mask(fb1);
+    products(0, 2, fb1);
+    big_barrier();
+    // phase 2
+    read_a(A1, k);
+    issue(B1, k + 2);
+    big_wait<14>();
+    big_barrier();
+    if constexpr (RAGGED) mask(fa);
+    products(4, 2, fb1);
+    big_barrier();
+    // phase 3
+    read_b(fbn, B0, k + 1);
+    issue(A1, k + 2);
+    big_wait<13>();
+    big_barrier();
+    products(4, 0, fb0);
+    big_barrier();
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) fb0[r][c] = fbn[r][c];
+  };
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    issue(B0, k);
+    issue_scales(k);
+    issue(A0, k);
+    issue(B1, k);
+    issue(A1, k);
+  }
+  big_wait<13>();  // B0, the scales and A0 of step 0
+  big_barrier();
+  read_b(fb0, B0, 0);
+  big_wait<13>();
+  big_barrier();
+  if (wm == 1) big_barrier();  // waves 4-7: half a phase behind
+#pragma unroll 1
+  for (int k = 0; k < n_full; ++k) step(k, std::false_type{});
+  if (n_full < n_k) step(n_full, std::true_type{});
+  if (wm == 0) big_barrier();
+  big_wait<0>();  // the last loads have left the LDS alone before the workgroup gives it up
+
+  // lane: row 128 (i / 4) + 64 wm + 16 (i % 4) + s, columns 64 wn + 16 j + 4 q .. + 3
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t m = bm * kBT + 128 * (i >> 2) + 64 * wm + 16 * (i & 3) + s;
+    if (m >= a.m) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t n = bn * kBT + 64 * wn + 16 * j + 4 * q;
+      if (n < a.n) store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
     }
   }
 }
@@ -433,7 +657,14 @@ __global__ void __launch_bounds__(64 * kFewWaves, TM * TN == 1 ? 4 : 2) few_rows
 }
 
 template <int FA, int FB, bool ROWS_B>
-void launch2(const MatArgs& a, bool bf16, hipStream_t st) {
+void launch2(const MatArgs& args, bool bf16, hipStream_t st) {
+  MatArgs a = args;
+  if (a.big && bf16) {
+    a.tiles_m = (int32_t)((a.m + kBT - 1) / kBT);
+    a.tiles_n = (int32_t)((a.n + kBT - 1) / kBT);
+    big_kernel<FA, FB, ROWS_B, __bf16><<<dim3((uint32_t)(((a.tiles_m * a.tiles_n + 7) / 8) * 8)), 512, 0, st>>>(a);
+    return;
+  }
   const dim3 grid((uint32_t)(((a.tiles_m * a.tiles_n + 7) / 8) * 8));
   if (bf16)
     matmul_kernel<FA, FB, ROWS_B, __bf16><<<grid, 256, 0, st>>>(a);
@@ -618,6 +849,7 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
     g.sa_block = p.m;
     g.sa_row = 1;
   }
+  g.big = p.m >= 512 && p.n >= 512 && p.k >= 128 && p.sa_row < (1 << 20) && p.sb_row < (1 << 20);
   if (pl.few) {
     const int plain = !pl.fuse ? 0 : p.a_type == SN_BF16 ? 1 : 2;
     if (g.fa)

@@ -179,7 +179,12 @@ def test_products(m, n, k, ra, rb, out):
     assert torch.equal(got, matmul_fp8(a, b, out_dtype=TORCH[out]))  # the same bits again
 
 
-@pytest.mark.parametrize("m,n,k", PRODUCTS)
+# sizes at which tiles, rounds of workgroups and splits of the sum change
+LARGE = [(512, 512, 128), (520, 515, 130), (1000, 777, 1000), (513, 1300, 2048), (600, 4100, 257), (2050, 640, 390),
+         (520, 600, 9000), (300, 520, 20000), (70, 300, 6000), (129, 2000, 4097)]
+
+
+@pytest.mark.parametrize("m,n,k", PRODUCTS + LARGE)
 @pytest.mark.parametrize("ra,rb", [(1, 128), (1, 1), (128, 128)])
 @pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
@@ -197,6 +202,17 @@ def test_products_of_whole_numbers_are_exact(m, n, k, ra, rb, fa, out):
         vals.append(fp8_blocks.values(v, scale, br))
     ref = torch.from_numpy((vals[0] @ vals[1].T).astype(np.float32)).to(TORCH[out])
     assert torch.equal(matmul_fp8(*mats, out_dtype=TORCH[out]).cpu(), ref)
+
+
+@pytest.mark.parametrize("m,n,k", LARGE)
+@pytest.mark.parametrize("ra,rb", [(1, 128), (1, 1), (128, 1)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_large_products(m, n, k, ra, rb, out):
+    a, av = matrix((31, m, k), m, k, "e4m3", ra)
+    b, bv = matrix((32, n, k), n, k, "e4m3", rb)
+    got = matmul_fp8(a, b, out_dtype=TORCH[out])
+    check_product(got, av, bv, out)
+    assert torch.equal(got, matmul_fp8(a, b, out_dtype=TORCH[out]))
 
 
 @pytest.mark.parametrize("fa,fb", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
