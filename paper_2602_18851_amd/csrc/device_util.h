@@ -59,15 +59,16 @@ __device__ __forceinline__ int stage_swz(int r) { return ((r >> 1) & 7) ^ ((r >>
 
 // Issues the loads of one tile: row r of the resource starts at byte
 // r * row_bytes; the tile takes columns [col_byte, col_byte + 128).  AUX is the
-// cache policy of the loads.
+// cache policy of the loads.  row0: the row of the staged tile that the first one
+// is (a multiple of 8).
 template <int R, int AUX>
 __device__ __forceinline__ void stage_issue(__amdgpu_buffer_rsrc_t rsrc, uint8_t* lds, uint32_t col_byte,
-                                            uint32_t row_bytes, int lane) {
+                                            uint32_t row_bytes, int lane, int row0 = 0) {
   const int sr = lane >> 3, p = lane & 7;
 #pragma unroll
   for (int j = 0; j < R / 8; ++j) {
     const int r = 8 * j + sr;
-    const uint32_t voff = (uint32_t)sr * row_bytes + col_byte + 16u * (uint32_t)(p ^ stage_swz(r));
+    const uint32_t voff = (uint32_t)sr * row_bytes + col_byte + 16u * (uint32_t)(p ^ stage_swz(row0 + r));
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(lds + 1024 * j), 16, voff, 8u * j * row_bytes, 0,
                                              AUX);
   }

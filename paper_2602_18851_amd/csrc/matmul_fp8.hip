@@ -39,6 +39,9 @@ struct MatArgs {
   int64_t sa_block, sa_row, sb_block, sb_row;
   int32_t a_shift, b_shift;  // log2 of the rows that share a scale (0 or 7)
   int32_t tiles_m, tiles_n;
+  int32_t splits, blocks_per_split;  // workgroups that share a tile's sum over k, and the 128-column blocks of each
+  float* parts;                      // their sums [splits][m][ld_parts], with splits > 1
+  int64_t ld_parts;
   int32_t big;
   int32_t fa, fb, c_bf16;    // formats (1: E5M2) and C's type, for the kernels that take any
 };
@@ -105,65 +108,71 @@ __device__ __forceinline__ void store4(TC* p, const f32x4& v, int n) {
     if (e < n) p[e] = (TC)v[e];
 }
 
-// Tiles of 128 x 128 by 4 waves of 64 x 64.  Blocks of 128 columns come through two LDS
-// stages of 32 KB, the next requested before the current one is multiplied.
-// The products are formed transposed (rows from B): a lane holds four
-// neighbouring columns of one row of C, with one scale of A.
-constexpr int kT = 128;
+__device__ __forceinline__ void bare_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+// At most N vector-memory operations outstanding and every LDS read complete.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+}
 
-template <int FA, int FB, bool ROWS_B, typename TC>
-__global__ void __launch_bounds__(256) matmul_kernel(MatArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t stage[2][2 * kT * 128];
+// Tiles of (64 WM) x (64 WN) by WM x WN waves of 64 x 64.  Blocks of 128 columns and their
+// scales come through STAGES stages in LDS, requested STAGES - 1 blocks ahead.  The products are
+// formed transposed (rows from B): a lane holds four neighbouring columns of one row
+// of C, with one scale of A.
+template <int FA, int FB, bool ROWS_B, typename TC, int WM, int WN, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(MatArgs a) {
+  constexpr int BM = 64 * WM, BN = 64 * WN, NW = WM * WN, ROWS = BM + BN;
+  constexpr int PM = BM / NW, PN = BN / NW;  // rows of A and of B a wave stages
+  constexpr int SCL = ROWS / 64;             // waves that stage scales, 64 rows each
+  constexpr int STAGE = ROWS * 128 + ROWS * 4;
+  static_assert(PM % 8 == 0 && PN % 8 == 0 && SCL <= NW, "staging splits evenly over the waves");
+  // One array: with two, the compiler waits for every load into LDS before it reads either.
+  __shared__ __attribute__((aligned(16))) uint8_t stage[STAGES * STAGE];
   const int lane = threadIdx.x & 63;
   const int wv = uni((int)(threadIdx.x >> 6));
   const int q = lane >> 4, s = lane & 15;
   const int per_xcd = gridDim.x / 8;
-  const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-  if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
+  const int unit = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (unit >= a.tiles_m * a.tiles_n * a.splits) return;  // whole workgroup
+  const int tile = unit / a.splits, split = unit % a.splits;
   const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
 
-  const int64_t am = bm * kT + 32 * wv, bnr = bn * kT + 32 * wv;  // rows this wave stages
-  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, 32, a.ld_a, a.k));
-  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.b + bnr * a.ld_b, range_bytes(bnr, a.n, 32, a.ld_b, a.k));
+  const int64_t am = bm * BM + PM * wv, bnr = bn * BN + PN * wv;  // rows this wave stages
+  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, PM, a.ld_a, a.k));
+  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.b + bnr * a.ld_b, range_bytes(bnr, a.n, PN, a.ld_b, a.k));
+  // scales of rows 64 wv .. + 63; rows past the last take the last one's
+  const bool sc_a = 64 * wv < BM;
+  const int64_t sc_row0 = sc_a ? bm * BM + 64 * wv : bn * BN + 64 * wv - BM, sc_rows = sc_a ? a.m : a.n;
+  const float* sc_at = (sc_a ? a.sa : a.sb) +
+                       (min(sc_row0 + lane, sc_rows - 1) >> (sc_a ? a.a_shift : a.b_shift)) * (sc_a ? a.sa_row : a.sb_row);
+  const int64_t sc_block = sc_a ? a.sa_block : a.sb_block;
   auto issue = [&](int kb) {
-    uint8_t* dst = stage[kb & 1] + 4096 * wv;
-    stage_issue<32, 0>(ra, dst, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane);
-    stage_issue<32, 0>(rb, dst + kT * 128, 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane);
+    uint8_t* st = stage + kb % STAGES * STAGE;
+    stage_issue<PM, 0>(ra, st + 128 * PM * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane, PM * wv);
+    stage_issue<PN, 0>(rb, st + 128 * (BM + PN * wv), 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane, PN * wv);
+    if (wv < SCL)
+      __builtin_amdgcn_global_load_lds(sc_at + kb * sc_block, (lds_void*)(st + 128 * ROWS + 256 * wv), 4, 0, 0);
   };
 
-  const int wm = wv >> 1, wn = wv & 1;
-  const int64_t m0 = bm * kT + 64 * wm, n0 = bn * kT + 64 * wn;
-  // scales of this lane's rows; rows past the last read the last one's, their results are dropped
-  const float* pa[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) pa[i] = a.sa + (min(m0 + 16 * i + s, a.m - 1) >> a.a_shift) * a.sa_row;
-  const float* pb[ROWS_B ? 16 : 1];
-  if constexpr (ROWS_B) {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) pb[j] = a.sb + min(n0 + 16 * (j >> 2) + 4 * q + (j & 3), a.n - 1) * a.sb_row;
-  } else {
-    pb[0] = a.sb + (min(n0, a.n - 1) >> 7) * a.sb_row;
-  }
-
+  const int wm = wv / WN, wn = wv % WN;
   f32x4 acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int n_kb = (int)((a.k + 127) / 128);
-  if (n_kb > 0) issue(0);
-#pragma unroll 1
-  for (int kb = 0; kb < n_kb; ++kb) {
-    float sa[4], sb[ROWS_B ? 16 : 1];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sa[i] = pa[i][kb * a.sa_block];
-#pragma unroll
-    for (int j = 0; j < (ROWS_B ? 16 : 1); ++j) sb[j] = pb[j][kb * a.sb_block];
-    __builtin_amdgcn_s_waitcnt(0);  // this wave's part of block kb is in LDS
-    __syncthreads();                // every part, and block kb - 1 fully read
-    if (kb + 1 < n_kb) issue(kb + 1);
-    const uint8_t* ta = stage[kb & 1];
-    const uint8_t* tb = ta + kT * 128;
+  // this workgroup's blocks of columns; the last of all may be ragged
+  const int kb0 = split * a.blocks_per_split, n_kb = min((int)((a.k + 127) / 128), kb0 + a.blocks_per_split);
+  auto block = [&](int kb, auto last_tag) {
+    constexpr bool LAST = decltype(last_tag)::value;  // columns from k on are whatever the rows hold there
+    const uint8_t* ta = stage + kb % STAGES * STAGE;
+    const uint8_t* tb = ta + BM * 128;
+    const float* sc = reinterpret_cast<const float*>(ta + 128 * ROWS);
     u32x4 fa[4][2], fb[4][2];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -171,59 +180,99 @@ __global__ void __launch_bounds__(256) matmul_kernel(MatArgs a) {
       for (int h = 0; h < 2; ++h) {
         fa[r][h] = stage_chunk(ta, 64 * wm + 16 * r + s, 4 * h + q);
         fb[r][h] = stage_chunk(tb, 64 * wn + 16 * r + s, 4 * h + q);
-      }
-    if (kb + 1 == n_kb) {  // columns from k on are whatever the rows hold there
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        if constexpr (LAST) {
+          const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
           keep_chunk(fa[r][h], keep);
           keep_chunk(fb[r][h], keep);
         }
       }
+    float sa[4];
+    f32x4 sb[ROWS_B ? 4 : 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sa[i] = sc[64 * wm + 16 * i + s];
+    if constexpr (ROWS_B) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sb[j] = *reinterpret_cast<const f32x4*>(sc + BM + 64 * wn + 16 * j + 4 * q);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sa[i] *= sc[BM + 64 * wn];
     }
-    f32x4 part[4][4];
+    auto add = [&](int i, int j, const f32x4& part) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[e], ROWS_B ? sa[i] * sb[j][e] : sa[i], acc[i][j][e]);
+    };
     if constexpr (sizeof(TC) == 2) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          part[i][j] = block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1]));
+          add(i, j, block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1])));
     } else {
+      // two columns of 16 x 16 blocks at a time: their sums and codes as float16 stay in registers
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        f16x8 ha[4], hb[4];
+      for (int jj = 0; jj < 4; jj += 2) {
+        f32x4 part[4][2];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          ha[r] = widen<FA>(fa[r][h >> 1][2 * (h & 1)], fa[r][h >> 1][2 * (h & 1) + 1]);
-          hb[r] = widen<FB>(fb[r][h >> 1][2 * (h & 1)], fb[r][h >> 1][2 * (h & 1) + 1]);
+        for (int h = 0; h < 4; ++h) {
+          const int w = 2 * (h & 1);
+          f16x8 hb[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) hb[j] = widen<FB>(fb[jj + j][h >> 1][w], fb[jj + j][h >> 1][w + 1]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f16x8 ha = widen<FA>(fa[i][h >> 1][w], fa[i][h >> 1][w + 1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+              part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                  hb[j], ha, h == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[i][j], 0, 0, 0);
+          }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                hb[j], ha[i], h == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[i][j], 0, 0, 0);
+          for (int j = 0; j < 2; ++j) add(i, jj + j, part[i][j]);
       }
     }
+  };
+  // Loads of a wave per block: one for 8 rows, and one of scales in the first SCL waves.  Block kb has landed when
+  // at most those of the STAGES - 2 blocks after it are outstanding.
+  constexpr int OWN = (PM + PN) / 8;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc[i][j][e] = fmaf(part[i][j][e], sa[i] * sb[ROWS_B ? 4 * j + e : 0], acc[i][j][e]);
+  for (int kb = 0; kb < STAGES - 1; ++kb)
+    if (kb0 + kb < n_kb) issue(kb0 + kb);
+  auto landed = [&](int kb) {
+    const int ahead = min(STAGES - 2, n_kb - 1 - kb);  // blocks requested after it
+    if (ahead == 0)
+      wait_loads<0>();
+    else if (wv < SCL)
+      wait_loads<OWN + 1>();
+    else
+      wait_loads<OWN>();
+    bare_barrier();  // every wave's part of it, and block kb - 1 fully read
+  };
+  static_assert(STAGES <= 3, "one block at most between the awaited one and the newest");
+#pragma unroll 1
+  for (int kb = kb0; kb + 1 < n_kb; ++kb) {
+    landed(kb);
+    if (kb + STAGES - 1 < n_kb) issue(kb + STAGES - 1);
+    block(kb, std::false_type{});
+  }
+  if (n_kb > kb0) {
+    landed(n_kb - 1);
+    block(n_kb - 1, std::true_type{});
   }
 
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + 16 * i + s;
+    const int64_t m = bm * BM + 64 * wm + 16 * i + s;
     if (m >= a.m) continue;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + 16 * j + 4 * q;
-      if (n < a.n)
+      const int64_t n = bn * BN + 64 * wn + 16 * j + 4 * q;
+      if (n >= a.n) continue;
+      if (a.splits > 1)  // rows of the parts are whole groups of four
+        *reinterpret_cast<f32x4*>(a.parts + ((int64_t)split * a.m + m) * a.ld_parts + n) = acc[i][j];
+      else
         store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
     }
   }
@@ -252,23 +301,12 @@ constexpr int kBT = 256;
 constexpr int kBHalf = 128 * 128;
 constexpr int kBStage = 4 * kBHalf;
 
-__device__ __forceinline__ void big_barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("" ::: "memory");
-}
-// At most N vector-memory operations outstanding and every LDS read complete.
-template <int N>
-__device__ __forceinline__ void big_wait() {
-  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
-}
-
-template <int FA, int FB, bool ROWS_B, typename TC>
+template <int FA, int FB, bool ROWS_B>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) big_kernel(MatArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t stage[2 * kBStage];
-  __shared__ float scales[2][2 * kBT];  // of the tile's rows of A, then of B
+  // two stages, then of each the scales of the tile's rows of A and of B; one array: with two, the compiler waits
+  // for every load into LDS before it reads either
+  __shared__ __attribute__((aligned(16))) uint8_t stage[2 * kBStage + 2 * 2 * kBT * 4];
+  float* const scales = reinterpret_cast<float*>(stage + 2 * kBStage);
   const int lane = threadIdx.x & 63;
   const int wv = uni((int)(threadIdx.x >> 6));
   const int q = lane >> 4, s = lane & 15;
@@ -314,7 +352,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int64_t sc_block = sc_a ? a.sa_block : a.sb_block;
   auto issue_scales = [&](int k) {
     const __amdgpu_buffer_rsrc_t r = make_rsrc(uni(sc_base + (k < n_k ? k : n_k - 1) * sc_block), 0x7fffffffu);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(scales[k & 1] + 64 * wv), 4, sc_off, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(scales + (k & 1) * 2 * kBT + 64 * wv), 4, sc_off, 0, 0, 0);
   };
   enum { A0 = 0, A1 = 1, B0 = 2, B1 = 3 };
 
@@ -342,7 +380,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
       for (int c = 0; c < 2; ++c) f[r][c] = stage_chunk(src, 32 * wn + 16 * r + s, 4 * c + q);
   };
   auto read_scales = [&](int k) {
-    const float* src = scales[k & 1];
+    const float* src = scales + (k & 1) * 2 * kBT;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sa[i] = src[128 * (i >> 2) + 64 * wm + 16 * (i & 3) + s];
     if constexpr (ROWS_B) {
@@ -382,38 +420,38 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     read_a(A0, k);
     read_scales(k);
     issue(B0, k + 2);
-    big_wait<13>();
-    big_barrier();
+    wait_loads<13>();
+    bare_barrier();
     if constexpr (RAGGED) {
       mask(fa);
       mask(fb0);
     }
     products(0, 0, fb0);
-    big_barrier();
+    bare_barrier();
     // phase 1
     read_b(fb1, B1, k);
     issue_scales(k + 2);
     issue(A0, k + 2);
-    big_wait<14>();
-    big_barrier();
+    wait_loads<14>();
+    bare_barrier();
     if constexpr (RAGGED) mask(fb1);
     products(0, 2, fb1);
-    big_barrier();
+    bare_barrier();
     // phase 2
     read_a(A1, k);
     issue(B1, k + 2);
-    big_wait<14>();
-    big_barrier();
+    wait_loads<14>();
+    bare_barrier();
     if constexpr (RAGGED) mask(fa);
     products(4, 2, fb1);
-    big_barrier();
+    bare_barrier();
     // phase 3
     read_b(fbn, B0, k + 1);
     issue(A1, k + 2);
-    big_wait<13>();
-    big_barrier();
+    wait_loads<13>();
+    bare_barrier();
     products(4, 0, fb0);
-    big_barrier();
+    bare_barrier();
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -427,17 +465,17 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     issue(B1, k);
     issue(A1, k);
   }
-  big_wait<13>();  // B0, the scales and A0 of step 0
-  big_barrier();
+  wait_loads<13>();  // B0, the scales and A0 of step 0
+  bare_barrier();
   read_b(fb0, B0, 0);
-  big_wait<13>();
-  big_barrier();
-  if (wm == 1) big_barrier();  // waves 4-7: half a phase behind
+  wait_loads<13>();
+  bare_barrier();
+  if (wm == 1) bare_barrier();  // waves 4-7: half a phase behind
 #pragma unroll 1
   for (int k = 0; k < n_full; ++k) step(k, std::false_type{});
   if (n_full < n_k) step(n_full, std::true_type{});
-  if (wm == 0) big_barrier();
-  big_wait<0>();  // the last loads have left the LDS alone before the workgroup gives it up
+  if (wm == 0) bare_barrier();
+  wait_loads<0>();  // the last loads have left the LDS alone before the workgroup gives it up
 
   // lane: row 128 (i / 4) + 64 wm + 16 (i % 4) + s, columns 64 wn + 16 j + 4 q .. + 3
 #pragma unroll
@@ -447,7 +485,7 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int64_t n = bn * kBT + 64 * wn + 16 * j + 4 * q;
-      if (n < a.n) store4(static_cast<TC*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
+      if (n < a.n) store4(static_cast<__bf16*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
     }
   }
 }
@@ -656,20 +694,41 @@ __global__ void __launch_bounds__(64 * kFewWaves, TM * TN == 1 ? 4 : 2) few_rows
   }
 }
 
+// Adds the parts of C, in order, and rounds once.
+template <typename TC>
+__global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
+  const int64_t per_row = a.ld_parts / 4, all = a.m * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / per_row, n = 4 * (i % per_row);
+    const float* p = a.parts + m * a.ld_parts + n;
+    f32x4 r = *reinterpret_cast<const f32x4*>(p);
+    for (int z = 1; z < a.splits; ++z) r += *reinterpret_cast<const f32x4*>(p + z * a.m * a.ld_parts);
+    store4(static_cast<TC*>(a.c) + m * a.ld_c + n, r, (int)min(a.n - n, (int64_t)4));
+  }
+}
+
 template <int FA, int FB, bool ROWS_B>
 void launch2(const MatArgs& args, bool bf16, hipStream_t st) {
   MatArgs a = args;
-  if (a.big && bf16) {
-    a.tiles_m = (int32_t)((a.m + kBT - 1) / kBT);
-    a.tiles_n = (int32_t)((a.n + kBT - 1) / kBT);
-    big_kernel<FA, FB, ROWS_B, __bf16><<<dim3((uint32_t)(((a.tiles_m * a.tiles_n + 7) / 8) * 8)), 512, 0, st>>>(a);
+  auto tiles = [&](int t) {
+    a.tiles_m = (int32_t)((a.m + t - 1) / t);
+    a.tiles_n = (int32_t)((a.n + t - 1) / t);
+    return dim3((uint32_t)(((int64_t)a.tiles_m * a.tiles_n * a.splits + 7) / 8 * 8));
+  };
+  if (a.big) {
+    const dim3 g = tiles(kBT);
+    big_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
     return;
   }
-  const dim3 grid((uint32_t)(((a.tiles_m * a.tiles_n + 7) / 8) * 8));
+  const dim3 g = tiles(128);
   if (bf16)
-    matmul_kernel<FA, FB, ROWS_B, __bf16><<<grid, 256, 0, st>>>(a);
+    tile_kernel<FA, FB, ROWS_B, __bf16, 2, 2, 2><<<g, 256, 0, st>>>(a);
   else
-    matmul_kernel<FA, FB, ROWS_B, float><<<grid, 256, 0, st>>>(a);
+    tile_kernel<FA, FB, ROWS_B, float, 2, 2, 2><<<g, 256, 0, st>>>(a);
+  if (a.splits > 1) {
+    const dim3 j((uint32_t)std::min<int64_t>((a.m * (a.ld_parts / 4) + 255) / 256, 4096));
+    bf16 ? join_kernel<__bf16><<<j, 256, 0, st>>>(a) : join_kernel<float><<<j, 256, 0, st>>>(a);
+  }
 }
 
 template <int FA, int FB>
@@ -719,7 +778,44 @@ void launch_few(const MatArgs& a, int plain, hipStream_t st) {
   }
 }
 
+// The kernel of a product of more than kFewRows rows, and over how many workgroups a tile's sum
+// is split: the cheapest by these costs in us.  A 256 x 256 tile takes 2.03 for a block of 128 columns,
+// one workgroup per compute unit (8192^3: 522 us); a 128 x 128 tile alone on its
+// unit 0.77 (256 x 8192 x 8192: 51 us), two of them 1.21 (1024 x 8192 x 8192: 79
+// us, by the large tiles 112), for a float32 C 1.2 and 2.15.  Parts are
+// written, read and joined at 5.5 TB/s in a launch more: 512 x 512 x 16384 takes 95 us in
+// one part, 53, 31 and 22 in 2, 4 and 8; 512 x 8192 x 8192 51 in one part, 53 in two.
+struct Way {
+  bool big;
+  int splits, blocks_per_split;
+};
+
+Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
+  auto up = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
+  const int64_t n_kb = up(k, 128), small = up(m, 128) * up(n, 128);
+  Way best{false, 1, (int)n_kb};
+  double cost = 1e30;
+  if (!f32 && n_kb > 0) {
+    best.big = true;
+    cost = 2.03 * (double)up(up(m, kBT) * up(n, kBT), 256) * (double)n_kb;
+  }
+  const double alone = f32 ? 1.2 : 0.77, both = f32 ? 2.15 : 1.21;
+  for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= n_kb); ++s) {
+    const int64_t per = up(n_kb, s), wgs = small * s, rest = wgs % 512;
+    if (s > 1 && (s - 1) * per >= n_kb) continue;  // a split without blocks
+    double c = (double)per * ((double)(wgs / 512) * both + (rest == 0 ? 0.0 : rest <= 256 ? alone : both));
+    if (s > 1) c += 2.5 + (double)(8 * s + (f32 ? 4 : 2)) * (double)m * (double)n / 5.5e6;
+    if (c < cost) {
+      cost = c;
+      best = Way{false, (int)s, (int)per};
+    }
+  }
+  return best;
+}
+
 struct MatPlan {
+  Way way;
+  int64_t off_parts, ld_parts;
   bool plain_a;
   bool few;   // the kernel for few rows
   bool fuse;  // ... which quantises a plain A itself
@@ -759,7 +855,7 @@ int resolve(sn_matmul& p, MatPlan& pl) {
   if (p.sa_block < 0 || p.sa_row < 0 || p.sb_block < 0 || p.sb_row < 0 || p.sa_block > kMost || p.sa_row > kMost ||
       p.sb_block > kMost || p.sb_row > kMost)
     return refuse(SN_EINVAL, "scale strides must be >= 0 and below 2^40");
-  if (((p.m + kT - 1) / kT) * ((p.n + kT - 1) / kT) >= (int64_t(1) << 30))
+  if (((p.m + 127) / 128) * ((p.n + 127) / 128) >= (int64_t(1) << 30))
     return refuse(SN_EINVAL, "m x n must stay below 2^30 tiles of 128 x 128");
   if (plain && ((p.m + 127) / 128) * ((p.k + 127) / 128) >= (int64_t(1) << 31))
     return refuse(SN_EINVAL, "a plain A must stay below 2^31 tiles of 128 x 128");
@@ -771,6 +867,15 @@ int resolve(sn_matmul& p, MatPlan& pl) {
     pl.ld_codes = round_up(p.k, 16);
     pl.off_scale = round_up(p.m * pl.ld_codes, 256);
     pl.bytes = pl.off_scale + round_up(p.m * ((p.k + 127) / 128) * 4, 256);
+  }
+  if (!pl.few) {
+    pl.way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
+    if (pl.way.big && (p.sa_row >= (1 << 20) || p.sb_row >= (1 << 20))) pl.way.big = false;
+    if (pl.way.splits > 1) {
+      pl.off_parts = pl.bytes;
+      pl.ld_parts = round_up(p.n, 4);
+      pl.bytes += round_up(pl.way.splits * p.m * pl.ld_parts * 4, 256);
+    }
   }
   return SN_OK;
 }
@@ -826,8 +931,6 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
   g.sb_row = p.sb_row;
   g.a_shift = p.a_block_rows == 128 ? 7 : 0;
   g.b_shift = p.b_block_rows == 128 ? 7 : 0;
-  g.tiles_m = (int32_t)((p.m + kT - 1) / kT);
-  g.tiles_n = (int32_t)((p.n + kT - 1) / kT);
   g.fa = p.a_type == SN_E5M2;
   g.fb = p.b_type == SN_E5M2;
   g.c_bf16 = p.c_type == SN_BF16;
@@ -849,7 +952,11 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
     g.sa_block = p.m;
     g.sa_row = 1;
   }
-  g.big = p.m >= 512 && p.n >= 512 && p.k >= 128 && p.sa_row < (1 << 20) && p.sb_row < (1 << 20);
+  g.big = pl.way.big;
+  g.splits = pl.way.splits;
+  g.blocks_per_split = pl.way.blocks_per_split;
+  g.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.off_parts);
+  g.ld_parts = pl.ld_parts;
   if (pl.few) {
     const int plain = !pl.fuse ? 0 : p.a_type == SN_BF16 ? 1 : 2;
     if (g.fa)
