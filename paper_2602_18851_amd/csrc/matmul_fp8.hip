@@ -278,28 +278,27 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(MatArgs a) {
   }
 }
 
-// Large products: tiles of 256 x 256 by 8 waves of 128 x 64, two per SIMD. A step is
-// a block of 128 columns, two stages of 64 KB in LDS.  A stage is four half
-// tiles of 128 rows (A0, A1; B0, B1); a wave takes 64 rows of each A half and 32 of each
-// B half, so a step falls into four phases of one quadrant (64 x 32, 8 products of 16 x 16 x 128):
-//   phase           0        1        2        3
-//   reads           A0, s    B1       A1       B0 of step k + 1
-//   multiplies      A0 B0    A0 B1    A1 B1    A1 B0
-//   requests        B0       s, A0    B1       A1        (of step k + 2)
-// (s: the scales of the block, one of each row of A and B.)  A phase is a memory part
-// and a product part with a bare barrier after each, and waves 4-7 run half a phase
-// behind waves 0-3, so on every SIMD one wave multiplies while the other reads.
+// Large products: tiles of 256 x 256 by 8 waves of 128 x 64, two per SIMD.  A step is
+// a block of 128 columns, two stages of 64 KB in LDS and the scales of its rows
+// of A and B.  A wave takes 64 rows of each half (128 rows) of A and 64 rows of B,
+// so a step falls into two phases of 64 x 64 (16 products of 16 x 16 x 128):
+//   phase           0                    1
+//   reads           A0, B, scales        A1
+//   multiplies      A0 B                 A1 B
+//   requests        A1 of step k + 1     A0, B and scales of step k + 2
+// A phase is a memory part and a product part with a bare barrier after each, and
+// waves 4-7 run half a phase behind waves 0-3, so on every SIMD one wave multiplies
+// while the other reads.  (With four phases of 64 x 32, 8192^3 took KFOUR us.)
 // Nothing is read or refilled too early:
-//   - data of phase P were requested in phase P - 7; before the barrier that ends the memory part of phase
-//     P - 1 every wave waits until only what it requested after them is outstanding: six
-//     half tiles of two loads and the scales among them, 13 or 14;
+//   - before the barrier that ends a memory part every wave waits until what the next phase reads has landed. That
+//     was requested two phases before it: since then 9 loads, of the two phases after, are outstanding at most;
 //   - a memory part ends with its reads complete, a barrier before any wave
 //     requests into their place.
 // Requests past the last step read nothing (an empty range; scales: the last block again)
 // and keep the count.
 constexpr int kBT = 256;
 constexpr int kBHalf = 128 * 128;
-constexpr int kBStage = 4 * kBHalf;
+constexpr int kBStage = 4 * kBHalf;  // A0, A1, B
 
 template <int FA, int FB, bool ROWS_B>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) big_kernel(MatArgs a) {
@@ -315,13 +314,12 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
   const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
 
-  // this wave stages rows 16 wv .. + 15 of every half tile.  Row r of B half h is row 64 (r / 32) + 32 h + r mod 32
-  // of the tile, so that a wave's 64 are one range.
+  // this wave stages rows 16 wv .. + 15 of every 128
   const uint8_t* base[4];
   uint32_t len[4];
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
-    const int64_t row = h < 2 ? bm * kBT + 128 * h + 16 * wv : bn * kBT + 64 * (wv >> 1) + 32 * (h & 1) + 16 * (wv & 1);
+    const int64_t row = (h < 2 ? bm : bn) * kBT + 128 * (h & 1) + 16 * wv;
     base[h] = h < 2 ? a.a + row * a.ld_a : a.b + row * a.ld_b;
     len[h] = range_bytes(row, h < 2 ? a.m : a.n, 16, h < 2 ? a.ld_a : a.ld_b, a.k);
   }
@@ -356,28 +354,21 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   enum { A0 = 0, A1 = 1, B0 = 2, B1 = 3 };
 
-  const int wm = wv >> 2, wn = wv & 3;  // 64 rows of each A half from 64 wm, 32 of each B half from 32 wn
+  const int wm = wv >> 2, wn = wv & 3;  // 64 rows of each A half from 64 wm, of B from 64 wn
   f32x4 acc[8][4];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 fa[4][2], fb0[2][2], fb1[2][2], fbn[2][2];  // [16 rows][half of the block's columns]
-  float sa[8];                    // scale of row 128 (i / 4) + 64 wm + 16 (i % 4) + s, times B's where that is one
-  f32x4 sb[ROWS_B ? 4 : 1];       // scales of rows 64 wn + 16 j + 4 q .. + 3 of B
-  auto read_a = [&](int h, int k) {
-    const uint8_t* src = stage + (k & 1) * kBStage + h * kBHalf;
+  u32x4 fa[4][2], fb[4][2];  // [16 rows][half of the block's columns]
+  float sa[8];               // scale of row 128 (i / 4) + 64 wm + 16 (i % 4) + s, times B's where that is one
+  f32x4 sb[ROWS_B ? 4 : 1];  // scales of rows 64 wn + 16 j + 4 q .. + 3 of B
+  auto read = [&](u32x4 (&f)[4][2], int k, int row) {
+    const uint8_t* src = stage + (k & 1) * kBStage + 128 * row;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) fa[r][c] = stage_chunk(src, 64 * wm + 16 * r + s, 4 * c + q);
-  };
-  auto read_b = [&](u32x4 (&f)[2][2], int h, int k) {
-    const uint8_t* src = stage + (k & 1) * kBStage + h * kBHalf;
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) f[r][c] = stage_chunk(src, 32 * wn + 16 * r + s, 4 * c + q);
+      for (int c = 0; c < 2; ++c) f[r][c] = stage_chunk(src, 16 * r + s, 4 * c + q);
   };
   auto read_scales = [&](int k) {
     const float* src = scales + (k & 1) * 2 * kBT;
@@ -393,82 +384,71 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
   };
   // zeroes columns >= k of operands of the ragged step
-  auto mask = [&](auto& f) {
+  auto mask = [&](u32x4 (&f)[4][2]) {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int keep = (int)(a.k - (int64_t)n_full * 128) - 16 * (4 * c + q);
 #pragma unroll
-      for (auto& x : f) keep_chunk(x[c], keep);
+      for (int r = 0; r < 4; ++r) keep_chunk(f[r][c], keep);
     }
   };
-  auto products = [&](int i0, int j0, const u32x4 (&fb)[2][2]) {
+  auto products = [&](int i0) {
+    // kFlight block sums are under way before the first is added to C, so that the matrix cores never wait for the
+    // additions nor these for them; in this order, which the compiler's own does not keep
+    constexpr int kFlight = 4;
+    f32x4 part[kFlight];
+    auto multiply = [&](int t) {
+      part[t % kFlight] = block_product<FB, FA>(join(fb[t & 3][0], fb[t & 3][1]), join(fa[t >> 2][0], fa[t >> 2][1]));
+      __builtin_amdgcn_sched_barrier(0);
+    };
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int t = 0; t < kFlight; ++t) multiply(t);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const f32x4 part = block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1]));
+    for (int t = 0; t < 16; ++t) {
+      const int i = i0 + (t >> 2), j = t & 3;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          acc[i0 + i][j0 + j][e] = fmaf(part[e], ROWS_B ? sa[i0 + i] * sb[j0 + j][e] : sa[i0 + i], acc[i0 + i][j0 + j][e]);
-      }
+      for (int e = 0; e < 4; ++e)
+        acc[i][j][e] = fmaf(part[t % kFlight][e], ROWS_B ? sa[i] * sb[j][e] : sa[i], acc[i][j][e]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (t + kFlight < 16) multiply(t + kFlight);
+    }
     __builtin_amdgcn_s_setprio(0);
+  };
+  auto request = [&](int k) {
+    issue(A0, k);
+    issue(B0, k);
+    issue(B1, k);
+    issue_scales(k);
   };
   auto step = [&](int k, auto ragged_tag) {
     constexpr bool RAGGED = decltype(ragged_tag)::value;
     // phase 0
-    read_a(A0, k);
+    read(fa, k, 64 * wm);
+    read(fb, k, 256 + 64 * wn);
     read_scales(k);
-    issue(B0, k + 2);
-    wait_loads<13>();
+    issue(A1, k + 1);
+    wait_loads<9>();
     bare_barrier();
     if constexpr (RAGGED) {
       mask(fa);
-      mask(fb0);
+      mask(fb);
     }
-    products(0, 0, fb0);
+    products(0);
     bare_barrier();
     // phase 1
-    read_b(fb1, B1, k);
-    issue_scales(k + 2);
-    issue(A0, k + 2);
-    wait_loads<14>();
-    bare_barrier();
-    if constexpr (RAGGED) mask(fb1);
-    products(0, 2, fb1);
-    bare_barrier();
-    // phase 2
-    read_a(A1, k);
-    issue(B1, k + 2);
-    wait_loads<14>();
+    read(fa, k, 128 + 64 * wm);
+    request(k + 2);
+    wait_loads<9>();
     bare_barrier();
     if constexpr (RAGGED) mask(fa);
-    products(4, 2, fb1);
+    products(4);
     bare_barrier();
-    // phase 3
-    read_b(fbn, B0, k + 1);
-    issue(A1, k + 2);
-    wait_loads<13>();
-    bare_barrier();
-    products(4, 0, fb0);
-    bare_barrier();
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) fb0[r][c] = fbn[r][c];
   };
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    issue(B0, k);
-    issue_scales(k);
-    issue(A0, k);
-    issue(B1, k);
-    issue(A1, k);
-  }
-  wait_loads<13>();  // B0, the scales and A0 of step 0
-  bare_barrier();
-  read_b(fb0, B0, 0);
-  wait_loads<13>();
+  request(0);
+  issue(A1, 0);
+  request(1);
+  wait_loads<9>();  // what phase 0 of step 0 reads
   bare_barrier();
   if (wm == 1) bare_barrier();  // waves 4-7: half a phase behind
 #pragma unroll 1
