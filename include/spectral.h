@@ -322,7 +322,7 @@ SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t cols, int6
  * The products sA sB are formed in float32 and have to stay below its largest
  * value.  Bytes of a code row past column k are not used. */
 typedef struct {
-  int64_t m, n, k;          /* m, n >= 0; k >= 0 (k = 0: C is zero)                   */
+  int64_t m, n, k;          /* 0 .. 2^34; k below 2^22 (k = 0: C is zero)             */
   int32_t a_type;           /* SN_E4M3, SN_E5M2; or SN_F32, SN_BF16: A is a plain
                                matrix [m][ld_a] that the call quantises by rows to
                                E4M3 on its way, bit for bit as

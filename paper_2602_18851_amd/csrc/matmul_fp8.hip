@@ -57,6 +57,17 @@ __device__ __forceinline__ f32x4 block_product(const i32x8& x, const i32x8& y) {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+// Place of tile t: bands of kBand tiles in m, column after column of a band, so that the tiles
+// that run at one time on an XCD share few rows of A and of B in its L2.
+// 8192^3 to bf16: 467 us column by column, 443, 432 and 427 in bands of 16, 8 and 4.
+constexpr int kBand = 4;
+__device__ __forceinline__ void place(int t, int tiles_m, int tiles_n, int64_t& bm, int64_t& bn) {
+  const int band = t / (kBand * tiles_n), first = band * kBand, in = t - first * tiles_n;
+  const int rows = min(kBand, tiles_m - first);
+  bm = first + in % rows;
+  bn = in / rows;
+}
+
 // Eight codes as float16, exactly (NaN codes as NaN).
 template <int F>
 __device__ __forceinline__ f16x8 widen(uint32_t w0, uint32_t w1) {
@@ -141,7 +152,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(MatArgs a) {
   const int unit = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if (unit >= a.tiles_m * a.tiles_n * a.splits) return;  // whole workgroup
   const int tile = unit / a.splits, split = unit % a.splits;
-  const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
+  int64_t bm, bn;
+  place(tile, a.tiles_m, a.tiles_n, bm, bn);
 
   const int64_t am = bm * BM + PM * wv, bnr = bn * BN + PN * wv;  // rows this wave stages
   const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, PM, a.ld_a, a.k));
@@ -288,7 +300,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(MatArgs a) {
 //   requests        A1 of step k + 1     A0, B and scales of step k + 2
 // A phase is a memory part and a product part with a bare barrier after each, and
 // waves 4-7 run half a phase behind waves 0-3, so on every SIMD one wave multiplies
-// while the other reads.  (With four phases of 64 x 32, 8192^3 took KFOUR us.)
+// while the other reads.  (8192^3 before the order of tiles below: 518 us in four phases of 64 x 32, 467
+// in two.)
 // Nothing is read or refilled too early:
 //   - before the barrier that ends a memory part every wave waits until what the next phase reads has landed. That
 //     was requested two phases before it: since then 9 loads, of the two phases after, are outstanding at most;
@@ -312,7 +325,8 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int per_xcd = gridDim.x / 8;
   const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
-  const int64_t bm = tile % a.tiles_m, bn = tile / a.tiles_m;
+  int64_t bm, bn;
+  place(tile, a.tiles_m, a.tiles_n, bm, bn);
 
   // this wave stages rows 16 wv .. + 15 of every 128
   const uint8_t* base[4];
@@ -466,6 +480,155 @@ __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))
     for (int j = 0; j < 4; ++j) {
       const int64_t n = bn * kBT + 64 * wn + 16 * j + 4 * q;
       if (n < a.n) store4(static_cast<__bf16*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
+    }
+  }
+}
+
+// Large float32 products: tiles of 256 x 128 by 8 waves of 64 x 64, with the matrix
+// instruction for float16.  As in big_kernel, waves 4-7 run half a step behind waves 0-3: on
+// every SIMD one wave reads its operands of a block of columns, and waits for the loads to come, while the other
+// multiplies.  Three stages in LDS: block k + 2 is requested in the memory part of block k, into the place of block k -
+// 1, which every wave has read by then; before the barrier that ends that part a wave waits until
+// only these 7 loads are outstanding, so that block k + 1 is there.
+constexpr int kWM = 256, kWN = 128, kWRows = kWM + kWN;
+constexpr int kWStage = kWRows * 128 + 8 * 64 * 4;  // codes, then a scale of each row (and room to keep 8 waves alike)
+
+template <int FA, int FB, bool ROWS_B>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) wide_kernel(MatArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t stage[3 * kWStage];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int per_xcd = gridDim.x / 8;
+  const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
+  int64_t bm, bn;
+  place(tile, a.tiles_m, a.tiles_n, bm, bn);
+
+  const int64_t am = bm * kWM + 32 * wv, bnr = bn * kWN + 16 * wv;  // rows this wave stages
+  const uint8_t* const pa = a.a + am * a.ld_a;
+  const uint8_t* const pb = a.b + bnr * a.ld_b;
+  const uint32_t len_a = range_bytes(am, a.m, 32, a.ld_a, a.k), len_b = range_bytes(bnr, a.n, 16, a.ld_b, a.k);
+  // scales of 64 rows: of A in waves 0-3, of B in waves 4-5 and, to no use, again in 6-7; rows past the last take the last one's
+  const bool sc_a = wv < 4;
+  const int64_t sc_row = sc_a ? bm * kWM + 64 * wv + lane : bn * kWN + 64 * (wv & 1) + lane;
+  const float* sc_at = (sc_a ? a.sa : a.sb) +
+                       (min(sc_row, (sc_a ? a.m : a.n) - 1) >> (sc_a ? a.a_shift : a.b_shift)) * (sc_a ? a.sa_row : a.sb_row);
+  const int64_t sc_block = sc_a ? a.sa_block : a.sb_block;
+  const int n_kb = (int)((a.k + 127) / 128);
+  auto request = [&](int kb, int st) {  // past the last block: an empty range, and its scales again
+    uint8_t* dst = stage + st * kWStage;
+    const bool in = kb < n_kb;
+    stage_issue<32, 0>(make_rsrc(pa, in ? len_a : 0u), dst + 128 * 32 * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane);
+    stage_issue<16, 0>(make_rsrc(pb, in ? len_b : 0u), dst + 128 * (kWM + 16 * wv), 128u * (uint32_t)kb,
+                       (uint32_t)a.ld_b, lane, 16 * wv);
+    __builtin_amdgcn_global_load_lds(sc_at + (in ? kb : n_kb - 1) * sc_block, (lds_void*)(dst + 128 * kWRows + 256 * wv),
+                                     4, 0, 0);
+  };
+
+  const int wm = wv >> 1, wn = wv & 1;
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto block = [&](int kb, int st, auto last_tag) {
+    constexpr bool LAST = decltype(last_tag)::value;  // columns from k on are whatever the rows hold there
+    const uint8_t* ta = stage + st * kWStage;
+    const uint8_t* tb = ta + kWM * 128;
+    const float* sc = reinterpret_cast<const float*>(ta + 128 * kWRows);
+    u32x4 fa[4][2], fb[4][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        fa[r][h] = stage_chunk(ta, 64 * wm + 16 * r + s, 4 * h + q);
+        fb[r][h] = stage_chunk(tb, 64 * wn + 16 * r + s, 4 * h + q);
+      }
+    float sa[4];
+    f32x4 sb[ROWS_B ? 4 : 1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sa[i] = sc[64 * wm + 16 * i + s];
+    if constexpr (ROWS_B) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sb[j] = *reinterpret_cast<const f32x4*>(sc + kWM + 64 * wn + 16 * j + 4 * q);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sa[i] *= sc[kWM + 64 * wn];
+    }
+    request(kb + 2, st == 0 ? 2 : st - 1);
+    wait_loads<7>();
+    bare_barrier();
+    if constexpr (LAST) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          keep_chunk(fa[r][h], keep);
+          keep_chunk(fb[r][h], keep);
+        }
+      }
+    }
+    // The 16 sums of the block stay in registers while its columns are widened and multiplied, 32 after 32.  Between the
+    // products of 32 columns go, in this order, the conversions of the next 32 and, in the last, the additions to C.
+    f32x4 part[4][4];
+    f16x8 ha[2][4], hb[2][4];
+    auto convert = [&](int h, int u) {  // one of the eight operands of columns 32 h .. + 31
+      const int w = 2 * (h & 1), r = u >> 1;
+      if (u & 1)
+        hb[h & 1][r] = widen<FB>(fb[r][h >> 1][w], fb[r][h >> 1][w + 1]);
+      else
+        ha[h & 1][r] = widen<FA>(fa[r][h >> 1][w], fa[r][h >> 1][w + 1]);
+    };
+    auto add = [&](int i, int j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[i][j][e], ROWS_B ? sa[i] * sb[j][e] : sa[i], acc[i][j][e]);
+    };
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) convert(0, u);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+#pragma unroll
+      for (int t = 0; t < 16; ++t) {
+        const int i = t & 3, j = t >> 2;
+        part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+            hb[h & 1][j], ha[h & 1][i], h == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : part[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (h < 3 && (t & 1)) convert(h + 1, t >> 1);
+        if (h == 3 && t >= 4) add(t & 3, (t - 4) >> 2);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) add(i, 3);
+    __builtin_amdgcn_s_setprio(0);
+    bare_barrier();
+  };
+  request(0, 0);
+  request(1, 1);
+  wait_loads<7>();
+  bare_barrier();
+  if (wv >= 4) bare_barrier();  // half a step behind
+  int st = 0;
+#pragma unroll 1
+  for (int kb = 0; kb + 1 < n_kb; ++kb) {
+    block(kb, st, std::false_type{});
+    st = st == 2 ? 0 : st + 1;
+  }
+  block(n_kb - 1, st, std::true_type{});
+  if (wv < 4) bare_barrier();
+  wait_loads<0>();  // the last loads have left the LDS alone before the workgroup gives it up
+
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t m = bm * kWM + 64 * wm + 16 * i + s;
+    if (m >= a.m) continue;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t n = bn * kWN + 64 * wn + 16 * j + 4 * q;
+      if (n < a.n) store4(static_cast<float*>(a.c) + m * a.ld_c + n, acc[i][j], (int)min(a.n - n, (int64_t)4));
     }
   }
 }
@@ -690,17 +853,22 @@ __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
 template <int FA, int FB, bool ROWS_B>
 void launch2(const MatArgs& args, bool bf16, hipStream_t st) {
   MatArgs a = args;
-  auto tiles = [&](int t) {
-    a.tiles_m = (int32_t)((a.m + t - 1) / t);
-    a.tiles_n = (int32_t)((a.n + t - 1) / t);
+  auto tiles = [&](int tm, int tn) {
+    a.tiles_m = (int32_t)((a.m + tm - 1) / tm);
+    a.tiles_n = (int32_t)((a.n + tn - 1) / tn);
     return dim3((uint32_t)(((int64_t)a.tiles_m * a.tiles_n * a.splits + 7) / 8 * 8));
   };
   if (a.big) {
-    const dim3 g = tiles(kBT);
-    big_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
+    if (bf16) {
+      const dim3 g = tiles(kBT, kBT);
+      big_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
+    } else {
+      const dim3 g = tiles(kWM, kWN);
+      wide_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
+    }
     return;
   }
-  const dim3 g = tiles(128);
+  const dim3 g = tiles(128, 128);
   if (bf16)
     tile_kernel<FA, FB, ROWS_B, __bf16, 2, 2, 2><<<g, 256, 0, st>>>(a);
   else
@@ -730,8 +898,19 @@ using sn::refuse;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Rows of A up to which the kernel for few rows runs.
+// Rows of A up to which there is a kernel for few rows.
 constexpr int64_t kFewRows = 64;
+
+// Its cost in us, as in choose(): 256 workgroups at a time, each wave an eighth of the columns, a block
+// at 0.66 and 0.015 a row for one tile of 16 rows of A, 2.0, 2.35 and 2.9 for 2 to 4 (1, 16, 24, 40 and 64 rows
+// against 8192 x 8192: 13.8, 17.4, 19.3, 21.9 and 26.3; tiles of 128 x 128 with the sum in parts 17.7 for 16 rows, 18.5,
+// 19.8 and 20.7; one row against 256 x 16384 11.4 and 17.3).
+double few_cost(int64_t m, int64_t n, int64_t k) {
+  const int t = (int)((m + 15) / 16);
+  const double block = t == 1 ? 0.66 + 0.015 * (double)m : t == 2 ? 2.0 : t == 3 ? 2.35 : 2.9;
+  const double wgs = (double)((n + (t == 1 ? 15 : 31)) / (t == 1 ? 16 : 32));
+  return std::max(1.0, wgs / 256.0) * (double)(((k + 127) / 128 + kFewWaves - 1) / kFewWaves) * block;
+}
 
 // LDS that the codes and scales of a plain A take.
 int64_t plain_bytes(int64_t m, int64_t k) { return m * ((k + 127) / 128) * (128 + 4); }
@@ -752,42 +931,46 @@ void launch_few(const MatArgs& a, int plain, hipStream_t st) {
   }
   switch (t) {
     case 1: return few_rows_kernel<1, 1, 0, FA, FB><<<one, W, 0, st>>>(a);
-    case 2: return few_rows_kernel<2, 1, 0, FA, FB><<<one, W, 0, st>>>(a);
+    case 2: return few_rows_kernel<2, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
     case 3: return few_rows_kernel<3, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
     default: return few_rows_kernel<4, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
   }
 }
 
 // The kernel of a product of more than kFewRows rows, and over how many workgroups a tile's sum
-// is split: the cheapest by these costs in us.  A 256 x 256 tile takes 2.03 for a block of 128 columns,
-// one workgroup per compute unit (8192^3: 522 us); a 128 x 128 tile alone on its
-// unit 0.77 (256 x 8192 x 8192: 51 us), two of them 1.21 (1024 x 8192 x 8192: 79
-// us, by the large tiles 112), for a float32 C 1.2 and 2.15.  Parts are
+// is split: the cheapest by these costs in us, each for a block of 128 columns.  Large tiles,
+// one workgroup per compute unit: 256 x 256 to bf16 1.75 (8192^3: 427 us, 4096^3
+// 60), 256 x 128 to float32 1.85 (1024 x 8192 x 16384: 239).  A 128 x 128 tile alone on its unit 0.77
+// (256 x 8192 x 8192: 51), two of them 1.21 (1024 x 8192 x 8192: 79, by the large
+// tiles 105), to float32 1.2 and 2.15 (1024 x 8192 x 16384: 264).  Parts are
 // written, read and joined at 5.5 TB/s in a launch more: 512 x 512 x 16384 takes 95 us in
 // one part, 53, 31 and 22 in 2, 4 and 8; 512 x 8192 x 8192 51 in one part, 53 in two.
 struct Way {
   bool big;
   int splits, blocks_per_split;
+  double cost;  // without the launch itself
 };
 
 Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
   auto up = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
   const int64_t n_kb = up(k, 128), small = up(m, 128) * up(n, 128);
-  Way best{false, 1, (int)n_kb};
+  Way best{false, 1, (int)n_kb, 0.0};
   double cost = 1e30;
-  if (!f32 && n_kb > 0) {
+  if (n_kb > 0) {
     best.big = true;
-    cost = 2.03 * (double)up(up(m, kBT) * up(n, kBT), 256) * (double)n_kb;
+    cost = (f32 ? 1.85 * (double)up(up(m, kWM) * up(n, kWN), 256) : 1.75 * (double)up(up(m, kBT) * up(n, kBT), 256)) *
+           (double)n_kb;
+    best.cost = cost;
   }
   const double alone = f32 ? 1.2 : 0.77, both = f32 ? 2.15 : 1.21;
   for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= n_kb); ++s) {
     const int64_t per = up(n_kb, s), wgs = small * s, rest = wgs % 512;
     if (s > 1 && (s - 1) * per >= n_kb) continue;  // a split without blocks
     double c = (double)per * ((double)(wgs / 512) * both + (rest == 0 ? 0.0 : rest <= 256 ? alone : both));
-    if (s > 1) c += 2.5 + (double)(8 * s + (f32 ? 4 : 2)) * (double)m * (double)n / 5.5e6;
+    if (s > 1) c += 4.0 + (double)(8 * s + (f32 ? 4 : 2)) * (double)m * (double)n / 5.5e6;
     if (c < cost) {
       cost = c;
-      best = Way{false, (int)s, (int)per};
+      best = Way{false, (int)s, (int)per, c};
     }
   }
   return best;
@@ -814,8 +997,8 @@ int resolve(sn_matmul& p, MatPlan& pl) {
   if ((p.a_block_rows != 1 && p.a_block_rows != 128) || (p.b_block_rows != 1 && p.b_block_rows != 128))
     return refuse(SN_EINVAL, "a_block_rows and b_block_rows must be 1 or 128");
   if (plain && p.a_block_rows != 1) return refuse(SN_EINVAL, "a plain A is quantised by rows: a_block_rows must be 1");
-  constexpr int64_t kMost = int64_t(1) << 40, kMostLd = int64_t(1) << 22;
-  if (p.m > kMost || p.n > kMost || p.k > kMostLd || p.ld_a > kMost || p.ld_b > kMost || p.ld_c > kMost)
+  constexpr int64_t kMost = int64_t(1) << 40, kMostRows = int64_t(1) << 34, kMostLd = int64_t(1) << 22;
+  if (p.m > kMostRows || p.n > kMostRows || p.k > kMostLd || p.ld_a > kMost || p.ld_b > kMost || p.ld_c > kMost)
     return refuse(SN_EINVAL, "m, n or a row stride is too large (k and code rows stay below 2^22)");
   if (p.ld_a == 0) p.ld_a = plain ? p.k : round_up(p.k, 16);
   if (p.ld_b == 0) p.ld_b = round_up(p.k, 16);
@@ -841,15 +1024,17 @@ int resolve(sn_matmul& p, MatPlan& pl) {
     return refuse(SN_EINVAL, "a plain A must stay below 2^31 tiles of 128 x 128");
   pl = MatPlan{};
   pl.plain_a = plain;
-  pl.few = p.m <= kFewRows;
-  pl.fuse = plain && p.m <= 32 && plain_bytes(p.m, p.k) <= kPlainBytes;
+  pl.way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
+  // within 2 us the kernel for few rows: its sums are the more exact ones, and it takes a plain A without a launch more
+  // (the choice is the same for codes, so that both give the same bits)
+  pl.few = p.m <= kFewRows && p.m > 0 && few_cost(p.m, p.n, p.k) <= pl.way.cost + 2.0;
+  pl.fuse = pl.few && plain && p.m <= 32 && plain_bytes(p.m, p.k) <= kPlainBytes;
   if (plain && !pl.fuse && p.m > 0 && p.k > 0) {
     pl.ld_codes = round_up(p.k, 16);
     pl.off_scale = round_up(p.m * pl.ld_codes, 256);
     pl.bytes = pl.off_scale + round_up(p.m * ((p.k + 127) / 128) * 4, 256);
   }
   if (!pl.few) {
-    pl.way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
     if (pl.way.big && (p.sa_row >= (1 << 20) || p.sb_row >= (1 << 20))) pl.way.big = false;
     if (pl.way.splits > 1) {
       pl.off_parts = pl.bytes;

@@ -248,8 +248,8 @@ def test_result_in_a_window(out, m, n, k, offset, extra):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("m,n,k,offset", [(1, 200, 1000, 0), (1, 65, 40, 3), (7, 129, 257, 0), (16, 300, 2100, 1), (33, 128, 384, 0),
-                                          (200, 130, 515, 0)])
+@pytest.mark.parametrize("m,n,k,offset", [(1, 200, 1000, 0), (1, 65, 40, 3), (7, 129, 257, 0), (16, 300, 2100, 1), (33, 128, 384, 0), (31, 200, 1536, 0),
+                                          (32, 64, 4096, 2), (17, 700, 8200, 0), (64, 900, 1030, 0), (200, 130, 515, 0)])
 def test_plain_operand_is_quantised_on_the_way(dtype, m, n, k, offset):
     room = torch.full((m, k + offset + 4), float("nan"), dtype=TORCH[dtype], device="cuda")
     x = room[:, offset:offset + k]
