@@ -298,8 +298,8 @@ SN_API int spectral_logits_fp8(sn_ctx* ctx, const void* const* x_layers, int64_t
  * Code rows are 16-byte aligned; ld_row and ld_col are multiples of 16 not
  * below cols and rows.  Codes are written up to the next multiple of 16
  * columns, zeros past the last.  One of row_codes and col_codes is required,
- * each with its scale.  Outputs must not overlap x or each other.  rows = 0
- * or cols = 0 does nothing.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE,
+ * each with its scale.  Outputs must not overlap x or each other.  rows x cols
+ * stays below 2^24 tiles of 128 x 128; rows = 0 or cols = 0 does nothing.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE,
  * SN_EHIP.
  *
  * These calls and spectral_rotary need no context: they queue on hip_stream
@@ -322,7 +322,8 @@ SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t cols, int6
  * The products sA sB are formed in float32 and have to stay below its largest
  * value.  Bytes of a code row past column k are not used. */
 typedef struct {
-  int64_t m, n, k;          /* 0 .. 2^34; k below 2^22 (k = 0: C is zero)             */
+  int64_t m, n, k;          /* >= 0 (k = 0: C is zero); m x n below 2^22 tiles of
+                               128 x 128, k below 2^22 - 128                          */
   int32_t a_type;           /* SN_E4M3, SN_E5M2; or SN_F32, SN_BF16: A is a plain
                                matrix [m][ld_a] that the call quantises by rows to
                                E4M3 on its way, bit for bit as
@@ -446,7 +447,7 @@ SN_API int spectral_workspace_bytes(const sn_shape* shape, const sn_params* para
  * the Gram form, 7 = row sweeps of the layer-level form (one-pass: its W_K
  * sweeps), 8 = its column sweeps (one-pass: those over W_Q or the group
  * sums), 9 = its group sums, reductions and finalize, 10 = projections of
- * the logit consumer, 11 = its logit kernels, 12 = the running-head lists of
+ * the logit consumer (and its rotary positions), 11 = its logit kernels, 12 = the running-head lists of
  * tolerance mode), the summed device time in
  * milliseconds and the number of launches since the previous read, then
  * resets both.  ms and launches point to SN_PROFILE_KINDS host elements

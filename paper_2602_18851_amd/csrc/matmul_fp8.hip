@@ -1018,16 +1018,17 @@ int resolve(sn_matmul& p, MatPlan& pl) {
   if (p.sa_block < 0 || p.sa_row < 0 || p.sb_block < 0 || p.sb_row < 0 || p.sa_block > kMost || p.sa_row > kMost ||
       p.sb_block > kMost || p.sb_row > kMost)
     return refuse(SN_EINVAL, "scale strides must be >= 0 and below 2^40");
-  if (((p.m + 127) / 128) * ((p.n + 127) / 128) >= (int64_t(1) << 30))
-    return refuse(SN_EINVAL, "m x n must stay below 2^30 tiles of 128 x 128");
-  if (plain && ((p.m + 127) / 128) * ((p.k + 127) / 128) >= (int64_t(1) << 31))
-    return refuse(SN_EINVAL, "a plain A must stay below 2^31 tiles of 128 x 128");
+  if (((p.m + 127) / 128) * ((p.n + 127) / 128) >= (int64_t(1) << 22))
+    return refuse(SN_EINVAL, "m x n must stay below 2^22 tiles of 128 x 128");
+  if (plain && ((p.m + 127) / 128) * ((p.k + 127) / 128) >= (int64_t(1) << 24))
+    return refuse(SN_EINVAL, "a plain A must stay below 2^24 tiles of 128 x 128");
   pl = MatPlan{};
   pl.plain_a = plain;
   pl.way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
   // within 2 us the kernel for few rows: its sums are the more exact ones, and it takes a plain A without a launch more
   // (the choice is the same for codes, so that both give the same bits)
-  pl.few = p.m <= kFewRows && p.m > 0 && few_cost(p.m, p.n, p.k) <= pl.way.cost + 2.0;
+  pl.few = p.m <= kFewRows && p.m > 0 && p.n < (int64_t(1) << 27) &&  // a launch has at most 2^32 lanes
+           few_cost(p.m, p.n, p.k) <= pl.way.cost + 2.0;
   pl.fuse = pl.few && plain && p.m <= 32 && plain_bytes(p.m, p.k) <= kPlainBytes;
   if (plain && !pl.fuse && p.m > 0 && p.k > 0) {
     pl.ld_codes = round_up(p.k, 16);

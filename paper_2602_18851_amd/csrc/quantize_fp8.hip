@@ -198,8 +198,8 @@ extern "C" SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t
   if (!aligned(x, dtype == SN_F32 ? 4 : 2) || !aligned(row_scale, 4) || !aligned(col_scale, 4))
     return refuse(SN_EINVAL, "x and the scales must be aligned to their type");
   if (rows > (int64_t(1) << 40) || cols > (int64_t(1) << 40) || ld_x > (int64_t(1) << 40) ||
-      ((rows + 127) / 128) * ((cols + 127) / 128) >= (int64_t(1) << 31))
-    return refuse(SN_EINVAL, "rows x cols must stay below 2^31 tiles of 128 x 128");
+      ((rows + 127) / 128) * ((cols + 127) / 128) >= (int64_t(1) << 24))
+    return refuse(SN_EINVAL, "rows x cols must stay below 2^24 tiles of 128 x 128");
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (int rc = check_stream(st)) return rc;
   QuantArgs a{};

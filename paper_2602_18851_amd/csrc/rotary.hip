@@ -95,6 +95,7 @@ struct RotaryArgs {
   HeadsArg<IO> t[2];
   const int64_t* positions;
   int64_t first, n_tokens;
+  int64_t group0;      // groups of tokens that earlier launches of the call turn
   int64_t period;      // tokens after which positions repeat (the layers of the consumer), or n_tokens
   float sign;          // -1 turns back
   int32_t n_tensors, tokens_per_group, splits;
@@ -118,12 +119,12 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
   __shared__ int skip[kMaxTokens];
   const int t = threadIdx.x;
   const int pairs = a.table.pairs, rest = a.table.head_dim - 2 * pairs;
-  const int64_t token0 = (int64_t)(blockIdx.x / a.splits) * a.tokens_per_group;
+  const int64_t token0 = (a.group0 + blockIdx.x / a.splits) * a.tokens_per_group;
   const int split = blockIdx.x % a.splits;
   const int n = (int)(a.n_tokens - token0 < a.tokens_per_group ? a.n_tokens - token0 : a.tokens_per_group);
   for (int i = t; i < n * pairs; i += kThreads) {
     const int k = i / pairs, j = i % pairs;
-    const int64_t row = (token0 + k) % a.period;
+    const int64_t row = a.n_tokens == a.period ? token0 + k : (token0 + k) % a.period;
     const int64_t p = a.positions ? a.positions[row] : a.first + row;
     const double f = a.table.turns[j], pd = (double)p;
     const float r = (float)fma(pd, f, -rint(pd * f));  // what whole turns leave
@@ -192,7 +193,10 @@ void launch_pairs(RotaryArgs<IO> a, hipStream_t st) {
   a.tokens_per_group = (int32_t)std::min<int64_t>(kMaxTokens, std::max<int64_t>(1, 4 * kThreads / per_token));
   const int64_t groups = (a.n_tokens + a.tokens_per_group - 1) / a.tokens_per_group;
   a.splits = groups >= 512 ? 1 : (int32_t)std::min<int64_t>((per_token + kThreads - 1) / kThreads, 64);
-  rotary_kernel<IO, V, INTERLEAVED><<<dim3((uint32_t)(groups * a.splits)), kThreads, 0, st>>>(a);
+  constexpr int64_t kMost = int64_t(1) << 20;  // groups of a launch, whose lanes are counted in 32 bits
+  for (; a.group0 < groups; a.group0 += kMost)
+    rotary_kernel<IO, V, INTERLEAVED>
+        <<<dim3((uint32_t)(std::min(kMost, groups - a.group0) * a.splits)), kThreads, 0, st>>>(a);
 }
 
 // Pairs a thread takes: as many as make 16-byte accesses (W elements, half as many

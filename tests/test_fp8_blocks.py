@@ -147,7 +147,8 @@ def matmul(**kw):
     (sp.SN_EINVAL, dict(b_block_rows=0)), (sp.SN_EINVAL, dict(a_type=sp.SN_F32, a_block_rows=128)),
     (sp.SN_EINVAL, dict(ld_a=96)), (sp.SN_EINVAL, dict(ld_a=104)), (sp.SN_EINVAL, dict(ld_b=120)),
     (sp.SN_EINVAL, dict(ld_c=19)), (sp.SN_EINVAL, dict(k=1 << 22)), (sp.SN_EINVAL, dict(ld_b=1 << 22)),
-    (sp.SN_EINVAL, dict(sa_block=-1)), (sp.SN_EINVAL, dict(m=1 << 30, n=1 << 30)),
+    (sp.SN_EINVAL, dict(sa_block=-1)), (sp.SN_EINVAL, dict(m=1 << 30, n=1 << 30)), (sp.SN_EINVAL, dict(m=1 << 18, n=1 << 18)),
+    (sp.SN_EINVAL, dict(m=1 << 35)),
     (sp.SN_EINVAL, dict(a_type=sp.SN_BF16, m=1 << 34, n=1, k=1 << 16))])
 def test_bad_products_are_refused(lib, code, kw):  # noqa: F811
     refused(code, sp.spectral_matmul_fp8_workspace_bytes, matmul(**kw))

@@ -274,6 +274,47 @@ def test_products_with_blocks_that_are_not_finite():
     assert np.isnan(got[bad]).all() and np.isfinite(got[~bad]).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(9, 200, 300), (70, 130, 300), (600, 700, 300), (300, 600, 6000)])
+@pytest.mark.parametrize("fmt,bad", [("e4m3", 0x7F), ("e4m3", 0xFF), ("e5m2", 0x7E), ("e5m2", 0x7C), ("e5m2", 0xFC)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_codes_that_are_not_finite(m, n, k, fmt, bad, out):
+    """A NaN or infinite code makes its row of C not finite and leaves every other row as it was."""
+    a, _ = matrix((40, m, k), m, k, fmt, 1)
+    b, _ = matrix((41, n, k), n, k, "e4m3", 128)
+    ref = matmul_fp8(a, b, out_dtype=TORCH[out])
+    a.codes.view(torch.uint8)[m // 2, k - 1] = bad
+    got = matmul_fp8(a, b, out_dtype=TORCH[out])
+    assert not torch.isfinite(got[m // 2]).any()  # an infinity times a zero code is NaN
+    rest = torch.arange(m, device="cuda") != m // 2
+    assert torch.equal(got[rest], ref[rest])
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Windows of matrices of 5 GB: their last rows start past 2^32 bytes."""
+    m, k = 41000, 200
+    r = rng(42)
+    room = torch.empty(m, 131072, dtype=torch.uint8, device="cuda")
+    x = on_gpu(r.integers(-4, 5, (m, k)), "bf16")
+    small, _ = quantize_fp8(x)
+    room[:, :k] = small.codes.view(torch.uint8)[:, :k]
+    part = Fp8Matrix(room.view(TORCH["e4m3"])[:, :208], small.scale, cols=k)
+    b, _ = matrix((43, 96, k), 96, k, "e4m3", 1)
+    for out in ("f32", "bf16"):
+        assert torch.equal(matmul_fp8(part, b, out_dtype=TORCH[out]), matmul_fp8(small, b, out_dtype=TORCH[out]))
+        assert torch.equal(matmul_fp8(b, part, out_dtype=TORCH[out]), matmul_fp8(b, small, out_dtype=TORCH[out]))
+        assert torch.equal(matmul_fp8(matrix((44, 3, k), 3, k, "e4m3", 1)[0], part, out_dtype=TORCH[out]),
+                           matmul_fp8(matrix((44, 3, k), 3, k, "e4m3", 1)[0], small, out_dtype=TORCH[out]))
+    del part
+    wide_x = room.view(-1).view(torch.bfloat16).view(m, 65536)[:, :k]
+    wide_x.copy_(x)
+    a, t = quantize_fp8(wide_x, cols=True)
+    ref_a, ref_t = quantize_fp8(x, cols=True)
+    for p, q in ((a, ref_a), (t, ref_t)):
+        assert torch.equal(p.codes.view(torch.uint8), q.codes.view(torch.uint8)) and torch.equal(p.scale, q.scale)
+    out = room.view(-1).view(torch.bfloat16).view(m, 65536)[:, 40000:40096]
+    assert torch.equal(matmul_fp8(small, b, out=out), matmul_fp8(small, b))
+
+
 def test_empty_sums_are_zero():
     a = Fp8Matrix(torch.empty(3, 0, dtype=TORCH["e4m3"], device="cuda"), torch.empty(0, 3, device="cuda"))
     b = Fp8Matrix(torch.empty(5, 0, dtype=TORCH["e4m3"], device="cuda"), torch.empty(0, 5, device="cuda"))

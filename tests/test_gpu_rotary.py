@@ -134,6 +134,27 @@ def test_padding_stays():
         assert torch.equal(o[live], r[live]) and (o[~live] == v).all()
 
 
+def test_many_tokens_and_far_rows():
+    """More groups of tokens than one launch takes, and rows that start past 2^32 bytes."""
+    plan = Rotary(2)
+    n = (1 << 24) + 100
+    x = torch.ones(n, 1, 2, device="cuda")
+    got = plan.apply(x)
+    for t in (0, 1, 1 << 20, (1 << 24) - 1, 1 << 24, n - 1):
+        assert abs(float(got[t, 0, 0]) - (math.cos(t) - math.sin(t))) < 16 * 2.0 ** -24
+        assert abs(float(got[t, 0, 1]) - (math.cos(t) + math.sin(t))) < 16 * 2.0 ** -24
+    del x, got
+    plan = Rotary(64)
+    room = torch.empty(700, 1 << 21, device="cuda")  # 5.9 GB
+    far = room[:, :128].view(700, 2, 64)
+    x = heads((8, 1), 700, 2, 64, "f32")
+    far.copy_(x)
+    ref = plan.apply(x)
+    assert torch.equal(plan.apply(far), ref)
+    plan.apply(far, out=far)
+    assert torch.equal(far, ref)
+
+
 def test_values_that_are_not_finite_stay_in_their_pair():
     plan = Rotary(64)
     x = heads((4, 1), 3, 2, 64, "f32")
