@@ -320,7 +320,8 @@ SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t cols, int6
  * y from x by rows and W by tiles, dx = dy W from dy by rows and W's
  * transpose by tiles, dW = dy^T x from the transposes of dy and x.
  * The products sA sB are formed in float32 and have to stay below its largest
- * value.  Bytes of a code row past column k are not used. */
+ * value.  Every row of codes, the last one too, holds k rounded up to 16 bytes; those past
+ * column k are not used. */
 typedef struct {
   int64_t m, n, k;          /* >= 0 (k = 0: C is zero); m x n below 2^22 tiles of
                                128 x 128, k below 2^22 - 128                          */

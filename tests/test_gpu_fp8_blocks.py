@@ -455,6 +455,27 @@ def test_calls_on_another_stream():
     assert all(torch.equal(p, q) for p, q in zip(ref, got))
 
 
+def test_calls_at_the_same_time():
+    """Products of both streams overlap on the chip; each has its own operands, results and workspace."""
+    sides = []
+    for k in range(2):
+        a, _ = matrix((50, k), 300, 6000, "e4m3", 1)
+        b, _ = matrix((51, k), 500, 6000, "e4m3", 128)
+        x = on_gpu(wide(rng(52, k), 100, 6000), "bf16")
+        ref = matmul_fp8(a, b, out_dtype=torch.float32), matmul_fp8(x, b)
+        ws = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+        sides.append((a, b, x, ref, ws, torch.cuda.Stream(), [torch.empty_like(t) for t in ref]))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for a, b, x, _, ws, s, out in sides:
+            with torch.cuda.stream(s):
+                matmul_fp8(a, b, out=out[0], workspace=ws)
+                matmul_fp8(x, b, out=out[1], workspace=ws)
+    torch.cuda.synchronize()
+    for _, _, _, ref, _, _, out in sides:
+        assert all(torch.equal(p, q) for p, q in zip(ref, out))
+
+
 def test_kept_workspace():
     x = on_gpu(wide(rng(26), 40, 900), "f32")
     b, _ = matrix((27, 100, 900), 100, 900, "e4m3", 128)

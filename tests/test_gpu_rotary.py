@@ -263,6 +263,32 @@ def test_logits_of_turned_queries_and_keys(dh, rot, layout, own_positions):
     assert (still != plain).float().mean() < 2.0 ** -8  # values within 2^-15 of a border between codes 2^-3 apart
 
 
+def test_logits_of_turned_heads_replay_from_a_graph():
+    L, seq, d, nq, nkv, dh = 2, 130, 256, 4, 2, 64
+    r = np.random.default_rng(20260305)
+    t = lambda *s: torch.from_numpy(r.standard_normal(s).astype(np.float32)).bfloat16().cuda()  # noqa: E731
+    x, wq, wk = t(L, seq, d), t(L, nq * dh, d) * 0.05, t(L, nkv * dh, d) * 0.05
+    scale, p = torch.tensor([0.05, 0.1], device="cuda"), torch.arange(seq, device="cuda")
+    est, plan = Spectral(L, d, nq, nkv, dh, "bf16", 0.1), Rotary(dh)
+
+    def call():
+        return est.logits_fp8(x, wq, wk, scale, want_codes=True, rotary=plan, positions=p)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for rep in range(4):
+        x.mul_(0.75)
+        p.add_(17)
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
 def test_projections_positions_and_scales_together():
     """One attention layer's front half as a program runs it: the scale from the estimator, queries and keys from 8-bit
     products, turned by their positions; the logits obey the bound of the unturned weights (Sec. 3.3), and the gradients
