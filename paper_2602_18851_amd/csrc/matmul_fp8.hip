@@ -131,17 +131,18 @@ __device__ __forceinline__ void wait_loads() {
   __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
 }
 
-// Tiles of 128 x 128 by 4 waves of 64 x 64, two workgroups to a compute unit.  Blocks of 128 columns and the
-// scales of their rows come through two stages in LDS, the next requested before the current one is
-// multiplied.  The products are formed transposed (rows from B): a lane holds four neighbouring columns of one row
+// Tiles of 128 x 128 by 4 waves of 64 x 64, two workgroups to a compute unit, or by 8 waves of 64 x 32.  Blocks of
+// 128 columns and the scales of their rows come through two stages in LDS, the next requested before the current one is
+// multiplied (three or four stages gain nothing: 512 x 8192 x 8192 46.6 and 46.4 us, two 45.7).  The products are formed transposed (rows from B): a lane holds four neighbouring columns of one row
 // of C, with one scale of A.  Scales through LDS, a block ahead, and not read as they are needed: 4096^3 to
-// float32 139 instead of 230 us, 256 x 8192 x 8192 to bf16 46 instead of 66; three stages, one workgroup a
-// unit, 189 and 73.
+// float32 139 instead of 230 us, 256 x 8192 x 8192 to bf16 46 instead of 66.
 constexpr int kT = 128;
 constexpr int kTStage = 2 * kT * 128 + 2 * kT * 4;  // rows of A, of B, then their scales
 
-template <int FA, int FB, bool ROWS_B, typename TC>
-__global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
+template <int FA, int FB, bool ROWS_B, typename TC, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) tile_kernel(MatArgs a) {
+  constexpr int ROWS = kT / WAVES;   // rows of each matrix a wave stages
+  constexpr int NJ = 16 / WAVES;     // columns of 16 x 16 blocks of a wave: 64 or 32 columns of C
   // one array: with two, the compiler waits for every load into LDS before it reads either
   __shared__ __attribute__((aligned(16))) uint8_t stage[2 * kTStage];
   const int lane = threadIdx.x & 63;
@@ -154,9 +155,9 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
   int64_t bm, bn;
   place(tile, a.tiles_m, a.tiles_n, bm, bn);
 
-  const int64_t am = bm * kT + 32 * wv, bnr = bn * kT + 32 * wv;  // rows this wave stages
-  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, 32, a.ld_a, a.k));
-  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.b + bnr * a.ld_b, range_bytes(bnr, a.n, 32, a.ld_b, a.k));
+  const int64_t am = bm * kT + ROWS * wv, bnr = bn * kT + ROWS * wv;  // rows this wave stages
+  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.a + am * a.ld_a, range_bytes(am, a.m, ROWS, a.ld_a, a.k));
+  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.b + bnr * a.ld_b, range_bytes(bnr, a.n, ROWS, a.ld_b, a.k));
   // and scales of 64 rows, of A in waves 0 and 1, of B in 2 and 3; rows past the last take the last one's
   const bool sc_a = wv < 2;
   const int64_t sc_row0 = (sc_a ? bm : bn) * kT + 64 * (wv & 1), sc_rows = sc_a ? a.m : a.n;
@@ -165,17 +166,17 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
   const int64_t sc_block = sc_a ? a.sa_block : a.sb_block;
   auto issue = [&](int kb) {
     uint8_t* st = stage + (kb & 1) * kTStage;
-    stage_issue<32, 0>(ra, st + 4096 * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane);
-    stage_issue<32, 0>(rb, st + 128 * kT + 4096 * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane);
-    __builtin_amdgcn_global_load_lds(sc_at + kb * sc_block, (lds_void*)(st + 2 * kT * 128 + 256 * wv), 4, 0, 0);
+    stage_issue<ROWS, 0>(ra, st + 128 * ROWS * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane, ROWS * wv);
+    stage_issue<ROWS, 0>(rb, st + 128 * (kT + ROWS * wv), 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane, ROWS * wv);
+    if (wv < 4) __builtin_amdgcn_global_load_lds(sc_at + kb * sc_block, (lds_void*)(st + 2 * kT * 128 + 256 * wv), 4, 0, 0);
   };
 
-  const int wm = wv >> 1, wn = wv & 1;
-  f32x4 acc[4][4];
+  const int wm = wv / (WAVES / 2), wn = wv % (WAVES / 2);  // rows from 64 wm, columns from 16 NJ wn
+  f32x4 acc[4][NJ];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   // this workgroup's blocks of columns; the last of all may be ragged
   const int kb0 = split * a.blocks_per_split, n_kb = min((int)((a.k + 127) / 128), kb0 + a.blocks_per_split);
   auto block = [&](int kb, auto last_tag) {
@@ -183,29 +184,31 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
     const uint8_t* ta = stage + (kb & 1) * kTStage;
     const uint8_t* tb = ta + kT * 128;
     const float* sc = reinterpret_cast<const float*>(ta + 2 * kT * 128);
-    u32x4 fa[4][2], fb[4][2];
+    u32x4 fa[4][2], fb[NJ][2];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int h = 0; h < 2; ++h) {
+      const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int r = 0; r < 4; ++r) {
         fa[r][h] = stage_chunk(ta, 64 * wm + 16 * r + s, 4 * h + q);
-        fb[r][h] = stage_chunk(tb, 64 * wn + 16 * r + s, 4 * h + q);
-        if constexpr (LAST) {
-          const int keep = (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q);
-          keep_chunk(fa[r][h], keep);
-          keep_chunk(fb[r][h], keep);
-        }
+        if constexpr (LAST) keep_chunk(fa[r][h], keep);
       }
+#pragma unroll
+      for (int r = 0; r < NJ; ++r) {
+        fb[r][h] = stage_chunk(tb, 16 * (NJ * wn + r) + s, 4 * h + q);
+        if constexpr (LAST) keep_chunk(fb[r][h], keep);
+      }
+    }
     float sa[4];
-    f32x4 sb[ROWS_B ? 4 : 1];
+    f32x4 sb[ROWS_B ? NJ : 1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) sa[i] = sc[64 * wm + 16 * i + s];
     if constexpr (ROWS_B) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sb[j] = *reinterpret_cast<const f32x4*>(sc + kT + 64 * wn + 16 * j + 4 * q);
+      for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const f32x4*>(sc + kT + 16 * (NJ * wn + j) + 4 * q);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sa[i] *= sc[kT + 64 * wn];
+      for (int i = 0; i < 4; ++i) sa[i] *= sc[kT + 16 * NJ * wn];
     }
     auto add = [&](int i, int j, const f32x4& part) {
 #pragma unroll
@@ -213,14 +216,14 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
     };
     if constexpr (sizeof(TC) == 2) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           add(i, j, block_product<FB, FA>(join(fb[j][0], fb[j][1]), join(fa[i][0], fa[i][1])));
     } else {
       // two columns of 16 x 16 blocks at a time: their sums and codes as float16 stay in registers
 #pragma unroll
-      for (int jj = 0; jj < 4; jj += 2) {
+      for (int jj = 0; jj < NJ; jj += 2) {
         f32x4 part[4][2];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
@@ -265,8 +268,8 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(MatArgs a) {
     const int64_t m = bm * kT + 64 * wm + 16 * i + s;
     if (m >= a.m) continue;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = bn * kT + 64 * wn + 16 * j + 4 * q;
+    for (int j = 0; j < NJ; ++j) {
+      const int64_t n = bn * kT + 16 * (NJ * wn + j) + 4 * q;
       if (n >= a.n) continue;
       if (a.splits > 1)  // rows of the parts are whole groups of four
         *reinterpret_cast<f32x4*>(a.parts + ((int64_t)split * a.m + m) * a.ld_parts + n) = acc[i][j];
@@ -855,10 +858,14 @@ void launch2(const MatArgs& args, bool big, bool bf16, hipStream_t st) {
     return;
   }
   const dim3 g = tiles(kT, kT);
-  if (bf16)
-    tile_kernel<FA, FB, ROWS_B, __bf16><<<g, 256, 0, st>>>(a);
+  // a workgroup alone on its compute unit: 8 waves (512 x 8192 x 8192 to bf16 48.6 us with 4, 44.6 with 8); else two of 4
+  // (1024 x 8192 x 8192 71.9 with 4, 74.2 with 8)
+  if ((int64_t)a.tiles_m * a.tiles_n * a.splits <= 256)
+    bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 8><<<g, 512, 0, st>>>(a)
+         : tile_kernel<FA, FB, ROWS_B, float, 8><<<g, 512, 0, st>>>(a);
   else
-    tile_kernel<FA, FB, ROWS_B, float><<<g, 256, 0, st>>>(a);
+    bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 4><<<g, 256, 0, st>>>(a)
+         : tile_kernel<FA, FB, ROWS_B, float, 4><<<g, 256, 0, st>>>(a);
   if (a.splits > 1) {
     const dim3 j((uint32_t)std::min<int64_t>((a.m * (a.ld_parts / 4) + 255) / 256, 4096));
     bf16 ? join_kernel<__bf16><<<j, 256, 0, st>>>(a) : join_kernel<float><<<j, 256, 0, st>>>(a);
@@ -926,11 +933,11 @@ void launch_few(const MatArgs& a, int plain, hipStream_t st) {
 // The kernel of a product of more than kFewRows rows, and over how many workgroups a tile's sum
 // is split: the cheapest by these costs in us, each for a block of 128 columns.  Large tiles,
 // one workgroup per compute unit: 256 x 256 to bf16 1.75 (8192^3: 427 us, 4096^3
-// 60), 256 x 128 to float32 1.85 (1024 x 8192 x 16384: 239).  A 128 x 128 tile alone on its unit 0.77
-// (256 x 8192 x 8192: 51), two of them 1.21 (1024 x 8192 x 8192: 79, by the large
-// tiles 105), to float32 1.2 and 2.15 (1024 x 8192 x 16384: 264).  Parts are
+// 60), 256 x 128 to float32 1.85 (1024 x 8192 x 16384: 239).  A 128 x 128 tile alone on its unit 0.67
+// (512 x 8192 x 8192: 45), two of them 1.12 (1024 x 8192 x 8192: 72, by the large
+// tiles 105), to float32 1.1 and 2.1 (1024 x 8192 x 16384: 264).  Parts are
 // written, read and joined at 5.5 TB/s in a launch more: 512 x 512 x 16384 takes 95 us in
-// one part, 53, 31 and 22 in 2, 4 and 8; 512 x 8192 x 8192 51 in one part, 53 in two.
+// one part, 53, 31 and 22 in 2, 4 and 8; 512 x 8192 x 8192 45 in one part, 53 in two.
 struct Way {
   bool big;
   int splits, blocks_per_split;
@@ -948,7 +955,7 @@ Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
            (double)n_kb;
     best.cost = cost;
   }
-  const double alone = f32 ? 1.2 : 0.77, both = f32 ? 2.15 : 1.21;
+  const double alone = f32 ? 1.1 : 0.67, both = f32 ? 2.1 : 1.12;
   for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= n_kb); ++s) {
     const int64_t per = up(n_kb, s), wgs = small * s, rest = wgs % 512;
     if (s > 1 && (s - 1) * per >= n_kb) continue;  // a split without blocks
