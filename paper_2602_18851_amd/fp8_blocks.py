@@ -66,6 +66,14 @@ class Fp8Matrix:
         self.codes, self.scale = codes, scale if any(scale.stride()) else scale.contiguous()
         self.rows, self.cols = rows, cols
 
+    @classmethod
+    def _made(cls, codes: torch.Tensor, scale: torch.Tensor, rows: int, cols: int, block_rows: int) -> "Fp8Matrix":
+        """One of the quantiser's own, which needs no checks."""
+        m = object.__new__(cls)
+        m.codes, m.scale, m.rows, m.cols, m.block_rows = codes, scale, rows, cols, block_rows
+        m.ld = (cols + 15) // 16 * 16
+        return m
+
     @property
     def values(self) -> torch.Tensor:
         """The codes [rows, cols] without the columns that fill up their rows."""
@@ -96,18 +104,21 @@ def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: b
     r, c = x.shape
     dev, dtype = x.device, _FORMATS[fmt]
 
+    block_rows = BLOCK if tile else 1
+
     def room(n, k):  # n code rows of k columns
         codes = torch.empty((n, (k + 15) // 16 * 16), dtype=dtype, device=dev)
-        return codes, torch.empty(((k + 127) // 128, (n + 127) // 128 if tile else n), dtype=torch.float32, device=dev)
+        scale = torch.empty(((k + 127) // 128, (n + 127) // 128 if tile else n), dtype=torch.float32, device=dev)
+        return Fp8Matrix._made(codes, scale, n, k, block_rows)
 
     a = room(r, c) if rows else None
     b = room(c, r) if cols else None
     if r and c:
-        ra = (a[0].data_ptr(), a[0].shape[1], a[1].data_ptr()) if rows else (0, 0, 0)
-        cb = (b[0].data_ptr(), b[0].shape[1], b[1].data_ptr()) if cols else (0, 0, 0)
+        ra = (a.codes.data_ptr(), a.ld, a.scale.data_ptr()) if rows else (0, 0, 0)
+        cb = (b.codes.data_ptr(), b.ld, b.scale.data_ptr()) if cols else (0, 0, 0)
         on_stream_of(dev, spectral_quantize_fp8, x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype],
                      1 if tile else 0, *ra, *cb)
-    return (Fp8Matrix(*a, cols=c) if rows else None), (Fp8Matrix(*b, cols=r) if cols else None)
+    return a, b
 
 
 def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
