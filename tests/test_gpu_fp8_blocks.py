@@ -204,6 +204,24 @@ def test_products_of_whole_numbers_are_exact(m, n, k, ra, rb, fa, out):
     assert torch.equal(matmul_fp8(*mats, out_dtype=TORCH[out]).cpu(), ref)
 
 
+@pytest.mark.parametrize("k", [1, 100, 128, 129, 256, 300, 512, 600])
+@pytest.mark.parametrize("rb", [1, 128])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_large_tiles_of_few_blocks(k, rb, out):
+    """Products of whole numbers as above, so wide that the large tiles run over one to five blocks of columns."""
+    g = torch.Generator(device="cuda").manual_seed(k)
+    vals, mats = [], []
+    for rows, br in ((8200, 1), (8300, rb)):
+        v = torch.randint(-4, 5, (rows, k), generator=g, device="cuda").float()
+        codes = torch.full((rows, -(-k // 16) * 16), 0x7F, dtype=torch.uint8, device="cuda")
+        codes[:, :k] = v.to(TORCH["e4m3"]).view(torch.uint8)
+        scale = torch.exp2(torch.randint(-1, 2, (-(-k // 128), -(-rows // br)), generator=g, device="cuda").float())
+        mats.append(Fp8Matrix(codes.view(TORCH["e4m3"]), scale, cols=k))
+        vals.append(v.double() * scale.t().repeat_interleave(br, 0)[:rows].repeat_interleave(128, 1)[:, :k].double())
+    ref = (vals[0] @ vals[1].t()).to(TORCH[out])
+    assert torch.equal(matmul_fp8(*mats, out_dtype=TORCH[out]), ref)
+
+
 @pytest.mark.parametrize("m,n,k", LARGE)
 @pytest.mark.parametrize("ra,rb", [(1, 128), (1, 1), (128, 1)])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
