@@ -44,6 +44,62 @@ def test_oracle_decodes_every_code():
         assert (fp8_blocks.round_to(fine, fmt) == fine).all() and fine.max() == fp8_blocks.FORMATS[fmt][2]
 
 
+def test_oracle_rounds_as_torch_does():
+    import torch
+
+    r = np.random.default_rng(3)
+    for fmt, dtype in (("e4m3", torch.float8_e4m3fn), ("e5m2", torch.float8_e5m2)):
+        v = (r.standard_normal(4000) * np.exp2(r.integers(-20, 7, 4000))).astype(np.float32)
+        ref = torch.from_numpy(v).to(dtype)
+        np.testing.assert_array_equal(fp8_blocks.round_to(v, fmt), ref.double().numpy())
+        np.testing.assert_array_equal(fp8_blocks.decode(ref.view(torch.uint8).numpy(), fmt), ref.double().numpy())
+
+
+def test_oracle_quantises_blocks():
+    x = np.zeros((130, 129))
+    x[0, 0], x[0, 128], x[129, 3] = 448.0, 1.0, -3.0
+    codes, scale = fp8_blocks.quantize(x, 128, "e4m3")
+    assert scale.tolist() == [[1.0, 2.0 ** -7], [2.0 ** -8, 2.0 ** -126]]  # 3 / 2^-7 = 384, 1 / 2^-8 = 256
+    np.testing.assert_array_equal(fp8_blocks.values(codes, scale, 128), x)
+    codes, scale = fp8_blocks.quantize(x, 1, "e4m3")
+    assert scale.shape == (2, 130) and codes[0, 128] == 256.0
+    np.testing.assert_array_equal(fp8_blocks.values(codes, scale, 1), x)
+
+
+def test_oracle_turns_pairs():
+    x = np.arange(1.0, 7.0).reshape(1, 1, 6)
+    quarter = np.array([math.pi / 2, math.pi])  # per position, of two pairs
+    np.testing.assert_allclose(rotary_oracle.rotate(x, [1], 4, "half", quarter, 1.0), [[[-3, -2, 1, -4, 5, 6]]], atol=1e-15)
+    np.testing.assert_allclose(rotary_oracle.rotate(x, [1], 4, "interleaved", quarter, 2.0), [[[-4, 2, -6, -8, 5, 6]]],
+                               atol=2e-15)
+    there = rotary_oracle.rotate(x, [7], 4, "half", quarter / 3, 1.0)
+    np.testing.assert_allclose(rotary_oracle.rotate(there, [7], 4, "half", quarter / 3, 1.0, inverse=True), x, atol=1e-14)
+
+
+def test_calls_go_to_the_tensors_device(monkeypatch):
+    """The tensors' device is the current one during a call, and the one before it again afterwards."""
+    import contextlib
+
+    import torch
+
+    from paper_2602_18851_amd import launch
+
+    seen, current = [], [0]
+
+    @contextlib.contextmanager
+    def device(index):
+        before, current[0] = current[0], index
+        yield
+        current[0] = before
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(launch, "_raw_stream", lambda index: 1000 + index)
+    for index in (0, 3):
+        launch.on_stream_of(torch.device("cuda", index), lambda *a: seen.append((current[0], *a)), "x")
+    assert seen == [(0, "x", 1000), (3, "x", 1003)] and current == [0]
+
+
 # ------------------------------------------------------------------ plans
 
 
