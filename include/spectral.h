@@ -403,12 +403,15 @@ typedef struct {
                                     (out_head >= n_tokens * out_token) */
 } sn_heads;
 
+#define SN_ROTARY_COPY_PADDING (1 << 30)
+
 /* Turns n_heads tensors (1 or 2: queries and keys) of the same tokens in one launch.
  *   dtype      SN_F32 or SN_BF16; turned in float32 and rounded once.
  *   positions  device int64 [n_tokens], or NULL: token t is at first + t.
  *              Angles are formed and reduced in double, exact to |p| 2^-48.  A
  *              token at a negative position is padding: its rows of out are left as
- *              they were.
+ *              they were or, with SN_ROTARY_COPY_PADDING, are x's own, not turned.
+ *   inverse    0, or 1 to turn back; SN_ROTARY_COPY_PADDING may be added.
  * n_tokens = 0 does nothing.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP. */
 SN_API int spectral_rotary(const sn_rotary* p, int32_t dtype, int64_t n_tokens, const int64_t* positions,
                            int64_t first, int32_t inverse, const sn_heads* heads, int32_t n_heads, void* hip_stream);

@@ -85,7 +85,8 @@ template <typename IO>
 struct HeadsArg {
   IO io;
   int32_t heads;
-  int32_t copy_rest;  // out is not x: the elements past rot_dim are copied
+  int32_t copy_rest;     // out is not x: the elements past rot_dim are copied
+  int32_t copy_padding;  // ... and so are whole rows of padding (else they are left as out holds them)
   int64_t x_token, x_head, out_token, out_head;
 };
 
@@ -145,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
     const int items = n * h.heads * chunks;
     for (int i = split * kThreads + t; i < items; i += a.splits * kThreads) {
       const int c = i % chunks, th = i / chunks, hd = th % h.heads, k = th / h.heads;
-      if (skip[k]) continue;
+      const bool pad = skip[k];
+      if (pad && !h.copy_padding) continue;
       const int64_t xi = (token0 + k) * h.x_token + hd * h.x_head, oi = (token0 + k) * h.out_token + hd * h.out_head;
       float cn[V], sn[V];
 #pragma unroll
@@ -159,6 +161,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           turn(x[2 * e], x[2 * e + 1], cn[e], sn[e], y[2 * e], y[2 * e + 1]);
+          if (pad) y[2 * e] = x[2 * e], y[2 * e + 1] = x[2 * e + 1];
         }
         h.io.store(oi + 2 * V * c, y);
       } else {
@@ -168,6 +171,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           turn(x0[e], x1[e], cn[e], sn[e], y0[e], y1[e]);
+          if (pad) y0[e] = x0[e], y1[e] = x1[e];
         }
         h.io.store(oi + V * c, y0);
         h.io.store(oi + pairs + V * c, y1);
@@ -177,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
       const int per = (rest + V - 1) / V, todo = n * h.heads * per;
       for (int i = split * kThreads + t; i < todo; i += a.splits * kThreads) {
         const int c = i % per, th = i / per, hd = th % h.heads, k = th / h.heads;
-        if (skip[k]) continue;
+        if (skip[k] && !h.copy_padding) continue;
         const int64_t xi = (token0 + k) * h.x_token + hd * h.x_head + 2 * pairs + V * c;
         const int64_t oi = (token0 + k) * h.out_token + hd * h.out_head + 2 * pairs + V * c;
         float x[V];
@@ -335,7 +339,7 @@ int run_rotary(const RotaryTable& table, int64_t n_tokens, const int64_t* positi
   a.positions = positions;
   a.first = first;
   a.n_tokens = a.period = n_tokens;
-  a.sign = inverse ? -1.f : 1.f;
+  a.sign = inverse & ~SN_ROTARY_COPY_PADDING ? -1.f : 1.f;
   a.n_tensors = n_heads;
   for (int w = 0; w < n_heads; ++w) {
     const sn_heads& s = heads[w];
@@ -343,6 +347,7 @@ int run_rotary(const RotaryTable& table, int64_t n_tokens, const int64_t* positi
     h.io = Plain<T>{static_cast<const T*>(s.x), static_cast<T*>(s.out)};
     h.heads = (int32_t)s.heads;
     h.copy_rest = s.x != s.out;
+    h.copy_padding = h.copy_rest && (inverse & SN_ROTARY_COPY_PADDING);
     h.x_token = s.x_token;
     h.x_head = s.x_head;
     h.out_token = s.out_token;

@@ -7,7 +7,7 @@ import ctypes
 import torch
 
 from .launch import on_stream_of
-from .spectral import SN_BF16, SN_F32, sn_rotary, spectral_rotary, spectral_rotary_frequencies
+from .spectral import SN_BF16, SN_F32, SN_ROTARY_COPY_PADDING, sn_rotary, spectral_rotary, spectral_rotary_frequencies
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "index": 3, "turns": 4}
@@ -36,9 +36,9 @@ class Rotary:
     def apply(self, q: torch.Tensor, k: torch.Tensor | None = None, positions: torch.Tensor | None = None,
               start: int = 0, inverse: bool = False, out=None):
         """q, k: float32 or bfloat16 [tokens, heads, head_dim], any token and head strides.  positions: int64 [tokens],
-        or None: token t is at start + t; rows of tokens at negative positions (padding) are left as out holds them.
-        inverse turns back: the gradient.  out: a tensor (with k: a pair) like q (and k), which may be the inputs
-        themselves; new tensors if None.  Returns the turned q, or (q, k)."""
+        or None: token t is at start + t; rows of tokens at negative positions (padding) are left as out holds them, and
+        are the input's own, not turned, in new tensors.  inverse turns back: the gradient.  out: a tensor (with k: a
+        pair) like q (and k), which may be the inputs themselves; new tensors if None.  Returns the turned q, or (q, k)."""
         xs = (q,) if k is None else (q, k)
         if out is None:
             outs = None
@@ -71,5 +71,6 @@ class Rotary:
                                       or positions.device != dev or not positions.is_contiguous()):
             raise ValueError(f"positions must be a contiguous int64 tensor [{n}] on {dev}")
         on_stream_of(dev, spectral_rotary, self.plan, _DTYPES[dtype], n, 0 if positions is None else positions.data_ptr(),
-                     start, 1 if inverse else 0, (ctypes.c_int64 * len(fields))(*fields), len(xs))
+                     start, (1 if inverse else 0) | (SN_ROTARY_COPY_PADDING if outs is None else 0),
+                     (ctypes.c_int64 * len(fields))(*fields), len(xs))
         return made[0] if k is None else tuple(made)

@@ -134,6 +134,38 @@ def test_padding_stays():
         assert torch.equal(o[live], r[live]) and (o[~live] == v).all()
 
 
+@pytest.mark.parametrize("d,rot", [(128, 128), (96, 40), (7, 6), (16, 12)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_padding_in_new_tensors_is_not_turned(d, rot, layout, dtype, inverse):
+    """The new tensors take memory that held NaN; their rows of padding are the input's, whatever these hold."""
+    plan = Rotary(d, rot_dim=rot, layout=layout, scaling="index", **SCALINGS["index"])
+    q, k = heads((9, 1), 21, 4, d, dtype), heads((9, 2), 21, 2, d, dtype)
+    q[3, 1, 0], q[3, 1, 1], q[20] = float("inf"), -0.0, 0.0
+    p = torch.arange(21, device="cuda")
+    p[[0, 3, 17, 20]] = torch.tensor([-1, -(1 << 40), -5, -2], device="cuda")
+
+    def poison():
+        for t in (q, k):
+            torch.full_like(t, float("nan"))
+
+    def same(a, b):  # bits, an infinity and a zero's sign among them
+        return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+    live = p >= 0
+    ref = plan.apply(q[live], k[live], positions=p[live], inverse=inverse)
+    torch.cuda.synchronize()
+    poison()
+    got = plan.apply(q, k, positions=p, inverse=inverse)
+    for o, x, r in zip(got, (q, k), ref):
+        assert same(o[live], r) and same(o[~live], x[~live])
+    ref = plan.apply(q[6:], inverse=inverse)
+    poison()
+    got = plan.apply(q, start=-6, inverse=inverse)
+    assert same(got[:6], q[:6]) and same(got[6:], ref)
+
+
 def test_many_tokens_and_far_rows():
     """More groups of tokens than one launch takes, and rows that start past 2^32 bytes."""
     plan = Rotary(2)
