@@ -113,12 +113,18 @@ def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: b
 
     a = room(r, c) if rows else None
     b = room(c, r) if cols else None
-    if r and c:
-        ra = (a.codes.data_ptr(), a.ld, a.scale.data_ptr()) if rows else (0, 0, 0)
-        cb = (b.codes.data_ptr(), b.ld, b.scale.data_ptr()) if cols else (0, 0, 0)
-        on_stream_of(dev, spectral_quantize_fp8, x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype],
-                     1 if tile else 0, *ra, *cb)
+    _quantize_into(x, ld, dtype, tile, a, b)
     return a, b
+
+
+def _quantize_into(x, ld, dtype, tile, a, b) -> None:
+    """x and its transpose into the quantiser's own matrices a and b (or None)."""
+    r, c = x.shape
+    if r and c:
+        ra = (a.codes.data_ptr(), a.ld, a.scale.data_ptr()) if a is not None else (0, 0, 0)
+        cb = (b.codes.data_ptr(), b.ld, b.scale.data_ptr()) if b is not None else (0, 0, 0)
+        on_stream_of(x.device, spectral_quantize_fp8, x.data_ptr(), r, c, ld, _CODES[x.dtype], _CODES[dtype],
+                     1 if tile else 0, *ra, *cb)
 
 
 def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
@@ -173,18 +179,22 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
 
 class LinearFp8:
     """y = x W^T with both sides in 8 bits, and its gradients.  The weight [N, K] (float32 or bfloat16) is quantised by
-    tiles, and so is its transpose for dx; ``set_weight`` does so again after an update.  ``backward=False`` (serving)
-    leaves the transpose out.  Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the
+    tiles, and so is its transpose for dx; ``set_weight`` does so again after an update, into the same memory, so that a
+    graph of the layer's calls goes on with the new weight.  ``backward=False`` (serving) leaves the transpose out.  Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the
     format of dy."""
 
     def __init__(self, weight: torch.Tensor, grad_fmt: str = "e4m3", backward: bool = True):
         if grad_fmt not in _FORMATS:
             raise ValueError("grad_fmt must be 'e4m3' or 'e5m2'")
         self.grad_fmt, self._back = grad_fmt, bool(backward)
-        self.set_weight(weight)
+        self.weight, self.weight_t = quantize_fp8(weight, tile=True, cols=self._back)
 
     def set_weight(self, weight: torch.Tensor) -> None:
-        self.weight, self.weight_t = quantize_fp8(weight, tile=True, cols=self._back)
+        """A new weight of the same shape, on the same device."""
+        ld, w = _plain(weight, "weight"), self.weight
+        if tuple(weight.shape) != (w.rows, w.cols) or weight.device != w.codes.device:
+            raise ValueError(f"weight must be [{w.rows}, {w.cols}] on {w.codes.device}")
+        _quantize_into(weight, ld, _FORMATS["e4m3"], True, w, self.weight_t)
 
     def forward(self, x: torch.Tensor, keep: bool = False, out_dtype: torch.dtype = torch.bfloat16):
         """x [M, K] -> y [M, N].  With ``keep``: (y, what backward needs of x)."""

@@ -460,6 +460,36 @@ def test_layer_step_replays_from_a_graph():
             assert torch.equal(a, b)
 
 
+def test_new_weight_reaches_a_captured_graph():
+    """The graph reads the layer's matrices where they are: set_weight rewrites them there."""
+    r = rng(28)
+    m, n, k = 70, 200, 300
+    x, w, dy = on_gpu(wide(r, m, k), "bf16"), on_gpu(0.02 * r.standard_normal((n, k)), "f32"), on_gpu(wide(r, m, n), "bf16")
+    layer = LinearFp8(w)
+
+    def step(layer):
+        y, kept = layer.forward(x, keep=True)
+        return (y, *layer.backward(dy, kept))
+
+    step(layer)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(layer)
+    places = [t.data_ptr() for m in (layer.weight, layer.weight_t) for t in (m.codes, m.scale)]
+    for rep in range(3):
+        new = on_gpu(0.02 * rng(28, rep).standard_normal((n, k)) * 4.0 ** rep, "bf16" if rep == 1 else "f32")
+        layer.set_weight(new)
+        assert places == [t.data_ptr() for m in (layer.weight, layer.weight_t) for t in (m.codes, m.scale)]
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(got, step(LinearFp8(new)), step(layer)):
+            assert torch.equal(a, b) and torch.equal(c, b)
+    for bad in (torch.zeros(n, k + 1, device="cuda"), torch.zeros(n, k), torch.zeros(k, n, device="cuda").t()):
+        with pytest.raises(ValueError):
+            layer.set_weight(bad)
+
+
 def test_calls_on_another_stream():
     a, av = matrix((23, 150, 700), 150, 700, "e4m3", 1)
     b, bv = matrix((24, 260, 700), 260, 700, "e4m3", 128)
