@@ -62,9 +62,7 @@ class Fp8Matrix:
             self.block_rows = BLOCK
         else:
             raise ValueError(f"scale must be [{kb}, {rows}] or [{kb}, {(rows + 127) // 128}], got {shape}")
-        # strides of two zeros say "dense" to the library
-        self.codes, self.scale = codes, scale if any(scale.stride()) else scale.contiguous()
-        self.rows, self.cols = rows, cols
+        self.codes, self.scale, self.rows, self.cols = codes, scale, rows, cols
 
     @classmethod
     def _made(cls, codes: torch.Tensor, scale: torch.Tensor, rows: int, cols: int, block_rows: int) -> "Fp8Matrix":
@@ -89,6 +87,13 @@ def _plain(x: torch.Tensor, name: str) -> int:
     if (cols > 1 and one != 1) or (rows > 1 and step < cols):
         raise ValueError(f"{name} must be row-major")
     return step if rows > 1 else cols
+
+
+def _scale_of(m: Fp8Matrix) -> torch.Tensor:
+    """The scales as a call reads them: one value for all is written out first, since strides of two zeros say "dense" to
+    the library."""
+    s = m.scale
+    return s if any(s.stride()) else s.contiguous()
 
 
 def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: bool = False,
@@ -140,8 +145,9 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         codes, sa, sa_block, sa_row, a_rows = a, 0, 0, 0, 1
         m, k = a.shape
     else:
-        ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a.scale.data_ptr(), a.block_rows, a.rows, a.cols
-        sa_block, sa_row = a.scale.stride()
+        a_scale = _scale_of(a)
+        ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a_scale.data_ptr(), a.block_rows, a.rows, a.cols
+        sa_block, sa_row = a_scale.stride()
     n, dev = b.rows, codes.device
     if b.cols != k:
         raise ValueError(f"a has {k} columns and b {b.cols}")
@@ -171,8 +177,9 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
         ws = workspace.data_ptr()
-    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *b.scale.stride())
-    on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b.scale.data_ptr(),
+    b_scale = _scale_of(b)
+    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *b_scale.stride())
+    on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b_scale.data_ptr(),
                  out.data_ptr(), ws, need)
     return out
 

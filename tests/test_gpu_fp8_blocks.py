@@ -251,6 +251,21 @@ def test_scales_of_any_strides(layout, m, n, k):
         check_product(matmul_fp8(a, b, out_dtype=torch.float32), av, bv, "f32")
 
 
+@pytest.mark.parametrize("m,n,k", [(5, 40, 100), (300, 260, 700)])
+def test_a_scale_of_the_whole_matrix_can_change(m, n, k):
+    """One value expanded over all blocks is read at each call, not when the matrix is made."""
+    a, _ = matrix((17, m, k), m, k, "e4m3", 1)
+    b, _ = matrix((18, n, k), n, k, "e4m3", 128)
+    sa, sb = torch.ones(1, 1, device="cuda"), torch.ones(1, 1, device="cuda")
+    a = Fp8Matrix(a.codes, sa.expand(a.scale.shape), cols=k)
+    b = Fp8Matrix(b.codes, sb.expand(b.scale.shape), cols=k)
+    ref = matmul_fp8(a, b, out_dtype=torch.float32)
+    for factor in (2.0, 0.25):
+        sa.fill_(factor)
+        sb.fill_(8.0)
+        assert torch.equal(matmul_fp8(a, b, out_dtype=torch.float32), 8 * factor * ref)
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,k", [(1, 37, 256), (70, 37, 256), (300, 515, 4000)])
 @pytest.mark.parametrize("offset,extra", [(0, 8), (1, 3), (2, 2)])
