@@ -346,6 +346,19 @@ typedef struct {
  * split over workgroups.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
 SN_API int spectral_matmul_fp8_workspace_bytes(const sn_matmul* p, int64_t* bytes);
 
+/* Which kernel the call runs (beside launches that quantise a plain A first or join parts), for labelling
+ * profiles and for tests: its kind, into how many parts the sum over k is split, and its launch; zeros where m or n is 0.
+ * Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
+typedef enum {
+  SN_MATMUL_FEW_ROWS = 1, /* B once, from memory to registers             */
+  SN_MATMUL_TILE_4 = 2,   /* tiles of 128 x 128 by 4 waves                */
+  SN_MATMUL_TILE_8 = 3,   /* ... by 8 waves, one to a compute unit        */
+  SN_MATMUL_WIDE = 4,     /* 256 x 128, large results in SN_F32           */
+  SN_MATMUL_BIG = 5       /* 256 x 256, large results in SN_BF16          */
+} sn_matmul_kernel;
+SN_API int spectral_matmul_fp8_kernel(const sn_matmul* p, int32_t* kernel, int32_t* parts, int64_t* workgroups,
+                                      int32_t* threads);
+
 /* Codes are 16-byte aligned, scales and C aligned to their type; sa is NULL
  * for a plain A.  C must not overlap the inputs.  Calls that can run at the
  * same time need workspaces of their own, graphs captured from them too.

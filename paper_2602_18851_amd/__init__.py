@@ -32,6 +32,7 @@ from .spectral import (  # noqa: F401
     spectral_logits_fp8_rotary,
     spectral_logits_workspace_bytes,
     spectral_matmul_fp8,
+    spectral_matmul_fp8_kernel,
     spectral_matmul_fp8_workspace_bytes,
     spectral_profile,
     spectral_profile_read,

@@ -839,49 +839,41 @@ __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
   }
 }
 
+// What a call runs: sn_matmul_kernel, and its workgroups of so many threads.
+struct Run {
+  int32_t kernel, threads;
+  int64_t workgroups;
+};
+
 template <int FA, int FB, bool ROWS_B>
-void launch2(const MatArgs& args, bool big, bool bf16, hipStream_t st) {
-  MatArgs a = args;
-  auto tiles = [&](int tm, int tn) {
-    a.tiles_m = (int32_t)((a.m + tm - 1) / tm);
-    a.tiles_n = (int32_t)((a.n + tn - 1) / tn);
-    return dim3((uint32_t)(((int64_t)a.tiles_m * a.tiles_n * a.splits + 7) / 8 * 8));
-  };
-  if (big) {
-    if (bf16) {
-      const dim3 g = tiles(kBT, kBT);
-      big_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
-    } else {
-      const dim3 g = tiles(kWM, kWN);
-      wide_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
-    }
-    return;
-  }
-  const dim3 g = tiles(kT, kT);
-  // a workgroup alone on its compute unit: 8 waves (512 x 8192 x 8192 to bf16 48.6 us with 4, 44.6 with 8); else two of 4
-  // (1024 x 8192 x 8192 71.9 with 4, 74.2 with 8)
-  if ((int64_t)a.tiles_m * a.tiles_n * a.splits <= 256)
-    bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 8><<<g, 512, 0, st>>>(a)
-         : tile_kernel<FA, FB, ROWS_B, float, 8><<<g, 512, 0, st>>>(a);
-  else
-    bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 4><<<g, 256, 0, st>>>(a)
-         : tile_kernel<FA, FB, ROWS_B, float, 4><<<g, 256, 0, st>>>(a);
-  if (a.splits > 1) {
-    const dim3 j((uint32_t)std::min<int64_t>((a.m * (a.ld_parts / 4) + 255) / 256, 4096));
-    bf16 ? join_kernel<__bf16><<<j, 256, 0, st>>>(a) : join_kernel<float><<<j, 256, 0, st>>>(a);
+void launch2(const MatArgs& a, const Run& run, bool bf16, hipStream_t st) {
+  const dim3 g((uint32_t)run.workgroups);
+  switch (run.kernel) {
+    case SN_MATMUL_BIG: return big_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
+    case SN_MATMUL_WIDE: return wide_kernel<FA, FB, ROWS_B><<<g, 512, 0, st>>>(a);
+    case SN_MATMUL_TILE_8:
+      return bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 8><<<g, 512, 0, st>>>(a)
+                  : tile_kernel<FA, FB, ROWS_B, float, 8><<<g, 512, 0, st>>>(a);
+    default:
+      return bf16 ? tile_kernel<FA, FB, ROWS_B, __bf16, 4><<<g, 256, 0, st>>>(a)
+                  : tile_kernel<FA, FB, ROWS_B, float, 4><<<g, 256, 0, st>>>(a);
   }
 }
 
 template <int FA, int FB>
-void launch1(const MatArgs& a, bool big, bool bf16, hipStream_t st) {
-  a.b_shift ? launch2<FA, FB, false>(a, big, bf16, st) : launch2<FA, FB, true>(a, big, bf16, st);
+void launch1(const MatArgs& a, const Run& run, bool bf16, hipStream_t st) {
+  a.b_shift ? launch2<FA, FB, false>(a, run, bf16, st) : launch2<FA, FB, true>(a, run, bf16, st);
 }
 
-void launch(const MatArgs& a, bool fa, bool fb, bool big, bool bf16, hipStream_t st) {
+void launch_tiles(const MatArgs& a, const Run& run, bool fa, bool fb, bool bf16, hipStream_t st) {
   if (fa)
-    fb ? launch1<1, 1>(a, big, bf16, st) : launch1<1, 0>(a, big, bf16, st);
+    fb ? launch1<1, 1>(a, run, bf16, st) : launch1<1, 0>(a, run, bf16, st);
   else
-    fb ? launch1<0, 1>(a, big, bf16, st) : launch1<0, 0>(a, big, bf16, st);
+    fb ? launch1<0, 1>(a, run, bf16, st) : launch1<0, 0>(a, run, bf16, st);
+  if (a.splits > 1) {
+    const dim3 j((uint32_t)std::min<int64_t>((a.m * (a.ld_parts / 4) + 255) / 256, 4096));
+    bf16 ? join_kernel<__bf16><<<j, 256, 0, st>>>(a) : join_kernel<float><<<j, 256, 0, st>>>(a);
+  }
 }
 
 // ------------------------------------------------------------------ host side
@@ -909,24 +901,24 @@ double few_cost(int64_t m, int64_t n, int64_t k) {
 int64_t plain_bytes(int64_t m, int64_t k) { return m * ((k + 127) / 128) * (128 + 4); }
 
 template <int FA, int FB>
-void launch_few(const MatArgs& a, int plain, hipStream_t st) {
+void launch_few(const MatArgs& a, const Run& run, int plain, hipStream_t st) {
   const int t = (int)((a.m + 15) / 16);
-  const dim3 one((uint32_t)((a.n + 15) / 16)), two((uint32_t)((a.n + 31) / 32));
+  const dim3 g((uint32_t)run.workgroups);
   constexpr int W = 64 * kFewWaves;
   if constexpr (FA == 0) {
     const size_t lds = (size_t)plain_bytes(a.m, a.k);
     if (plain == 1)
-      return t == 1 ? few_rows_kernel<1, 1, 1, FA, FB><<<one, W, lds, st>>>(a)
-                    : few_rows_kernel<2, 1, 1, FA, FB><<<one, W, lds, st>>>(a);
+      return t == 1 ? few_rows_kernel<1, 1, 1, FA, FB><<<g, W, lds, st>>>(a)
+                    : few_rows_kernel<2, 1, 1, FA, FB><<<g, W, lds, st>>>(a);
     if (plain == 2)
-      return t == 1 ? few_rows_kernel<1, 1, 2, FA, FB><<<one, W, lds, st>>>(a)
-                    : few_rows_kernel<2, 1, 2, FA, FB><<<one, W, lds, st>>>(a);
+      return t == 1 ? few_rows_kernel<1, 1, 2, FA, FB><<<g, W, lds, st>>>(a)
+                    : few_rows_kernel<2, 1, 2, FA, FB><<<g, W, lds, st>>>(a);
   }
   switch (t) {
-    case 1: return few_rows_kernel<1, 1, 0, FA, FB><<<one, W, 0, st>>>(a);
-    case 2: return few_rows_kernel<2, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
-    case 3: return few_rows_kernel<3, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
-    default: return few_rows_kernel<4, 2, 0, FA, FB><<<two, W, 0, st>>>(a);
+    case 1: return few_rows_kernel<1, 1, 0, FA, FB><<<g, W, 0, st>>>(a);
+    case 2: return few_rows_kernel<2, 2, 0, FA, FB><<<g, W, 0, st>>>(a);
+    case 3: return few_rows_kernel<3, 2, 0, FA, FB><<<g, W, 0, st>>>(a);
+    default: return few_rows_kernel<4, 2, 0, FA, FB><<<g, W, 0, st>>>(a);
   }
 }
 
@@ -971,6 +963,8 @@ Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
 
 struct MatPlan {
   Way way;
+  Run run;
+  int32_t tiles_m, tiles_n;
   int64_t off_parts, ld_parts;
   bool plain_a;
   bool few;   // the kernel for few rows
@@ -978,6 +972,26 @@ struct MatPlan {
   int64_t ld_codes;  // of a plain A's codes
   int64_t off_scale, bytes;
 };
+
+// The launch of the kernel that the plan chose.
+void set_run(const sn_matmul& p, MatPlan& pl) {
+  if (pl.few) {
+    const int64_t cols = p.m <= 16 || pl.fuse ? 16 : 32;  // of C that a workgroup takes
+    pl.run = Run{SN_MATMUL_FEW_ROWS, 64 * kFewWaves, (p.n + cols - 1) / cols};
+    return;
+  }
+  const bool f32 = p.c_type == SN_F32;
+  const int tm = !pl.way.big ? kT : f32 ? kWM : kBT, tn = !pl.way.big ? kT : f32 ? kWN : kBT;
+  pl.tiles_m = (int32_t)((p.m + tm - 1) / tm);
+  pl.tiles_n = (int32_t)((p.n + tn - 1) / tn);
+  const int64_t units = (int64_t)pl.tiles_m * pl.tiles_n * pl.way.splits;
+  // a 128 x 128 tile alone on its compute unit: 8 waves (512 x 8192 x 8192 to bf16 48.6 us with 4, 44.6 with 8); else two
+  // of 4 (1024 x 8192 x 8192 71.9 with 4, 74.2 with 8)
+  const bool eight = pl.way.big || units <= 256;
+  pl.run.kernel = !pl.way.big ? (eight ? SN_MATMUL_TILE_8 : SN_MATMUL_TILE_4) : f32 ? SN_MATMUL_WIDE : SN_MATMUL_BIG;
+  pl.run.threads = eight ? 512 : 256;
+  pl.run.workgroups = (units + 7) / 8 * 8;  // whole rounds of the XCDs
+}
 
 // Checks the description and fills in its defaults.
 int resolve(sn_matmul& p, MatPlan& pl) {
@@ -1036,6 +1050,7 @@ int resolve(sn_matmul& p, MatPlan& pl) {
       pl.bytes += round_up(pl.way.splits * p.m * pl.ld_parts * 4, 256);
     }
   }
+  if (p.m > 0 && p.n > 0) set_run(p, pl);
   return SN_OK;
 }
 
@@ -1047,6 +1062,20 @@ extern "C" SN_API int spectral_matmul_fp8_workspace_bytes(const sn_matmul* desc,
   MatPlan pl;
   if (int rc = resolve(p, pl)) return rc;
   *bytes = pl.bytes;
+  return SN_OK;
+}
+
+extern "C" SN_API int spectral_matmul_fp8_kernel(const sn_matmul* desc, int32_t* kernel, int32_t* parts,
+                                                 int64_t* workgroups, int32_t* threads) {
+  if (!desc || !kernel || !parts || !workgroups || !threads)
+    return refuse(SN_ENULL, "p, kernel, parts, workgroups and threads must not be NULL");
+  sn_matmul p = *desc;
+  MatPlan pl;
+  if (int rc = resolve(p, pl)) return rc;
+  *kernel = pl.run.kernel;
+  *parts = pl.run.kernel == 0 ? 0 : pl.few ? 1 : pl.way.splits;
+  *workgroups = pl.run.workgroups;
+  *threads = pl.run.threads;
   return SN_OK;
 }
 
@@ -1114,14 +1143,16 @@ extern "C" SN_API int spectral_matmul_fp8(const sn_matmul* desc, const void* a, 
   g.blocks_per_split = pl.way.blocks_per_split;
   g.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + pl.off_parts);
   g.ld_parts = pl.ld_parts;
+  g.tiles_m = pl.tiles_m;
+  g.tiles_n = pl.tiles_n;
   if (pl.few) {
     const int plain = !pl.fuse ? 0 : p.a_type == SN_BF16 ? 1 : 2;
     if (fa)
-      fb ? launch_few<1, 1>(g, plain, st) : launch_few<1, 0>(g, plain, st);
+      fb ? launch_few<1, 1>(g, pl.run, plain, st) : launch_few<1, 0>(g, pl.run, plain, st);
     else
-      fb ? launch_few<0, 1>(g, plain, st) : launch_few<0, 0>(g, plain, st);
+      fb ? launch_few<0, 1>(g, pl.run, plain, st) : launch_few<0, 0>(g, pl.run, plain, st);
   } else {
-    launch(g, fa, fb, pl.way.big, g.c_bf16 != 0, st);
+    launch_tiles(g, pl.run, fa, fb, g.c_bf16 != 0, st);
   }
   return sn::launched("product");
 }

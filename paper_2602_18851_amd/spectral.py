@@ -46,6 +46,7 @@ EXPORTED = (
     "spectral_logits_fp8_rotary",
     "spectral_quantize_fp8",
     "spectral_matmul_fp8_workspace_bytes",
+    "spectral_matmul_fp8_kernel",
     "spectral_matmul_fp8",
     "spectral_rotary_frequencies",
     "spectral_rotary",
@@ -183,6 +184,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.spectral_quantize_fp8.restype = ctypes.c_int
     lib.spectral_matmul_fp8_workspace_bytes.argtypes = [ctypes.POINTER(sn_matmul), ctypes.POINTER(i64)]
     lib.spectral_matmul_fp8_workspace_bytes.restype = ctypes.c_int
+    lib.spectral_matmul_fp8_kernel.argtypes = [ctypes.POINTER(sn_matmul), ctypes.POINTER(i32), ctypes.POINTER(i32),
+                                               ctypes.POINTER(i64), ctypes.POINTER(i32)]
+    lib.spectral_matmul_fp8_kernel.restype = ctypes.c_int
     lib.spectral_matmul_fp8.argtypes = [ctypes.POINTER(sn_matmul), vp, vp, vp, vp, vp, vp, i64, vp]
     lib.spectral_matmul_fp8.restype = ctypes.c_int
     lib.spectral_rotary_frequencies.argtypes = [ctypes.POINTER(sn_rotary), dp, dp]
@@ -345,6 +349,18 @@ def spectral_matmul_fp8_workspace_bytes(p: sn_matmul) -> int:
     out = ctypes.c_int64(0)
     _check(load_library().spectral_matmul_fp8_workspace_bytes(ctypes.byref(p), ctypes.byref(out)))
     return out.value
+
+
+MATMUL_KERNELS = ("none", "few_rows", "tile_4", "tile_8", "wide", "big")
+
+
+def spectral_matmul_fp8_kernel(p: sn_matmul) -> tuple[str, int, int, int]:
+    """(name of the kernel, parts of the sum, workgroups, threads of each) of a product."""
+    kernel, parts, threads = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
+    workgroups = ctypes.c_int64()
+    _check(load_library().spectral_matmul_fp8_kernel(ctypes.byref(p), ctypes.byref(kernel), ctypes.byref(parts),
+                                                     ctypes.byref(workgroups), ctypes.byref(threads)))
+    return MATMUL_KERNELS[kernel.value], parts.value, workgroups.value, threads.value
 
 
 def spectral_matmul_fp8(p: sn_matmul, a: int, sa: int, b: int, sb: int, c: int, workspace: int, workspace_bytes: int,

@@ -233,6 +233,25 @@ def test_empty_products_do_nothing(lib):  # noqa: F811
     assert lib.spectral_matmul_fp8_workspace_bytes(None, None) == sp.SN_ENULL
 
 
+@pytest.mark.parametrize("want,kw", [
+    (("none", 0, 0, 0), dict(m=0)), (("none", 0, 0, 0), dict(n=0)), (("few_rows", 1, 1, 512), dict(k=0, n=16)),
+    (("few_rows", 1, 512, 512), dict(m=1, n=8192, k=8192, a_type=sp.SN_BF16)),
+    (("few_rows", 1, 100, 512), dict(m=24, n=1600, k=1600, a_type=sp.SN_BF16)),  # 16 rows of B each, A quantised there
+    (("few_rows", 1, 50, 512), dict(m=24, n=1600, k=1600)),                      # 32 rows of B each
+    (("tile_8", 4, 256, 512), dict(m=1001, n=999, k=3001, b_block_rows=1, c_type=sp.SN_F32)),
+    (("tile_8", 1, 256, 512), dict(m=512, n=8192, k=8192)), (("tile_4", 1, 512, 256), dict(m=1024, n=8192, k=8192)),
+    (("big", 1, 1024, 512), dict(m=8192, n=8192, k=8192)), (("wide", 1, 256, 512), dict(m=1024, n=8192, k=16384, c_type=sp.SN_F32)),
+    (("tile_4", 1, 512, 256), dict(m=1024, n=8192, k=16384, c_type=sp.SN_F32, sa_row=1 << 20))])
+def test_kernels_of_products(lib, want, kw):  # noqa: F811
+    assert sp.spectral_matmul_fp8_kernel(matmul(**kw)) == want
+
+
+def test_kernel_query_refuses(lib):  # noqa: F811
+    refused(sp.SN_EINVAL, sp.spectral_matmul_fp8_kernel, matmul(m=-1))
+    assert lib.spectral_matmul_fp8_kernel(None, None, None, None, None) == sp.SN_ENULL
+    assert lib.spectral_matmul_fp8_kernel(ctypes.byref(matmul()), None, None, None, None) == sp.SN_ENULL
+
+
 def test_plain_operand_needs_room_for_its_codes(lib):  # noqa: F811
     got = sp.spectral_matmul_fp8_workspace_bytes(matmul(a_type=sp.SN_BF16, m=100, k=1000))
     assert got >= 100 * 1008 + 8 * 100 * 4
