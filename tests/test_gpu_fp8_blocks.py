@@ -322,6 +322,102 @@ def test_codes_that_are_not_finite(m, n, k, fmt, bad, out):
     assert torch.equal(got[rest], ref[rest])
 
 
+# The kernels of the large products, each at sizes that the choice gives it (checked, so that other costs in it cannot take the
+# coverage away): ragged rows, columns and sums, long sums, sums in parts.
+KERNELS = [("big", 1, "bf16", 3100, 3300, 1000), ("big", 1, "bf16", 4050, 4003, 2500), ("wide", 1, "f32", 2100, 2201, 1500),
+           ("wide", 1, "f32", 4050, 2043, 2507), ("tile_4", 1, "bf16", 2100, 2203, 1500), ("tile_4", 1, "f32", 300, 21700, 700),
+           ("tile_4", 3, "bf16", 1700, 1501, 16384), ("tile_4", 3, "f32", 1700, 1502, 16390), ("tile_8", 1, "bf16", 1030, 3002, 1900),
+           ("tile_8", 2, "f32", 1300, 1298, 9000)]
+FORMATS = [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2"), ("e5m2", "e5m2")]
+SHARED = [((1, 128), "dense"), ((1, 1), "transposed"), ((128, 128), "strided"), ((128, 1), "dense")]  # rows to a scale, its strides
+
+
+def pinned(kernel, parts, a, b, out):
+    from paper_2602_18851_amd import sn_matmul, spectral_matmul_fp8_kernel
+    from paper_2602_18851_amd.fp8_blocks import _CODES
+
+    got = spectral_matmul_fp8_kernel(sn_matmul(a.rows, b.rows, a.cols, _CODES[a.codes.dtype], _CODES[b.codes.dtype],
+                                               _CODES[TORCH[out]], a.block_rows, b.block_rows, a.ld, b.ld))
+    assert got[:2] == (kernel, parts)
+
+
+def gpu_matrix(seed, rows, cols, fmt, block_rows, layout, whole=False):
+    """A matrix made on the GPU, NaN codes past its columns, and its values in float64.  whole: numbers up to 4 with powers of
+    two as scales, whose products sum exactly in float32; else codes of all sizes with scales of any value."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    if whole:
+        v = torch.randint(-4, 5, (rows, cols), generator=g, device="cuda").float()
+    else:
+        v = torch.randn(rows, cols, generator=g, device="cuda")
+        v *= torch.exp2(torch.randint(-6, 7, (rows, 1), generator=g, device="cuda").float())
+        v = (v * torch.exp2(torch.randint(-3, 4, (1, cols), generator=g, device="cuda").float())).clamp(-400, 400)
+    v = v.to(TORCH[fmt])
+    codes = torch.full((rows, -(-cols // 16) * 16 + 16 * (seed % 3)), 0x7F, dtype=torch.uint8, device="cuda")
+    codes[:, :cols] = v.view(torch.uint8)
+    shape = -(-cols // 128), -(-rows // block_rows)
+    scale = torch.randint(-1, 2, shape, generator=g, device="cuda").float() if whole else \
+        8 * torch.rand(shape, generator=g, device="cuda") - 4
+    scale = torch.exp2(scale)
+    if layout == "transposed":
+        scale = scale.t().contiguous().t()
+    elif layout == "strided":
+        scale = torch.stack([scale, torch.full_like(scale, float("nan"))], dim=2)[:, :, 0]
+    of = scale.double().t().repeat_interleave(block_rows, 0)[:rows].repeat_interleave(128, 1)[:, :cols]
+    return Fp8Matrix(codes.view(TORCH[fmt]), scale, cols=cols), v.double() * of
+
+
+@pytest.mark.parametrize("kernel,parts,out,m,n,k", KERNELS)
+@pytest.mark.parametrize("fa,fb", FORMATS)
+@pytest.mark.parametrize("shared", SHARED)
+def test_every_kernel_sums_whole_numbers_exactly(kernel, parts, out, m, n, k, fa, fb, shared):
+    (ra, rb), layout = shared
+    a, av = gpu_matrix(1, m, k, fa, ra, layout, whole=True)
+    b, bv = gpu_matrix(2, n, k, fb, rb, layout, whole=True)
+    pinned(kernel, parts, a, b, out)
+    ref = (av @ bv.t()).to(TORCH[out])
+    assert torch.equal(matmul_fp8(a, b, out_dtype=TORCH[out]), ref)
+    # into a window that starts at an odd element of rows of an odd length: what lies around it stays
+    room = torch.full((m + 1, n + 4 + (n + 1) % 2), 7.0, dtype=TORCH[out], device="cuda")
+    assert torch.equal(matmul_fp8(a, b, out=room[:m, 1:1 + n]), ref)
+    room[:m, 1:1 + n] = 7.0
+    assert (room == 7.0).all()
+
+
+@pytest.mark.parametrize("kernel,parts,out,m,n,k", KERNELS)
+@pytest.mark.parametrize("fa,fb", FORMATS)
+@pytest.mark.parametrize("shared", SHARED)
+def test_every_kernel_with_codes_of_all_sizes(kernel, parts, out, m, n, k, fa, fb, shared):
+    """The tolerance of check_product, formed on the GPU."""
+    (ra, rb), layout = shared
+    a, av = gpu_matrix(3, m, k, fa, ra, layout)
+    b, bv = gpu_matrix(4, n, k, fb, rb, layout)
+    pinned(kernel, parts, a, b, out)
+    got = matmul_fp8(a, b, out_dtype=TORCH[out])
+    ref = av @ bv.t()
+    tol = (2 * 128 + 3 + -(-k // 128) + 64) * 2.0 ** -24 + (7 * 2.0 ** -13 if out == "bf16" else 0.0)
+    tol = tol * (av.abs_() @ bv.abs_().t()) + ref.abs() * (2.0 ** -8 if out == "bf16" else 2.0 ** -24) + 1e-40
+    assert ((got.double() - ref).abs_() <= tol).all()
+    assert torch.equal(got, matmul_fp8(a, b, out_dtype=TORCH[out]))  # the same bits again
+
+
+@pytest.mark.parametrize("kernel,parts,out,m,n,k", KERNELS)
+@pytest.mark.parametrize("fa,bad_a", [("e4m3", 0x7F), ("e5m2", 0x7C), ("e5m2", 0xFD)])
+@pytest.mark.parametrize("rb", [1, 128])
+def test_every_kernel_keeps_codes_that_are_not_finite_in_their_row_and_column(kernel, parts, out, m, n, k, fa, bad_a, rb):
+    a, _ = gpu_matrix(5, m, k, fa, 1, "dense")
+    b, _ = gpu_matrix(6, n, k, "e4m3", rb, "dense")
+    pinned(kernel, parts, a, b, out)
+    ref = matmul_fp8(a, b, out_dtype=TORCH[out])
+    assert torch.isfinite(ref).all()
+    i, j = m - 2, n // 3
+    a.codes.view(torch.uint8)[i, k - 1] = bad_a
+    b.codes.view(torch.uint8)[j, 0] = 0xFF
+    got = matmul_fp8(a, b, out_dtype=TORCH[out])
+    assert not torch.isfinite(got[i]).any() and torch.isnan(got[:, j]).all()
+    got[i], got[:, j] = ref[i], ref[:, j]
+    assert torch.equal(got, ref)
+
+
 def test_rows_beyond_32_bit_offsets():
     """Windows of matrices of 5 GB: their last rows start past 2^32 bytes."""
     m, k = 41000, 200
