@@ -1034,7 +1034,8 @@ int resolve(sn_matmul& p, MatPlan& pl) {
   pl.way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
   // within 2 us the kernel for few rows: its sums are the more exact ones, and it takes a plain A without a launch more
   // (the choice is the same for codes, so that both give the same bits)
-  pl.few = p.m <= kFewRows && p.m > 0 && p.n < (int64_t(1) << 27) &&  // a launch has at most 2^32 lanes
+  // 512 lanes for 16 columns of C have to stay below the 2^32 of a launch
+  pl.few = p.m <= kFewRows && p.m > 0 && p.n <= (int64_t(1) << 27) - 16 &&
            few_cost(p.m, p.n, p.k) <= pl.way.cost + 2.0;
   pl.fuse = pl.few && plain && p.m <= 32 && plain_bytes(p.m, p.k) <= kPlainBytes;
   if (plain && !pl.fuse && p.m > 0 && p.k > 0) {

@@ -246,6 +246,20 @@ def test_kernels_of_products(lib, want, kw):  # noqa: F811
     assert sp.spectral_matmul_fp8_kernel(matmul(**kw)) == want
 
 
+@pytest.mark.parametrize("m", [1, 16, 17, 64, 65, 300])
+@pytest.mark.parametrize("k", [1, 768, 1024, 1 << 20])
+@pytest.mark.parametrize("c", [sp.SN_F32, sp.SN_BF16])
+def test_launches_stay_below_32_bits_of_lanes(lib, m, k, c):  # noqa: F811
+    sizes = [b + d for b in (1 << 22, 1 << 27, 1 << 28, 1 << 29) for d in (-33, -32, -17, -16, -15, -1, 0, 1, 16)]
+    run = 0
+    for n in sizes:
+        if -(-m // 128) * -(-n // 128) < 1 << 22:
+            _, _, workgroups, threads = sp.spectral_matmul_fp8_kernel(matmul(m=m, n=n, k=k, c_type=c))
+            assert 0 < workgroups * threads < 1 << 32, n
+            run += 1
+    assert run
+
+
 def test_kernel_query_refuses(lib):  # noqa: F811
     refused(sp.SN_EINVAL, sp.spectral_matmul_fp8_kernel, matmul(m=-1))
     assert lib.spectral_matmul_fp8_kernel(None, None, None, None, None) == sp.SN_ENULL
