@@ -299,13 +299,13 @@ SN_API int spectral_logits_fp8(sn_ctx* ctx, const void* const* x_layers, int64_t
  * below cols and rows.  Codes are written up to the next multiple of 16
  * columns, zeros past the last.  One of row_codes and col_codes is required,
  * each with its scale.  Outputs must not overlap x or each other.  rows x cols
- * stays below 2^24 tiles of 128 x 128; rows = 0 or cols = 0 does nothing.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE,
- * SN_EHIP.
+ * stays below 2^24 tiles of 128 x 128; rows = 0 or cols = 0 does nothing.  Errors:
+ * SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP.
  *
  * These calls and spectral_rotary need no context: they queue on hip_stream
- * (NULL: the default stream), which belongs to the current HIP device, as
- * the pointers do (else SN_ESTATE), allocate nothing, never wait, and can be
- * captured into a HIP graph. */
+ * (NULL: the default stream), which has to belong to the current HIP device (else
+ * SN_ESTATE), allocate nothing, never wait, and can be captured into a HIP
+ * graph.  The pointers are of that device; this is not checked. */
 SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t cols, int64_t ld_x, int32_t dtype,
                                  int32_t format, int32_t tiles, uint8_t* row_codes, int64_t ld_row,
                                  float* row_scale, uint8_t* col_codes, int64_t ld_col, float* col_scale,
@@ -314,13 +314,19 @@ SN_API int spectral_quantize_fp8(const void* x, int64_t rows, int64_t cols, int6
 /* C = A B^T of two such matrices, A [m][k] and B [n][k]:
  *     C[i][j] = sum_b sA[b][i / ra] sB[b][j / rb] sum_{c in block b} A[i][c] B[j][c],
  * the inner sums on the matrix cores, the outer in float32, rounded once to
- * C's type.  With C in SN_F32 the products are exact and summed in float32.  With C in
- * SN_BF16 the matrix cores add them in eights, each kept to 2^-13 of its eight's
- * largest (a normal block's sum to 1.5e-5 of itself), at twice the rate.  The three products of a linear layer y = x W^T are of this form:
+ * C's type.  With C in SN_F32 the products are exact and summed in float32.  With
+ * C in SN_BF16 the matrix cores may add them in eights, each kept to 2^-13 of its
+ * eight's largest (a normal block's sum to 1.5e-5 of itself), at twice the rate;
+ * where the terms cancel to less than 2^-5 of their size and that shows, take
+ * SN_F32 and round.  Which kernel runs (spectral_matmul_fp8_kernel), and so the
+ * last bits of a row of C, depends on m, n and k; the same call gives the same bits.
+ * The three products of a linear layer y = x W^T are of this form:
  * y from x by rows and W by tiles, dx = dy W from dy by rows and W's
  * transpose by tiles, dW = dy^T x from the transposes of dy and x.
- * The products sA sB are formed in float32 and have to stay below its largest
- * value.  Every row of codes, the last one too, holds k rounded up to 16 bytes; those past
+ * The products sA sB are formed in float32, before they meet the inner sums: they
+ * have to stay below its largest value, and below 2^-126 (its smallest normal
+ * value) they lose digits, below 2^-149 their block's share of C.  Every row of
+ * codes, the last one too, holds k rounded up to 16 bytes; those past
  * column k are not used. */
 typedef struct {
   int64_t m, n, k;          /* >= 0 (k = 0: C is zero); m x n below 2^22 tiles of

@@ -135,7 +135,9 @@ def _quantize_into(x, ld, dtype, tile, a, b) -> None:
 def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:
     """a b^T: a [M, K] an Fp8Matrix, or a float32 or bfloat16 tensor that is quantised by rows to E4M3 on the way; b
-    [N, K] an Fp8Matrix.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8 scratch for callers
+    [N, K] an Fp8Matrix.  A float32 result sums exact products in float32; for a bfloat16 one the matrix cores may add them in
+    eights, each kept to 2^-13 of its eight's largest (include/spectral.h).  Scales: any whose products of one of a and one
+    of b lie between 2^-126 and the largest float32.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8 scratch for callers
     that keep it (a new tensor where it is too small); calls that can run at the same time need their own."""
     if not isinstance(b, Fp8Matrix):
         raise ValueError("b must be an Fp8Matrix")

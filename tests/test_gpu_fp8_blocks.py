@@ -418,6 +418,34 @@ def test_every_kernel_keeps_codes_that_are_not_finite_in_their_row_and_column(ke
     assert torch.equal(got, ref)
 
 
+@pytest.mark.parametrize("kernel,parts,out,m,n,k", KERNELS + [("few_rows", 1, "f32", 9, 700, 1500), ("few_rows", 1, "bf16", 40, 700, 1500)])
+@pytest.mark.parametrize("ea,eb", [(-63, -63), (-126, 0), (20, -123), (63, 40), (126, -126)])
+@pytest.mark.parametrize("rb", [1, 128])
+def test_scales_at_the_ends_of_the_range(kernel, parts, out, m, n, k, ea, eb, rb):
+    """Products of scales from 2^-126, the smallest that keeps all digits, to 2^103 (C below 2^127), and scales far apart, against
+    the same call with scales near one: a power of two changes no digit of a C that is normal itself."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    mats = []
+    for rows, block_rows in ((m, 1), (n, rb)):  # codes up to 4: a block's sum stays below 2^11
+        v = torch.randint(-4, 5, (rows, k), generator=g, device="cuda").float()
+        codes = torch.zeros(rows, -(-k // 16) * 16, dtype=torch.uint8, device="cuda")
+        codes[:, :k] = v.to(TORCH["e4m3"]).view(torch.uint8)
+        scale = 1 + 0.5 * torch.rand(-(-k // 128), -(-rows // block_rows), generator=g, device="cuda")
+        mats.append((codes.view(TORCH["e4m3"]), scale))
+    (a, sa), (b, sb) = mats
+
+    def call(ea, eb):
+        p, q = (Fp8Matrix(c, s * 2.0 ** e, cols=k) for (c, s), e in (((a, sa), ea), ((b, sb), eb)))
+        pinned(kernel, parts, p, q, out)
+        return matmul_fp8(p, q, out_dtype=TORCH[out]).double()
+
+    want = call(0, 0) * 2.0 ** (ea + eb)
+    got = call(ea, eb)
+    # sums that cancel below the smallest normal value are rounded to its 2^-149 (bf16: 2^-133) at every block
+    sub = 2.0 ** -126 * 2.0 ** (-7 if out == "bf16" else -23) * (2 + k // 128)
+    assert torch.isfinite(got).all() and ((got - want).abs() <= sub).all()
+
+
 def test_rows_beyond_32_bit_offsets():
     """Windows of matrices of 5 GB: their last rows start past 2^32 bytes."""
     m, k = 41000, 200
