@@ -407,8 +407,8 @@ typedef struct {
   int64_t trained;    /* T >= 1; INDEX and TURNS only                          */
 } sn_rotary;
 
-/* The rot_dim / 2 angles per position (radians) and the amplitude of a plan
- * (host doubles).  Errors: SN_ENULL, SN_EINVAL. */
+/* The rot_dim / 2 angles per position (radians) and the amplitude, to float32, of
+ * a plan (host doubles).  Errors: SN_ENULL, SN_EINVAL. */
 SN_API int spectral_rotary_frequencies(const sn_rotary* p, double* freq, double* amplitude);
 
 /* One tensor of heads: element e of head h of token t is at
@@ -427,7 +427,8 @@ typedef struct {
 /* Turns n_heads tensors (1 or 2: queries and keys) of the same tokens in one launch.
  *   dtype      SN_F32 or SN_BF16; turned in float32 and rounded once.
  *   positions  device int64 [n_tokens], or NULL: token t is at first + t.
- *              Angles are formed and reduced in double, exact to |p| 2^-48.  A
+ *              Angles are formed and reduced in double, exact to |p| 2^-48, and
+ *              their cosines and sines, times the amplitude, rounded to float32 once.  A
  *              token at a negative position is padding: its rows of out are left as
  *              they were or, with SN_ROTARY_COPY_PADDING, are x's own, not turned.
  *   inverse    0, or 1 to turn back; SN_ROTARY_COPY_PADDING may be added.

@@ -14,7 +14,7 @@ constexpr int kMaxPairs = 128;  // rot_dim <= 256
 // What a launch needs of a plan, passed by value: pair frequencies in turns per position.
 struct RotaryTable {
   double turns[kMaxPairs];
-  float amplitude;
+  double amplitude;
   int32_t pairs, head_dim, interleaved;
 };
 

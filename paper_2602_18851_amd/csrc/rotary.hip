@@ -1,9 +1,9 @@
 // Rotary positions of queries and keys (spectral_rotary; Sec. 3.3 of the paper): pairs (x0, x1) of a head turn by
 // p f_i, the token's position times the pair's frequency, or back.
 //
-// A far position's angle is many turns: p f_i is formed in turns in double, its
-// whole part taken off exactly (one fused multiply-add), and only the rest, at
-// most half a turn, is rounded to float for the sine and cosine.
+// A far position's angle is many turns: p f_i is formed in turns in double and its
+// whole part taken off exactly (one fused multiply-add).  The sine and cosine of the rest,
+// at most half a turn, are formed in double too, and rounded to float once, with the amplitude.
 
 #include <hip/hip_runtime.h>
 
@@ -108,6 +108,29 @@ __device__ __forceinline__ void turn(float x0, float x1, float c, float s, float
   y1 = fmaf(x0, s, x1 * c);
 }
 
+// Sine and cosine of r turns, |r| <= 1/2, to 2^-34 of themselves: the quarter turns off, then the Taylor series of the rest, at
+// most an eighth of a turn.
+__device__ __forceinline__ void sine_cosine(double r, double& sn, double& cn) {
+  const double quarters = rint(4.0 * r);
+  const double x = fma(quarters, -0.25, r) * 6.283185307179586476925, x2 = x * x;
+  double s = -1.0 / 39916800.0, c = 1.0 / 479001600.0;
+  s = fma(s, x2, 1.0 / 362880.0);
+  c = fma(c, x2, -1.0 / 3628800.0);
+  s = fma(s, x2, -1.0 / 5040.0);
+  c = fma(c, x2, 1.0 / 40320.0);
+  s = fma(s, x2, 1.0 / 120.0);
+  c = fma(c, x2, -1.0 / 720.0);
+  s = fma(s, x2, -1.0 / 6.0);
+  c = fma(c, x2, 1.0 / 24.0);
+  s = fma(s * x2, x, x);
+  c = fma(c, x2, -0.5);
+  c = fma(c, x2, 1.0);
+  const int q = (int)quarters;  // -2 .. 2
+  const double a = q & 1 ? c : s, b = q & 1 ? s : c;
+  sn = q & 2 ? -a : a;
+  cn = (q + 1) & 2 ? -b : b;
+}
+
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 16;  // tokens of one workgroup
 
@@ -130,11 +153,11 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
     const int64_t row = a.n_tokens == a.period ? token0 + k : (token0 + k) % a.period;
     const int64_t p = a.positions ? a.positions[row] : a.first + row;
     const double f = a.table.turns[j], pd = (double)p;
-    const float r = (float)fma(pd, f, -rint(pd * f));  // what whole turns leave
-    float sn, cn;
-    sincospif(2.f * r, &sn, &cn);
-    cs[k * 2 * pairs + j] = cn * a.table.amplitude;
-    cs[k * 2 * pairs + pairs + j] = sn * a.table.amplitude * a.sign;
+    const double r = fma(pd, f, -rint(pd * f));  // what whole turns leave
+    double sn, cn;
+    sine_cosine(r, sn, cn);
+    cs[k * 2 * pairs + j] = (float)(cn * a.table.amplitude);
+    cs[k * 2 * pairs + pairs + j] = (float)(sn * a.table.amplitude) * a.sign;
     if (j == 0) skip[k] = p < 0;
   }
   __syncthreads();
@@ -293,7 +316,7 @@ int form_table(const sn_rotary* p, RotaryTable& t) {
   t.pairs = p->rot_dim / 2;
   t.head_dim = p->head_dim;
   t.interleaved = p->layout == SN_ROTARY_INTERLEAVED;
-  t.amplitude = p->scaling == SN_ROTARY_INDEX ? (float)(1.0 + 0.1 * std::log(p->factor)) : 1.f;
+  t.amplitude = p->scaling == SN_ROTARY_INDEX ? 1.0 + 0.1 * std::log(p->factor) : 1.0;
   for (int i = 0; i < kMaxPairs; ++i) {
     double f = i < t.pairs ? std::pow(base, -2.0 * i / rot) : 0.0;
     double mix = 0.0;  // share of the divided frequency
@@ -339,7 +362,7 @@ extern "C" SN_API int spectral_rotary_frequencies(const sn_rotary* p, double* fr
   RotaryTable t{};
   if (int rc = rotary_table(p, t)) return rc;
   for (int i = 0; i < t.pairs; ++i) freq[i] = t.turns[i] * 6.283185307179586476925;
-  *amplitude = t.amplitude;
+  *amplitude = (float)t.amplitude;
   return SN_OK;
 }
 

@@ -77,6 +77,24 @@ def test_scaled_frequencies_and_far_positions(scaling, layout):
     check(plan.apply(x, positions=torch.from_numpy(p).cuda()), x, p, 64, layout, freq, amp)
 
 
+@pytest.mark.parametrize("scaling", list(SCALINGS))
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_cosines_and_sines_are_rounded_once(scaling, layout, inverse):
+    """The pair (1, 0) turns into its cosine and sine times the amplitude, with nothing else rounded: half a unit of float32
+    (2^-24 of the value) and what the double operations before it leave: the angle's p 2^-48, and 2^-34 of the value, the first
+    term left out of the sine's series at an eighth of a turn, (pi / 4)^13 / 13! beside 0.7."""
+    plan = Rotary(64, layout=layout, base=500000.0, scaling=scaling, **SCALINGS[scaling])
+    freq, amp = rotary_oracle.frequencies(64, base=500000.0, scaling=scaling, **SCALINGS[scaling])
+    p = np.concatenate([np.arange(3000), np.random.default_rng(5).integers(3000, 1 << 20, 1000)])
+    x = torch.zeros(len(p), 1, 64, device="cuda")
+    x[..., slice(0, 32) if layout == "half" else slice(0, 64, 2)] = 1.0
+    got = plan.apply(x, positions=torch.from_numpy(p).cuda(), inverse=inverse)
+    ref = rotary_oracle.rotate(host(x), p, 64, layout, freq, amp, inverse)
+    tol = np.abs(ref) * (2.0 ** -24 + 2.0 ** -34) + amp * p[:, None, None] * 2.0 ** -48
+    assert (np.abs(host(got) - ref) <= tol).all()
+
+
 def test_turning_back_is_the_gradient():
     """<R x, g> = <x, R^T g> by differences: the map is linear, so a central difference is exact but for float32."""
     plan = Rotary(32, rot_dim=24, layout="interleaved", scaling="index", **SCALINGS["index"])
