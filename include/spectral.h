@@ -438,9 +438,11 @@ SN_API int spectral_rotary(const sn_rotary* p, int32_t dtype, int64_t n_tokens, 
 
 /* spectral_logits_fp8 with queries and keys turned by their positions before
  * the logits: S_h[i][j] = (R_i Q_h[i]) . (R_j K_{g(h)}[j]) / sqrt(d_h), on the
- * float32 projections.  rotary->head_dim is the context's.  positions: device int64
+ * projections as the consumer holds them, float32 sums split into two bf16 halves (2^-17
+ * of the value), and held so again after the turn.  rotary->head_dim is the context's.  positions: device int64
  * [seq_len], the same for every layer, or NULL (row i at position i); a row at a
- * negative position is not turned.  All else as spectral_logits_fp8. */
+ * negative position is not turned, nor, without amplitude, is one at zero.  All else
+ * as spectral_logits_fp8. */
 SN_API int spectral_logits_fp8_rotary(sn_ctx* ctx, const void* const* x_layers, int64_t ld_x, int32_t seq_len,
                                       const void* const* wq_layers, const void* const* wk_layers,
                                       const float* scale, const sn_rotary* rotary, const int64_t* positions,

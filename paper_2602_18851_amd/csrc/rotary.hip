@@ -56,7 +56,7 @@ struct Plain {
   }
 };
 
-// Values as bf16 hi + lo planes (the logit consumer's projections).
+// Values as bf16 hi + lo planes (the logit consumer's projections), 2^-17 of the value each time they are split.
 struct Planes {
   uint16_t* hi;
   uint16_t* lo;
@@ -100,6 +100,7 @@ struct RotaryArgs {
   int64_t period;      // tokens after which positions repeat (the layers of the consumer), or n_tokens
   float sign;          // -1 turns back
   int32_t n_tensors, tokens_per_group, splits;
+  int32_t zero_stays;  // in place without amplitude: rows at position zero are not read and split again
 };
 
 // One pair, the same operations in every variant, so that they give the same bits.
@@ -158,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs<IO> a) {
     sine_cosine(r, sn, cn);
     cs[k * 2 * pairs + j] = (float)(cn * a.table.amplitude);
     cs[k * 2 * pairs + pairs + j] = (float)(sn * a.table.amplitude) * a.sign;
-    if (j == 0) skip[k] = p < 0;
+    if (j == 0) skip[k] = a.zero_stays ? p <= 0 : p < 0;
   }
   __syncthreads();
   const int chunks = pairs / V;
@@ -337,6 +338,7 @@ int launch_rotary_planes(const RotaryTable& t, int64_t layers, int64_t seq, cons
   a.positions = positions;
   a.n_tokens = layers * seq;
   a.period = seq;
+  a.zero_stays = t.amplitude == 1.0;
   a.sign = 1.f;
   a.n_tensors = 2;
   const int64_t heads[2] = {q_heads, k_heads};

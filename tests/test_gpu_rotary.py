@@ -313,6 +313,27 @@ def test_logits_of_turned_queries_and_keys(dh, rot, layout, own_positions):
     assert (still != plain).float().mean() < 2.0 ** -8  # values within 2^-15 of a border between codes 2^-3 apart
 
 
+@pytest.mark.parametrize("dh,rot,layout", [(64, 64, "half"), (16, 12, "interleaved"), (128, 96, "half")])
+def test_rows_that_do_not_turn_keep_their_logits(dh, rot, layout):
+    """Rows at position zero and at negative ones give the codes, maxima and counts of the call without positions; with an
+    amplitude only the negative ones do."""
+    L, seq, d, nq, nkv = 2, 70, 200, 4, 2
+    r = np.random.default_rng([20260306, dh, rot])
+    t = lambda *s: torch.from_numpy(r.standard_normal(s).astype(np.float32)).bfloat16().cuda()  # noqa: E731
+    x, wq, wk = t(L, seq, d), t(L, nq * dh, d) * 0.05, t(L, nkv * dh, d) * 0.05
+    est, scale = Spectral(L, d, nq, nkv, dh, "bf16", 0.1), torch.tensor([0.004, 0.01], device="cuda")
+    plain = est.logits_fp8(x, wq, wk, scale, want_codes=True)
+    p = torch.zeros(seq, dtype=torch.int64, device="cuda")
+    p[::3] = -4
+    got = est.logits_fp8(x, wq, wk, scale, want_codes=True, rotary=Rotary(dh, rot_dim=rot, layout=layout), positions=p)
+    assert all(torch.equal(a, b) for a, b in zip(plain, got))
+    loud = Rotary(dh, rot_dim=rot, layout=layout, scaling="index", **SCALINGS["index"])
+    got = est.logits_fp8(x, wq, wk, scale, want_codes=True, rotary=loud, positions=p)
+    stay = torch.nonzero(p < 0).flatten()
+    assert torch.equal(got[2][:, :, stay][..., stay], plain[2][:, :, stay][..., stay])
+    assert not torch.equal(got[2], plain[2])
+
+
 def test_logits_of_turned_heads_replay_from_a_graph():
     L, seq, d, nq, nkv, dh = 2, 130, 256, 4, 2, 64
     r = np.random.default_rng(20260305)
