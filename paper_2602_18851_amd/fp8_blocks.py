@@ -3,6 +3,8 @@
 ``quantize_fp8``, ``matmul_fp8`` and ``LinearFp8`` check torch tensors and pass
 them to spectral_quantize_fp8 and spectral_matmul_fp8 (include/spectral.h) on
 the current stream of the tensors' device; all arithmetic runs in the HIP kernels.
+Gradients are calls of their own (``LinearFp8.backward``), which autograd does not record: a tensor that
+requires gradients is refused unless these are off (torch.no_grad, or inside an autograd.Function).
 """
 
 from __future__ import annotations
@@ -11,7 +13,7 @@ import functools
 
 import torch
 
-from .launch import on_stream_of
+from .launch import on_stream_of, refuse_autograd
 from .spectral import (SN_BF16, SN_E4M3, SN_E5M2, SN_F32, sn_matmul, spectral_matmul_fp8,
                        spectral_matmul_fp8_workspace_bytes, spectral_quantize_fp8)
 
@@ -82,6 +84,7 @@ def _plain(x: torch.Tensor, name: str) -> int:
     """The row stride of a plain matrix."""
     if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN or x.dim() != 2 or not x.is_cuda:
         raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 CUDA tensor")
+    refuse_autograd(x, name)
     rows, cols = x.shape
     step, one = x.stride()
     if (cols > 1 and one != 1) or (rows > 1 and step < cols):
@@ -190,16 +193,18 @@ class LinearFp8:
     """y = x W^T with both sides in 8 bits, and its gradients.  The weight [N, K] (float32 or bfloat16) is quantised by
     tiles, and so is its transpose for dx; ``set_weight`` does so again after an update, into the same memory, so that a
     graph of the layer's calls goes on with the new weight.  ``backward=False`` (serving) leaves the transpose out.  Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the
-    format of dy."""
+    format of dy.  The weight may be a parameter: its gradient is what
+    ``backward`` returns."""
 
     def __init__(self, weight: torch.Tensor, grad_fmt: str = "e4m3", backward: bool = True):
         if grad_fmt not in _FORMATS:
             raise ValueError("grad_fmt must be 'e4m3' or 'e5m2'")
         self.grad_fmt, self._back = grad_fmt, bool(backward)
-        self.weight, self.weight_t = quantize_fp8(weight, tile=True, cols=self._back)
+        self.weight, self.weight_t = quantize_fp8(weight.detach(), tile=True, cols=self._back)
 
     def set_weight(self, weight: torch.Tensor) -> None:
         """A new weight of the same shape, on the same device."""
+        weight = weight.detach()
         ld, w = _plain(weight, "weight"), self.weight
         if tuple(weight.shape) != (w.rows, w.cols) or weight.device != w.codes.device:
             raise ValueError(f"weight must be [{w.rows}, {w.cols}] on {w.codes.device}")

@@ -1,4 +1,4 @@
-"""Calls on the current torch stream of a tensor's device."""
+"""Calls on the current torch stream of a tensor's device, and what they refuse."""
 
 from __future__ import annotations
 
@@ -14,3 +14,10 @@ def on_stream_of(device: torch.device, call, *args) -> None:
     else:
         with torch.cuda.device(index):
             call(*args, _raw_stream(index))
+
+
+def refuse_autograd(x: torch.Tensor, name: str) -> None:
+    """Raises where autograd would expect x's gradient of a call that it does not see."""
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires gradients, which this call does not record: pass {name}.detach() or call it "
+                         "under torch.no_grad(), and call the gradient yourself")

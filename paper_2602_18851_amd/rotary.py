@@ -6,7 +6,7 @@ import ctypes
 
 import torch
 
-from .launch import on_stream_of
+from .launch import on_stream_of, refuse_autograd
 from .spectral import SN_BF16, SN_F32, SN_ROTARY_COPY_PADDING, sn_rotary, spectral_rotary, spectral_rotary_frequencies
 
 _LAYOUTS = {"half": 0, "interleaved": 1}
@@ -37,8 +37,9 @@ class Rotary:
               start: int = 0, inverse: bool = False, out=None):
         """q, k: float32 or bfloat16 [tokens, heads, head_dim], any token and head strides.  positions: int64 [tokens],
         or None: token t is at start + t; rows of tokens at negative positions (padding) are left as out holds them, and
-        are the input's own, not turned, in new tensors.  inverse turns back: the gradient.  out: a tensor (with k: a
-        pair) like q (and k), which may be the inputs themselves; new tensors if None.  Returns the turned q, or (q, k)."""
+        are the input's own, not turned, in new tensors.  inverse turns back: the gradient.  Autograd does not record the
+        call: q and k that require gradients are refused unless these are off.  out: a tensor (with k: a pair) like q (and
+        k), which may be the inputs themselves; new tensors if None.  Returns the turned q, or (q, k)."""
         xs = (q,) if k is None else (q, k)
         if out is None:
             outs = None
@@ -54,6 +55,7 @@ class Rotary:
             if len(shape) != 3 or shape[0] != n or shape[2] != d or x.dtype != dtype or dtype not in _DTYPES \
                     or not x.is_cuda or x.device != dev:
                 raise ValueError(f"q and k must be [tokens, heads, {d}] float32 or bfloat16 CUDA tensors of one type")
+            refuse_autograd(x, "qk"[i])
             xt, xh, xe = x.stride()
             if outs is None:
                 o = torch.empty(shape, dtype=dtype, device=dev)

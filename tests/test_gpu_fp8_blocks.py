@@ -571,6 +571,39 @@ def test_gradients_against_differences():
         assert (loss(x, up) - loss(x, down)) / 4 == float(dw[i, j])
 
 
+def test_tensors_that_require_gradients():
+    """Refused where autograd would wait for a gradient that it never gets; taken with gradients off, as weights, and inside
+    a function that calls the gradients itself."""
+    r = rng(29)
+    m, n, k = 40, 70, 200
+    x = on_gpu(wide(r, m, k), "bf16").requires_grad_()
+    w = torch.nn.Parameter(on_gpu(0.02 * r.standard_normal((n, k)), "f32"))
+    dy = on_gpu(wide(r, m, n), "bf16")
+    layer = LinearFp8(w)
+    layer.set_weight(w)
+    for bad in (lambda: layer.forward(x), lambda: layer.forward(x, keep=True), lambda: quantize_fp8(x), lambda: quantize_fp8(w),
+                lambda: matmul_fp8(x, layer.weight),
+                lambda: layer.backward(dy.clone().requires_grad_(), layer.forward(x.detach(), keep=True)[1])):
+        with pytest.raises(ValueError, match="requires gradients"):
+            bad()
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            y, ctx.kept = layer.forward(x, keep=True)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            return layer.backward(dy, ctx.kept)
+
+    Linear.apply(x, w).backward(dy)
+    with torch.no_grad():
+        y, kept = layer.forward(x, keep=True)
+    dx, dw = layer.backward(dy, kept)
+    assert torch.equal(x.grad, dx) and torch.equal(w.grad, dw) and torch.equal(y, layer.forward(x.detach()))
+
+
 # ------------------------------------------------------- streams and graphs
 
 

@@ -237,6 +237,16 @@ def test_empty_and_refused_calls():
         Rotary(64, rot_dim=65)
 
 
+def test_heads_that_require_gradients_are_refused():
+    plan = Rotary(64)
+    q, k = heads((10, 1), 4, 2, 64, "f32"), heads((10, 2), 4, 2, 64, "f32").requires_grad_()
+    for bad in (lambda: plan.apply(k), lambda: plan.apply(q, k), lambda: plan.apply(q, k, out=(q, k.detach().clone()))):
+        with pytest.raises(ValueError, match="requires gradients"):
+            bad()
+    with torch.no_grad():
+        assert torch.equal(plan.apply(q, k)[1], plan.apply(k.detach()))
+
+
 def test_rotary_replays_from_a_graph_and_on_another_stream():
     plan = Rotary(128, scaling="turns", **SCALINGS["turns"])
     q, k = heads((6, 1), 70, 8, 128, "bf16"), heads((6, 2), 70, 2, 128, "bf16")
@@ -316,12 +326,13 @@ def test_logits_of_turned_queries_and_keys(dh, rot, layout, own_positions):
 @pytest.mark.parametrize("dh,rot,layout", [(64, 64, "half"), (16, 12, "interleaved"), (128, 96, "half")])
 def test_rows_that_do_not_turn_keep_their_logits(dh, rot, layout):
     """Rows at position zero and at negative ones give the codes, maxima and counts of the call without positions; with an
-    amplitude only the negative ones do."""
-    L, seq, d, nq, nkv = 2, 70, 200, 4, 2
+    amplitude only the negative ones do.  (One value in 2^10 splits into other halves the second time, so that of 128 maxima
+    over sums of d_h products some would move.)"""
+    L, seq, d, nq, nkv = 4, 130, 200, 32, 8
     r = np.random.default_rng([20260306, dh, rot])
     t = lambda *s: torch.from_numpy(r.standard_normal(s).astype(np.float32)).bfloat16().cuda()  # noqa: E731
     x, wq, wk = t(L, seq, d), t(L, nq * dh, d) * 0.05, t(L, nkv * dh, d) * 0.05
-    est, scale = Spectral(L, d, nq, nkv, dh, "bf16", 0.1), torch.tensor([0.004, 0.01], device="cuda")
+    est, scale = Spectral(L, d, nq, nkv, dh, "bf16", 0.1), torch.tensor([0.004, 0.01] * 2, device="cuda")
     plain = est.logits_fp8(x, wq, wk, scale, want_codes=True)
     p = torch.zeros(seq, dtype=torch.int64, device="cuda")
     p[::3] = -4
