@@ -84,7 +84,8 @@ def _plain(x: torch.Tensor, name: str) -> int:
     """The row stride of a plain matrix."""
     if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN or x.dim() != 2 or not x.is_cuda:
         raise ValueError(f"{name} must be a two-dimensional float32 or bfloat16 CUDA tensor")
-    refuse_autograd(x, name)
+    if x.requires_grad:
+        refuse_autograd(name)
     rows, cols = x.shape
     step, one = x.stride()
     if (cols > 1 and one != 1) or (rows > 1 and step < cols):
@@ -92,11 +93,15 @@ def _plain(x: torch.Tensor, name: str) -> int:
     return step if rows > 1 else cols
 
 
-def _scale_of(m: Fp8Matrix) -> torch.Tensor:
-    """The scales as a call reads them: one value for all is written out first, since strides of two zeros say "dense" to
-    the library."""
+def _scale_of(m: Fp8Matrix):
+    """The scales as a call reads them, and their strides: one value for all is written out first, since strides of two
+    zeros say "dense" to the library."""
     s = m.scale
-    return s if any(s.stride()) else s.contiguous()
+    strides = s.stride()
+    if strides == (0, 0):
+        s = s.contiguous()
+        strides = s.stride()
+    return s, strides
 
 
 def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: bool = False,
@@ -150,9 +155,8 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         codes, sa, sa_block, sa_row, a_rows = a, 0, 0, 0, 1
         m, k = a.shape
     else:
-        a_scale = _scale_of(a)
+        a_scale, (sa_block, sa_row) = _scale_of(a)
         ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a_scale.data_ptr(), a.block_rows, a.rows, a.cols
-        sa_block, sa_row = a_scale.stride()
     n, dev = b.rows, codes.device
     if b.cols != k:
         raise ValueError(f"a has {k} columns and b {b.cols}")
@@ -182,8 +186,8 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
         ws = workspace.data_ptr()
-    b_scale = _scale_of(b)
-    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *b_scale.stride())
+    b_scale, sb = _scale_of(b)
+    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *sb)
     on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b_scale.data_ptr(),
                  out.data_ptr(), ws, need)
     return out

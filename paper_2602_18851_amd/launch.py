@@ -16,8 +16,8 @@ def on_stream_of(device: torch.device, call, *args) -> None:
             call(*args, _raw_stream(index))
 
 
-def refuse_autograd(x: torch.Tensor, name: str) -> None:
-    """Raises where autograd would expect x's gradient of a call that it does not see."""
-    if x.requires_grad and torch.is_grad_enabled():
+def refuse_autograd(name: str) -> None:
+    """Raises where autograd would expect the gradient, of a call that it does not see, of a tensor that requires it."""
+    if torch.is_grad_enabled():
         raise ValueError(f"{name} requires gradients, which this call does not record: pass {name}.detach() or call it "
                          "under torch.no_grad(), and call the gradient yourself")

@@ -55,7 +55,8 @@ class Rotary:
             if len(shape) != 3 or shape[0] != n or shape[2] != d or x.dtype != dtype or dtype not in _DTYPES \
                     or not x.is_cuda or x.device != dev:
                 raise ValueError(f"q and k must be [tokens, heads, {d}] float32 or bfloat16 CUDA tensors of one type")
-            refuse_autograd(x, "qk"[i])
+            if x.requires_grad:
+                refuse_autograd("qk"[i])
             xt, xh, xe = x.stride()
             if outs is None:
                 o = torch.empty(shape, dtype=dtype, device=dev)
