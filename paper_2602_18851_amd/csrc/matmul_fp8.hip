@@ -133,9 +133,10 @@ __device__ __forceinline__ void wait_loads() {
 
 // Tiles of 128 x 128 by 4 waves of 64 x 64, two workgroups to a compute unit, or by 8 waves of 64 x 32.  Blocks of
 // 128 columns and the scales of their rows come through two stages in LDS, the next requested before the current one is
-// multiplied (three or four stages gain nothing: 512 x 8192 x 8192 46.6 and 46.4 us, two 45.7).  The products are formed transposed (rows from B): a lane holds four neighbouring columns of one row
-// of C, with one scale of A.  Scales through LDS, a block ahead, and not read as they are needed: 4096^3 to
-// float32 139 instead of 230 us, 256 x 8192 x 8192 to bf16 46 instead of 66.
+// multiplied (three or four stages gain nothing: by 4 waves, 512 x 8192 x 8192 46.6 and 46.4 us, two 45.7).  The products are
+// formed transposed (rows from B): a lane holds four neighbouring columns of one row of C, with one scale of A.  Scales
+// through LDS, a block ahead, and not read as they are needed: by 4 waves, 4096^3 to float32 139 instead of 230 us, 256 x
+// 8192 x 8192 to bf16 46 instead of 66 (by 8 waves 31.6).
 constexpr int kT = 128;
 constexpr int kTStage = 2 * kT * 128 + 2 * kT * 4;  // rows of A, of B, then their scales
 
