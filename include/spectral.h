@@ -343,17 +343,21 @@ typedef struct {
                                rounded up to 16 (codes), n (C).  Code rows are
                                multiples of 16 bytes and below 2^22.                  */
   int64_t sa_block, sa_row; /* strides of sA in elements, from a column block to the
-                               next and from a row (tile) to the next; both 0: dense  */
+                               next and from a row (tile) to the next; both 0: dense;
+                               one scale for all of A: both SN_STRIDE_ZERO            */
   int64_t sb_block, sb_row;
 } sn_matmul;
+
+#define SN_STRIDE_ZERO (-((int64_t)1 << 62))
 
 /* Device scratch (256-byte aligned) that the call needs, possibly 0: the codes
  * and scales of a plain A, and float32 parts of C where the sum over k is
  * split over workgroups.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
 SN_API int spectral_matmul_fp8_workspace_bytes(const sn_matmul* p, int64_t* bytes);
 
-/* Which kernel the call runs (beside launches that quantise a plain A first or join parts), for labelling
- * profiles and for tests: its kind, into how many parts the sum over k is split, and its launch; zeros where m or n is 0.
+/* Which kernel the call runs (beside launches that quantise a plain A
+ * first or join parts), for labelling profiles and for tests: its kind, into how
+ * many parts the sum over k is split, and its launch; zeros where m or n is 0.
  * Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
 typedef enum {
   SN_MATMUL_FEW_ROWS = 1, /* B once, from memory to registers             */

@@ -1023,6 +1023,8 @@ int resolve(sn_matmul& p, MatPlan& pl) {
     p.sb_row = 1;
     p.sb_block = (p.n + p.b_block_rows - 1) / p.b_block_rows;
   }
+  for (int64_t* s : {&p.sa_block, &p.sa_row, &p.sb_block, &p.sb_row})
+    if (*s == SN_STRIDE_ZERO) *s = 0;
   if (p.sa_block < 0 || p.sa_row < 0 || p.sb_block < 0 || p.sb_row < 0 || p.sa_block > kMost || p.sa_row > kMost ||
       p.sb_block > kMost || p.sb_row > kMost)
     return refuse(SN_EINVAL, "scale strides must be >= 0 and below 2^40");

@@ -14,7 +14,7 @@ import functools
 import torch
 
 from .launch import on_stream_of, refuse_autograd
-from .spectral import (SN_BF16, SN_E4M3, SN_E5M2, SN_F32, sn_matmul, spectral_matmul_fp8,
+from .spectral import (SN_BF16, SN_E4M3, SN_E5M2, SN_F32, SN_STRIDE_ZERO, sn_matmul, spectral_matmul_fp8,
                        spectral_matmul_fp8_workspace_bytes, spectral_quantize_fp8)
 
 BLOCK = 128
@@ -93,15 +93,10 @@ def _plain(x: torch.Tensor, name: str) -> int:
     return step if rows > 1 else cols
 
 
-def _scale_of(m: Fp8Matrix):
-    """The scales as a call reads them, and their strides: one value for all is written out first, since strides of two
-    zeros say "dense" to the library."""
-    s = m.scale
-    strides = s.stride()
-    if strides == (0, 0):
-        s = s.contiguous()
-        strides = s.stride()
-    return s, strides
+def _scale_strides(m: Fp8Matrix) -> tuple[int, int]:
+    """Two zeros, one value expanded over all blocks, would say "dense" to the library."""
+    strides = m.scale.stride()
+    return strides if strides != (0, 0) else (SN_STRIDE_ZERO, SN_STRIDE_ZERO)
 
 
 def quantize_fp8(x: torch.Tensor, tile: bool = False, rows: bool = True, cols: bool = False,
@@ -145,8 +140,9 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
     """a b^T: a [M, K] an Fp8Matrix, or a float32 or bfloat16 tensor that is quantised by rows to E4M3 on the way; b
     [N, K] an Fp8Matrix.  A float32 result sums exact products in float32; for a bfloat16 one the matrix cores may add them in
     eights, each kept to 2^-13 of its eight's largest (include/spectral.h).  Scales: any whose products of one of a and one
-    of b lie between 2^-126 and the largest float32.  ``out``: [M, N] float32 or bfloat16, rows contiguous.  ``workspace``: uint8 scratch for callers
-    that keep it (a new tensor where it is too small); calls that can run at the same time need their own."""
+    of b lie between 2^-126 and the largest float32.  ``out``: [M, N] float32 or bfloat16, rows contiguous, apart from a
+    and b.  ``workspace``: uint8 scratch for callers that keep it (a new tensor where it is too small); calls that can run at
+    the same time need their own."""
     if not isinstance(b, Fp8Matrix):
         raise ValueError("b must be an Fp8Matrix")
     plain = not isinstance(a, Fp8Matrix)
@@ -155,8 +151,8 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         codes, sa, sa_block, sa_row, a_rows = a, 0, 0, 0, 1
         m, k = a.shape
     else:
-        a_scale, (sa_block, sa_row) = _scale_of(a)
-        ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a_scale.data_ptr(), a.block_rows, a.rows, a.cols
+        ld_a, codes, sa, a_rows, m, k = a.ld, a.codes, a.scale.data_ptr(), a.block_rows, a.rows, a.cols
+        sa_block, sa_row = _scale_strides(a)
     n, dev = b.rows, codes.device
     if b.cols != k:
         raise ValueError(f"a has {k} columns and b {b.cols}")
@@ -186,9 +182,8 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
         elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
         ws = workspace.data_ptr()
-    b_scale, sb = _scale_of(b)
-    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *sb)
-    on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b_scale.data_ptr(),
+    p = sn_matmul(*kinds, ld_a, b.ld, ld_c, sa_block, sa_row, *_scale_strides(b))
+    on_stream_of(dev, spectral_matmul_fp8, p, codes.data_ptr(), sa, b.codes.data_ptr(), b.scale.data_ptr(),
                  out.data_ptr(), ws, need)
     return out
 
@@ -196,9 +191,9 @@ def matmul_fp8(a, b: Fp8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: to
 class LinearFp8:
     """y = x W^T with both sides in 8 bits, and its gradients.  The weight [N, K] (float32 or bfloat16) is quantised by
     tiles, and so is its transpose for dx; ``set_weight`` does so again after an update, into the same memory, so that a
-    graph of the layer's calls goes on with the new weight.  ``backward=False`` (serving) leaves the transpose out.  Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the
-    format of dy.  The weight may be a parameter: its gradient is what
-    ``backward`` returns."""
+    graph of the layer's calls goes on with the new weight.  ``backward=False`` (serving) leaves the transpose out.
+    Activations are quantised by rows of the matrix that sums over them; ``grad_fmt`` is the format of dy.  The weight may
+    be a parameter: its gradient is what ``backward`` returns."""
 
     def __init__(self, weight: torch.Tensor, grad_fmt: str = "e4m3", backward: bool = True):
         if grad_fmt not in _FORMATS:

@@ -21,6 +21,7 @@ SN_FLAG_VALU_K_SWEEP = 1
 SN_FLAG_GRAM = 2
 SN_FLAG_LAYER = 4
 SN_ROTARY_COPY_PADDING = 1 << 30
+SN_STRIDE_ZERO = -(1 << 62)
 KIND_NAMES = ("k_sweep_first", "q_sweep", "k_sweep", "finalize", "gram_sweep", "gram_iterate", "gram_final_sweeps",
               "layer_row_sweeps", "layer_col_sweeps", "layer_reduce", "logits_projection", "logits_fp8",
               "tail_lists")

@@ -260,6 +260,16 @@ def test_launches_stay_below_32_bits_of_lanes(lib, m, k, c):  # noqa: F811
     assert run
 
 
+def test_strides_of_one_scale(lib):  # noqa: F811
+    """SN_STRIDE_ZERO stands for a stride of zero; no other negative one is taken."""
+    zero = dict(sa_block=sp.SN_STRIDE_ZERO, sa_row=sp.SN_STRIDE_ZERO, sb_block=sp.SN_STRIDE_ZERO, sb_row=sp.SN_STRIDE_ZERO)
+    assert sp.spectral_matmul_fp8_kernel(matmul(m=8192, n=8192, k=8192, **zero))[0] == "big"
+    for name in zero:
+        sp.spectral_matmul_fp8_workspace_bytes(matmul(**{name: sp.SN_STRIDE_ZERO}))
+        for bad in (-1, sp.SN_STRIDE_ZERO + 1, sp.SN_STRIDE_ZERO - 1):
+            refused(sp.SN_EINVAL, sp.spectral_matmul_fp8_workspace_bytes, matmul(**{name: bad}))
+
+
 def test_kernel_query_refuses(lib):  # noqa: F811
     refused(sp.SN_EINVAL, sp.spectral_matmul_fp8_kernel, matmul(m=-1))
     assert lib.spectral_matmul_fp8_kernel(None, None, None, None, None) == sp.SN_ENULL

@@ -251,7 +251,8 @@ def test_scales_of_any_strides(layout, m, n, k):
         check_product(matmul_fp8(a, b, out_dtype=torch.float32), av, bv, "f32")
 
 
-@pytest.mark.parametrize("m,n,k", [(5, 40, 100), (300, 260, 700)])
+@pytest.mark.parametrize("m,n,k", [(5, 40, 100), (5, 400, 1500), (300, 260, 700), (2100, 2200, 300), (300, 21700, 300),
+                                   (3100, 3300, 300)])
 def test_a_scale_of_the_whole_matrix_can_change(m, n, k):
     """One value expanded over all blocks is read at each call, not when the matrix is made."""
     a, _ = matrix((17, m, k), m, k, "e4m3", 1)
@@ -259,11 +260,13 @@ def test_a_scale_of_the_whole_matrix_can_change(m, n, k):
     sa, sb = torch.ones(1, 1, device="cuda"), torch.ones(1, 1, device="cuda")
     a = Fp8Matrix(a.codes, sa.expand(a.scale.shape), cols=k)
     b = Fp8Matrix(b.codes, sb.expand(b.scale.shape), cols=k)
-    ref = matmul_fp8(a, b, out_dtype=torch.float32)
-    for factor in (2.0, 0.25):
-        sa.fill_(factor)
-        sb.fill_(8.0)
-        assert torch.equal(matmul_fp8(a, b, out_dtype=torch.float32), 8 * factor * ref)
+    ones = [Fp8Matrix(t.codes, torch.ones_like(t.scale).contiguous(), cols=k) for t in (a, b)]
+    for out in (torch.float32, torch.bfloat16):
+        ref = matmul_fp8(*ones, out_dtype=out)
+        for factor in (1.0, 2.0, 0.25):
+            sa.fill_(factor)
+            sb.fill_(8.0)
+            assert torch.equal(matmul_fp8(a, b, out_dtype=out), 8 * factor * ref)
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
