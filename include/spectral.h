@@ -58,7 +58,7 @@ extern "C" {
 
 /* Weights, tokens and heads are SN_F32 or SN_BF16; 8-bit matrices (see
  * spectral_quantize_fp8) OCP E4M3FN or E5M2 codes. */
-typedef enum { SN_F32 = 0, SN_BF16 = 1, SN_E4M3 = 2, SN_E5M2 = 3 } sn_dtype;
+typedef enum { SN_F32 = 0, SN_BF16 = 1, SN_E4M3 = 2, SN_E5M2 = 3, SN_I8 = 4 } sn_dtype;
 
 typedef struct {
   int32_t n_layers;    /* L >= 1                                                  */
@@ -375,6 +375,148 @@ SN_API int spectral_matmul_fp8_kernel(const sn_matmul* p, int32_t* kernel, int32
  * Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP. */
 SN_API int spectral_matmul_fp8(const sn_matmul* p, const void* a, const float* sa, const void* b, const float* sb,
                                void* c, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ---- 8-bit integers with a scale for each row -------------------------
+ *
+ * A matrix X [rows][cols] in 8-bit integers is codes [rows][ld] (ld a multiple of
+ * 16, at least cols) and a float32 scale for each row (a token of activations, an
+ * output channel of a weight):  X[r][c] = code[r][c] * scale[r].
+ *
+ * spectral_quantize_int8 forms them from x: a row's scale is max |x| / 127,
+ * rounded to float32, 2^-126 at least; a code is x / scale rounded to the nearest
+ * whole number, ties to even, from -127 to 127.  A row that holds an
+ * infinity or a NaN gets scale NaN and codes zero.
+ *   x      device [rows][ld_x] (ld_x = 0: cols) of dtype SN_F32 or SN_BF16, any
+ *          alignment of the type.
+ *   codes  device [rows][ld], rows 16-byte aligned; written up to the next
+ *          multiple of 16 columns, zeros past the last.
+ *   scale  device [rows].
+ * Outputs must not overlap x or each other.  rows = 0 does nothing.  Errors:
+ * SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP.  These calls and those of
+ * the cache below need no context either: see spectral_quantize_fp8. */
+SN_API int spectral_quantize_int8(const void* x, int64_t rows, int64_t cols, int64_t ld_x, int32_t dtype,
+                                  int8_t* codes, int64_t ld, float* scale, void* hip_stream);
+
+/* C = A B^T of two such matrices, A [m][k] and B [n][k]:
+ *     C[i][j] = sA[i] sB[j] sum_c A[i][c] B[j][c],
+ * the sum exact in 32 bits, rounded to float32 and multiplied by the product of the scales (rounded
+ * too); then rounded to C's type.  Every kernel gives the same bits.  Scales are any float32;
+ * their product may leave float32's range where C does not.  Codes may be
+ * -128.  Every row of codes, the last one too, holds k rounded up to 16 bytes;
+ * those past column k are not used. */
+typedef struct {
+  int64_t m, n, k;          /* >= 0 (k = 0: the sums are zero); m x n below 2^22 tiles of
+                               128 x 128, k below 2^17                              */
+  int32_t a_type;           /* SN_I8; or SN_F32, SN_BF16: A is a plain matrix [m][ld_a]
+                               that the call quantises on its way, bit for bit as
+                               spectral_quantize_int8 does                          */
+  int32_t c_type;           /* SN_F32 or SN_BF16                                    */
+  int64_t ld_a, ld_b, ld_c; /* row strides in elements; 0 means k (plain A), k
+                               rounded up to 16 (codes), n (C).  Code rows are
+                               multiples of 16 bytes and below 2^22.                */
+  int64_t sa_row, sb_row;   /* strides of the scales in elements; 0: one after the
+                               other; one scale for all rows: SN_STRIDE_ZERO        */
+} sn_matmul_int8;
+
+/* Device scratch (256-byte aligned) that the call needs, possibly 0: the codes
+ * and scales of a plain A, and parts of the sums where they are split over
+ * workgroups.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
+SN_API int spectral_matmul_int8_workspace_bytes(const sn_matmul_int8* p, int64_t* bytes);
+
+/* Which kernel the call runs, as spectral_matmul_fp8_kernel. */
+SN_API int spectral_matmul_int8_kernel(const sn_matmul_int8* p, int32_t* kernel, int32_t* parts, int64_t* workgroups,
+                                       int32_t* threads);
+
+/* Codes are 16-byte aligned, scales and C aligned to their type; sa is NULL
+ * for a plain A.  C must not overlap the inputs.  Calls that can run at the
+ * same time need workspaces of their own, graphs captured from them too.
+ * Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP. */
+SN_API int spectral_matmul_int8(const sn_matmul_int8* p, const void* a, const float* sa, const int8_t* b,
+                                const float* sb, void* c, void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* ---- a cache of keys and values in 8 bits -------------------------------
+ *
+ * Places of tokens, in pages: codes [pages][heads][page][head_dim] and float32
+ * scales [pages][heads][page], of keys and of values.  A row, the head_dim elements
+ * of one place and head, has one scale, a power of two from 2^-126 on (or NaN):
+ * element e is code[e] * scale.  Slot n is place n % page of page n / page. */
+typedef struct {
+  void* k;             /* codes of keys, 16-byte aligned                             */
+  float* k_scale;      /* their scales, 16-byte aligned                              */
+  void* v;             /* the same of values                                         */
+  float* v_scale;
+  int64_t pages;       /* >= 0, below 2^31                                           */
+  int32_t heads;       /* 1 .. 65536                                                 */
+  int32_t page;        /* places of a page, a power of two, 16 .. 65536              */
+  int32_t head_dim;    /* a multiple of 16, 16 .. 256                                */
+  int32_t format;      /* SN_E4M3 or SN_E5M2                                         */
+  int64_t code_page;   /* elements from a page's codes to the next one's, and from its
+                          scales; multiples of 16 and 4; 0: dense                    */
+  int64_t scale_page;
+} sn_cache;
+
+/* Writes the keys and values of tokens to their slots: a row's scale is the smallest
+ * power of two, 2^-126 at least, with max |x| / scale <= R (448 or 57344), and a
+ * code x / scale rounded to nearest even; a row that holds an infinity or a
+ * NaN gets scale and codes NaN.
+ *   dtype  SN_F32 or SN_BF16: of k and v, element e of head h of token t at
+ *          t * token + h * head + e (strides in elements, any alignment of the type).
+ *   slots  device int64 [tokens]; a token whose slot is not in [0, pages * page) is
+ *          padding and not written.  The others differ: of tokens with the same slot the
+ *          place holds some mixture.
+ * spectral_cache_read is the way back: code * scale rounded to dtype; zeros for a
+ * slot outside.  Its results' rows must not overlap (else SN_EINVAL).  tokens = 0 does
+ * nothing; tokens * heads stays below 2^31.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE,
+ * SN_ESTATE, SN_EHIP. */
+SN_API int spectral_cache_write(const sn_cache* cache, int32_t dtype, int64_t tokens, const void* k, int64_t k_token,
+                                int64_t k_head, const void* v, int64_t v_token, int64_t v_head, const int64_t* slots,
+                                void* hip_stream);
+SN_API int spectral_cache_read(const sn_cache* cache, int32_t dtype, int64_t tokens, const int64_t* slots, void* k,
+                               int64_t k_token, int64_t k_head, void* v, int64_t v_token, int64_t v_head,
+                               void* hip_stream);
+
+/* Attention of the last `drafts` tokens of each sequence over the cache, theirs
+ * among it:  out = softmax(scale q K^T) V  over the places that a token sees.  A
+ * sequence of n places has them in the pages of its row of the table, in order; the last
+ * `drafts` of them are the drafted tokens' (with fewer places, the first drafted
+ * tokens have none).  Every token sees all places before these, and of these
+ *   masks NULL: those of the drafted tokens up to itself;
+ *   else: drafted token j where bit j of its mask is set (a tree: its ancestors and itself).
+ * A token that sees nothing gets zeros.  A place whose page is not in [0, pages)
+ * is not seen.  Query head h reads head h / (q_heads / heads) of the cache.  What a
+ * place holds that a token does not see, NaN and infinities too, does not
+ * reach its result; a row that is not finite makes NaN of who sees it.
+ *   q        device, element e of head h of drafted token i of sequence b at
+ *            b * q_batch + i * q_draft + h * q_head + e; out the same.
+ *   table    device int32 [batch][table_ld] (0: table_cols), page numbers.
+ *   lengths  device int32 [batch], taken between 0 and table_cols * page.
+ *   masks    device int64 [batch][drafts] (mask_batch elements apart; 0: one
+ *            for all sequences), or NULL.
+ * Queries in SN_F32 are held to 2^-24 and the weights to 2^-24 of a row's
+ * largest; with SN_BF16 the weights to 2^-16.  Sums are float32.  The
+ * same call gives the same bits.  Calls that can run at the same time need
+ * workspaces of their own, graphs captured from them too; the workspace depends on the sizes
+ * here, not on lengths, which a graph may change between replays.  batch = 0 does nothing. */
+typedef struct {
+  int32_t dtype;       /* SN_F32 or SN_BF16, of q and out                            */
+  int32_t batch;       /* 0 .. 2^20                                                  */
+  int32_t drafts;      /* 1 .. 64 tokens of each sequence                            */
+  int32_t q_heads;     /* a multiple of the cache's heads                            */
+  int32_t table_cols;  /* pages of the longest sequence; times page below 2^31 - 32  */
+  float scale;         /* finite, positive                                           */
+  int64_t q_batch, q_draft, q_head;
+  int64_t out_batch, out_draft, out_head;
+  int64_t table_ld, mask_batch;
+} sn_attend;
+
+/* Device scratch (256-byte aligned) that the call needs, possibly 0.  Errors: SN_ENULL,
+ * SN_EINVAL, SN_EDTYPE. */
+SN_API int spectral_cache_attend_workspace_bytes(const sn_cache* cache, const sn_attend* p, int64_t* bytes);
+
+/* Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP. */
+SN_API int spectral_cache_attend(const sn_cache* cache, const sn_attend* p, const void* q, const int32_t* table,
+                                 const int32_t* lengths, const int64_t* masks, void* out, void* workspace,
+                                 int64_t workspace_bytes, void* hip_stream);
 
 /* ---- rotary positions -------------------------------------------------
  *

@@ -22,6 +22,8 @@ fp8_consumer     Stage 3 of the geometry-aware forward pass up to the E4M3
                  the overflow count per head.
 fp8_blocks       8-bit matrices with a scale for each block of 128.
 rotary           Rotary positions as complex rotations.
+int8_rows        8-bit integers with a scale for each row.
+cache            The 8-bit cache of keys and values and attention over it.
 
 Every function here is pinned by the ``-m "not gpu"`` tests against values
 the paper prints, closed forms or textbook routines; none is "parity

@@ -13,16 +13,24 @@ from .spectral import (  # noqa: F401
     SN_FLAG_GRAM,
     SN_FLAG_LAYER,
     SN_FLAG_VALU_K_SWEEP,
+    SN_I8,
     Spectral,
     SpectralError,
     load_library,
+    sn_attend,
+    sn_cache,
     sn_heads,
     sn_matmul,
+    sn_matmul_int8,
     sn_params,
     sn_rotary,
     sn_shape,
     spectral_alpha_select,
     spectral_auto_alpha,
+    spectral_cache_attend,
+    spectral_cache_attend_workspace_bytes,
+    spectral_cache_read,
+    spectral_cache_write,
     spectral_destroy,
     spectral_overflow_terms,
     spectral_slack_ratio,
@@ -34,9 +42,13 @@ from .spectral import (  # noqa: F401
     spectral_matmul_fp8,
     spectral_matmul_fp8_kernel,
     spectral_matmul_fp8_workspace_bytes,
+    spectral_matmul_int8,
+    spectral_matmul_int8_kernel,
+    spectral_matmul_int8_workspace_bytes,
     spectral_profile,
     spectral_profile_read,
     spectral_quantize_fp8,
+    spectral_quantize_int8,
     spectral_rotary,
     spectral_rotary_frequencies,
     spectral_set_stream,
@@ -49,7 +61,8 @@ from .spectral import (  # noqa: F401
 
 # modules that need torch, loaded with the first of their names
 _TORCH = {"Fp8Matrix": "fp8_blocks", "LinearFp8": "fp8_blocks", "matmul_fp8": "fp8_blocks",
-          "quantize_fp8": "fp8_blocks", "Rotary": "rotary"}
+          "quantize_fp8": "fp8_blocks", "Rotary": "rotary", "Int8Matrix": "int8_rows", "matmul_int8": "int8_rows",
+          "quantize_int8": "int8_rows", "Fp8Cache": "fp8_cache"}
 
 
 def __getattr__(name):

@@ -16,7 +16,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", name)
            for name in ("spectral.hip", "sweeps.hip", "gram.hip", "gram_heads.hip", "layer_form.hip", "logits_fp8.hip",
-                       "quantize_fp8.hip", "matmul_fp8.hip", "rotary.hip", "calibration.cpp")]
+                       "quantize_fp8.hip", "matmul_fp8.hip", "rotary.hip", "quantize_int8.hip", "matmul_int8.hip",
+                       "cache_fp8.hip", "attend_fp8.hip", "calibration.cpp")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libspectral.so")
 ARCH = "gfx950"

@@ -1,0 +1,719 @@
+// Attention of single tokens and of trees of drafted tokens over an 8-bit cache (spectral_cache_attend):
+//   S = scale q K^T over the places that a token sees, O = softmax(S) V.
+//
+// The query heads of a key head and the drafted tokens are rows of one product, so the cache is read once for
+// all of them.  Every product is formed transposed: S^T = K Q^T, then O^T = V^T P^T.  The columns, one to each
+// lane % 16, are query rows, and the places of S^T that a lane holds are those of P^T that the second product
+// asks it for, so that P stays in registers.
+//
+// Codes become bf16 with their row's scale, a power of two, on the way: exactly (bf16 has float32's range; parts of
+// values below 2^-126 are lost).  Products of bf16 are exact and summed in float32.  Queries in float32 are three
+// parts of bf16 (2^-24), P, in float32 with its running maximum and sum, two parts (2^-16: nothing beside a bf16
+// result) or three.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "cache_fp8.h"
+#include "device_util.h"
+#include "fp8_device.h"
+
+namespace {
+
+using namespace sn_dev;
+using sn::CacheView;
+
+constexpr int kStep = 32;  // places that a wave takes at a time
+
+struct AttendArgs {
+  CacheView c;
+  const void* q;
+  void* out;
+  int64_t q_batch, q_draft, q_head, out_batch, out_draft, out_head;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* lengths;
+  const int64_t* masks;  // or NULL: a drafted token sees those before it and itself
+  int64_t mask_batch;
+  int32_t batch, drafts, group, rows;  // rows = drafts * group, of a key head
+  int32_t max_places;
+  int32_t row_waves, row_blocks;  // waves of a workgroup with rows of their own, and workgroups that share a key head's rows
+  int32_t target, least;          // workgroups to aim at, and the least steps of one
+  float c_log2;                   // scale * log2(e)
+  float* part_out;                // [unit][rows of a workgroup][head_dim], where a sequence is split
+  float2* part_stat;              // maximum and sum of each row
+};
+
+// ---- how the places are shared out --------------------------------------
+//
+// Lengths are known on the device only, and every workgroup derives the same plan from them: all sequences'
+// steps of kStep places, over `target` workgroups, give the steps of one (`least` at least, which hide its start and end);
+// a sequence is cut into as many equal chunks as that asks for, one at least.  A unit, a chunk
+// of one key head's rows, is one workgroup's.
+struct Split {
+  int64_t per;  // steps that a unit may take
+};
+
+__device__ __forceinline__ int steps_of(const AttendArgs& a, int b) {
+  const int n = min(max(a.lengths[b], 0), a.max_places);
+  return (int)(((int64_t)n + kStep - 1) / kStep);
+}
+
+__device__ __forceinline__ Split plan(const AttendArgs& a, int lane) {
+  int64_t all = 0;
+  for (int b = lane; b < a.batch; b += 64) all += steps_of(a, b);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
+  const int64_t per = (all * a.c.heads * a.row_blocks + a.target - 1) / a.target;
+  return Split{max(per, (int64_t)a.least)};
+}
+
+__device__ __forceinline__ int chunks_of(int steps, const Split& s) {
+  return max(1, (int)((steps + s.per - 1) / s.per));
+}
+
+// ---- arithmetic ------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t bits(__bf16 x) { return __builtin_bit_cast(uint16_t, x); }
+
+// The bf16 parts of eight values, the nearest first.
+template <int PARTS>
+__device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&part)[PARTS]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float rest = x[e];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      part[p][e] = (__bf16)rest;
+      if (p + 1 < PARTS) rest -= (float)part[p][e];
+    }
+  }
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Codes 0, 1 or 2, 3 of a word, times 2^e of the scale, as bf16.
+template <bool E5M2, bool HIGH>
+__device__ __forceinline__ uint32_t widen2(uint32_t w, float scale) {
+  if constexpr (E5M2)
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, scale, HIGH));
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HIGH));
+}
+
+__device__ __forceinline__ f32x4 multiply(const bf16x8& x, const bf16x8& y, const f32x4& sum) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, sum, 0, 0, 0);
+}
+
+// Over the four quarters of a wave, lanes with one lane % 16.
+__device__ __forceinline__ float quarters_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float quarters_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+constexpr float kNone = -__builtin_inff();
+
+// exp2 of the distance to a running maximum; a row that has seen nothing has none.
+__device__ __forceinline__ float weight_of(float m, float to, float c) {
+  return m == kNone ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
+}
+
+// Waves of a workgroup, with NT blocks of 16 rows in a wave.
+constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
+
+// D: head_dim rounded up to 64, 128 or 256.  Lane q * 16 + s of a wave holds
+//   of K: places s of each of two groups of 16, bytes 16 q .. + 15 of every 64;
+//   of V: places 4 q .. 4 q + 3 of each group, D / 16 bytes from D / 16 s on;
+//   of S^T and P^T: those places of V for row s of each block;
+//   of O^T: for row s, D / 4 elements from D / 4 q on.
+template <int D, bool E5M2, bool F32, int NT>
+__global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 256 ? 1 : 2) attend_kernel(AttendArgs a) {
+  constexpr int W = waves_of(NT), KC = D / 64, VB = D / 16, QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
+  constexpr int REGS = NT * (D / 4 + 2);  // of a wave's result: O, maximum, sum
+  __shared__ float merge[W / 2][REGS][64];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int dh = a.c.head_dim, T = a.drafts;
+
+  // which unit this is
+  const Split split = plan(a, lane);
+  const int per_chunk = a.c.heads * a.row_blocks;  // units of a chunk
+  int64_t left = blockIdx.x;                       // units before this one, less those of the sequences before
+  int b = -1;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int64_t mine = 0;
+    if (b0 + lane < a.batch) mine = (int64_t)chunks_of(steps_of(a, b0 + lane), split) * per_chunk;
+    int64_t sum = mine;  // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t o = __shfl_up(sum, d);
+      if (lane >= d) sum += o;
+    }
+    const uint64_t there = __ballot(sum > left);
+    if (there) {
+      const int at = __builtin_ctzll(there);
+      b = b0 + at;
+      left -= __shfl(sum - mine, at);
+      break;
+    }
+    left -= __shfl(sum, 63);
+  }
+  if (b < 0) return;  // whole workgroup: past the last unit
+  b = uni(b);
+  const int in_seq = uni((int)left);
+  const int chunk = in_seq / per_chunk, rest = in_seq % per_chunk;
+  const int h = rest % a.c.heads, rb = rest / a.c.heads;
+  const int len = uni(min(max(a.lengths[b], 0), a.max_places));
+  const int steps = uni(steps_of(a, b)), n_chunks = uni(chunks_of(steps, split));
+  const int per = (steps + n_chunks - 1) / n_chunks;
+  const int step0 = chunk * per, step1 = min(steps, step0 + per);
+
+  const int rw = wv % a.row_waves, part = wv / a.row_waves, parts = W / a.row_waves;
+  const int row0 = (rb * a.row_waves + rw) * 16 * NT;  // this wave's rows
+  const bool rows_there = row0 < a.rows;
+
+  // queries and what each sees of the drafted tokens
+  bf16x8 qf[NT][KC][2][QP];
+  uint64_t sees[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = row0 + 16 * n + s, i = min(r, a.rows - 1) / a.group, g = min(r, a.rows - 1) % a.group;
+    const int64_t at = b * a.q_batch + i * a.q_draft + ((int64_t)h * a.group + g) * a.q_head;
+    sees[n] = a.masks ? (uint64_t)a.masks[b * a.mask_batch + i] : ((uint64_t)2 << i) - 1;
+    sees[n] &= ~(uint64_t)0 >> (64 - T);
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int d = 64 * c + 16 * q + 8 * u;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (d < dh && r < a.rows) {
+          if constexpr (F32) {
+            Eight<float> v;
+            v.load(static_cast<const float*>(a.q) + at + d, 0, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = v.value(e);
+          } else {
+            Eight<__bf16> v;
+            v.load(static_cast<const __bf16*>(a.q) + at + d, 0, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = v.value(e);
+          }
+        }
+        split8<QP>(x, qf[n][c][u]);
+      }
+  }
+
+  // One step's part of the cache in registers.
+  struct Tile {
+    u32x4 k[2][KC];
+    float ks[2];
+    uint32_t v[2][4][VB / 4];
+    f32x4 vs[2];
+    int place;       // its first
+    bool there[2];   // whether the table has a page for each group
+  };
+  int page_a = -1, page_b = -1;  // lane l: pages of this wave's step l of the current 64
+  const int count = rows_there && step1 - step0 > part ? (step1 - step0 - part + parts - 1) / parts : 0;
+  auto load = [&](Tile& t, int i) {  // this wave's step i, in order
+    if ((i & 63) == 0) {
+      auto page_of = [&](int place) {
+        const int id = place >= 0 && place < len ? a.table[b * a.table_ld + (place >> a.c.page_shift)] : -1;
+        return id >= 0 && id < a.c.pages ? id : -1;
+      };
+      const int64_t mine = (int64_t)(step0 + part) + (int64_t)parts * (i + lane);
+      const int place = mine < step1 ? (int)mine * kStep : -1;
+      page_a = page_of(place);
+      page_b = page_of(place < 0 ? -1 : place + 16);
+    }
+    t.place = (step0 + part + parts * i) * kStep;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int id = __builtin_amdgcn_readlane(g ? page_b : page_a, i & 63);
+      t.there[g] = id >= 0;
+      // a group without a page reads page 0, to no use
+      const int in = (h << a.c.page_shift) + (id >= 0 ? (t.place + 16 * g) & (a.c.page - 1) : 0);
+      const int64_t page = id >= 0 ? id : 0;
+      const uint8_t* kp = a.c.k + page * a.c.code_page + (int64_t)in * dh;
+      const uint8_t* vp = a.c.v + page * a.c.code_page + (int64_t)in * dh;
+      const float* ksp = a.c.k_scale + page * a.c.scale_page + in;
+      const float* vsp = a.c.v_scale + page * a.c.scale_page + in;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        t.k[g][c] = u32x4{0, 0, 0, 0};
+        if (64 * c + 16 * q < dh) t.k[g][c] = *reinterpret_cast<const u32x4*>(kp + s * dh + 64 * c + 16 * q);
+      }
+      t.ks[g] = ksp[s];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int w = 0; w < VB / 4; ++w) t.v[g][e][w] = 0;
+        if (VB * s < dh) {
+          typedef uint32_t words __attribute__((ext_vector_type(VB / 4)));
+          if constexpr (VB == 4) {
+            t.v[g][e][0] = *reinterpret_cast<const uint32_t*>(vp + (4 * q + e) * dh + VB * s);
+          } else {
+            const words x = *reinterpret_cast<const words*>(vp + (4 * q + e) * dh + VB * s);
+#pragma unroll
+            for (int w = 0; w < VB / 4; ++w) t.v[g][e][w] = x[w];
+          }
+        }
+      }
+      t.vs[g] = *reinterpret_cast<const f32x4*>(vsp + 4 * q);
+    }
+  };
+
+  f32x4 acc[NT][VB];
+  float top[NT], total[NT];  // total: of the places that this lane holds
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    top[n] = kNone;
+    total[n] = 0.f;
+#pragma unroll
+    for (int j = 0; j < VB; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c_log2 = a.c_log2;
+
+  auto process = [&](Tile& t) {
+    // all places of the step are seen by every row, unless it holds drafted tokens, the end, or lacks a page
+    const bool edge = !t.there[0] || !t.there[1] || t.place + kStep > len - T;
+    f32x4 st[NT][2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) st[n][g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          __builtin_amdgcn_sched_barrier(0);
+          const uint32_t w0 = t.k[g][c][2 * u], w1 = t.k[g][c][2 * u + 1];
+          const u32x4 wide = {widen2<E5M2, false>(w0, t.ks[g]), widen2<E5M2, true>(w0, t.ks[g]),
+                              widen2<E5M2, false>(w1, t.ks[g]), widen2<E5M2, true>(w1, t.ks[g])};
+          const bf16x8 kf = __builtin_bit_cast(bf16x8, wide);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int p = QP - 1; p >= 0; --p) st[n][g] = multiply(kf, qf[n][c][u][p], st[n][g]);
+        }
+    }
+    uint32_t seen[NT];  // bit 4 g + e
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        seen[n] = 0;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          // four places from drafted token j on: ones before the first, zeros past the last
+          const int j = t.place + 16 * g + 4 * q - (len - T);
+          const int before = min(max(-j, 0), 4);
+          const uint32_t of_tree = (uint32_t)(sees[n] >> min(max(j, 0), 63)) << before | ((1u << before) - 1u);
+          const uint32_t four = t.there[g] & (j < 64) ? of_tree & 15u : 0u;
+          seen[n] |= four << (4 * g);
+          f32x4 of_seen;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) of_seen[e] = four >> e & 1u ? st[n][g][e] : kNone;
+          st[n][g] = of_seen;
+        }
+      }
+    }
+    bf16x8 pf[NT][PP];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float m = fmaxf(fmaxf(fmaxf(st[n][0][0], st[n][0][1]), fmaxf(st[n][0][2], st[n][0][3])),
+                      fmaxf(fmaxf(st[n][1][0], st[n][1][1]), fmaxf(st[n][1][2], st[n][1][3])));
+      m = fmaxf(quarters_max(m), top[n]);
+      if (__ballot(m > top[n])) {
+        const float w = weight_of(top[n], m, c_log2);
+        total[n] *= w;
+#pragma unroll
+        for (int j = 0; j < VB; ++j) acc[n][j] *= w;
+        top[n] = m;
+      }
+      const float base = m == kNone ? 0.f : m * c_log2;
+      float p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(fmaf(st[n][e >> 2][e & 3], c_log2, -base));
+        total[n] += p[e];
+      }
+      split8<PP>(p, pf[n]);
+    }
+    // V, place by place, to pairs of places of one element each: place pairs 01 and 23 of both groups
+    auto values = [&](int w, u32x4 (&vt)[4]) {  // elements 4 w .. 4 w + 3
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int h2 = 0; h2 < 2; ++h2) {
+          uint32_t x[2][2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            x[e][0] = widen2<E5M2, false>(t.v[g][2 * h2 + e][w], t.vs[g][2 * h2 + e]);
+            x[e][1] = widen2<E5M2, true>(t.v[g][2 * h2 + e][w], t.vs[g][2 * h2 + e]);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            vt[2 * u][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x05040100u);
+            vt[2 * u + 1][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x07060302u);
+          }
+        }
+    };
+    auto add = [&](int j, const u32x4& vt) {
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, vt);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p) acc[n][j] = multiply(vf, pf[n][p], acc[n][j]);
+    };
+#pragma unroll
+    for (int w = 0; w < VB / 4; ++w) {
+      __builtin_amdgcn_sched_barrier(0);  // a few converted values at a time
+      u32x4 vt[4];
+      values(w, vt);
+      if (edge) {
+        // Values that are not finite reach only the rows that see them: here they count as zeros, and whoever sees one
+        // gets NaN.
+        uint32_t bad[4][4], any = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint32_t v = vt[j][x];
+            const uint32_t lo = (v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
+            const uint32_t hi = (v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+            bad[j][x] = lo | hi;
+            any |= lo | hi;
+          }
+        if (__ballot(any != 0)) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            u32x4 ones;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              vt[j][x] &= ~bad[j][x];
+              ones[x] = bad[j][x] & 0x3f803f80u;  // 1 in bf16
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              u32x4 who;
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                who[x] = (seen[n] >> (2 * x) & 1 ? 0x3f80u : 0u) | (seen[n] >> (2 * x + 1) & 1 ? 0x3f800000u : 0u);
+              const f32x4 n_bad = multiply(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, who),
+                                           f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[n][4 * w + j][e] = n_bad[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[n][4 * w + j][e];
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add(4 * w + j, vt[j]);
+    }
+  };
+
+  if (count > 0) {
+    Tile now, next;
+    load(next, 0);
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {
+      now = next;
+      if (i + 1 < count) load(next, i + 1);  // on its way while this one is processed
+      __builtin_amdgcn_sched_barrier(0);
+      process(now);
+    }
+  }
+
+  // the parts' results meet in LDS, half of them at a time, lane for lane
+#pragma unroll 1
+  for (int half = parts / 2; half >= 1; half /= 2) {
+    float(*at)[64] = merge[(part - (part >= half ? half : 0)) * a.row_waves + rw];
+    if (part >= half && part < 2 * half) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        at[n * (D / 4 + 2)][lane] = top[n];
+        at[n * (D / 4 + 2) + 1][lane] = total[n];
+#pragma unroll
+        for (int j = 0; j < VB; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) at[n * (D / 4 + 2) + 2 + 4 * j + e][lane] = acc[n][j][e];
+      }
+    }
+    __syncthreads();
+    if (part < half) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const float other = at[n * (D / 4 + 2)][lane], m = fmaxf(top[n], other);
+        const float w0 = weight_of(top[n], m, c_log2), w1 = weight_of(other, m, c_log2);
+        top[n] = m;
+        total[n] = total[n] * w0 + at[n * (D / 4 + 2) + 1][lane] * w1;
+#pragma unroll
+        for (int j = 0; j < VB; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[n][j][e] = acc[n][j][e] * w0 + at[n * (D / 4 + 2) + 2 + 4 * j + e][lane] * w1;
+      }
+    }
+    __syncthreads();
+  }
+  if (part != 0 || !rows_there) return;
+
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int r = row0 + 16 * n + s;
+    const float sum = quarters_sum(total[n]);
+    if (r >= a.rows) continue;
+    if (n_chunks > 1) {
+      const int64_t at = (int64_t)blockIdx.x * (16 * NT * a.row_waves) + 16 * NT * rw + 16 * n + s;
+      if (q == 0) a.part_stat[at] = make_float2(top[n], sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (VB * (4 * q + e) < dh)
+#pragma unroll
+          for (int j = 0; j < VB; j += 4)
+            *reinterpret_cast<f32x4*>(a.part_out + at * dh + VB * (4 * q + e) + j) =
+                f32x4{acc[n][j][e], acc[n][j + 1][e], acc[n][j + 2][e], acc[n][j + 3][e]};
+      }
+      continue;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int i = r / a.group, g = r % a.group;
+    const int64_t at = b * a.out_batch + i * a.out_draft + ((int64_t)h * a.group + g) * a.out_head;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (VB * (4 * q + e) < dh)
+#pragma unroll
+        for (int j = 0; j < VB; j += 4) {
+          const f32x4 x = f32x4{acc[n][j][e], acc[n][j + 1][e], acc[n][j + 2][e], acc[n][j + 3][e]} * inv;
+          const int64_t to = at + VB * (4 * q + e) + j;
+          if constexpr (F32) {
+            *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.out) + to) = x;
+          } else {
+            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+            typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+            *reinterpret_cast<bf16x4_any*>(static_cast<__bf16*>(a.out) + to) =
+                bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+          }
+        }
+    }
+  }
+}
+
+// Joins the chunks of a row, in order: a workgroup a row, groups of lanes every so many chunks, 4 elements a lane.
+template <bool F32>
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) {
+  __shared__ f32x4 sums[256];
+  __shared__ float2 stats[16];
+  const int lane = threadIdx.x & 63, t = threadIdx.x;
+  const int heads_q = a.c.heads * a.group;
+  const int row = blockIdx.x % (a.drafts * heads_q), b = blockIdx.x / (a.drafts * heads_q);
+  const Split split = plan(a, lane);
+  const int n_chunks = uni(chunks_of(steps_of(a, b), split));
+  if (n_chunks == 1) return;  // whole workgroup: written already
+  const int per_chunk = a.c.heads * a.row_blocks;
+  int64_t before = 0;  // units of the sequences before
+  for (int x = lane; x < b; x += 64) before += (int64_t)chunks_of(steps_of(a, x), split) * per_chunk;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
+  const int i = row / heads_q, hq = row % heads_q, h = hq / a.group, r = i * a.group + hq % a.group;
+  const int rb = r / unit_rows, in = r % unit_rows, dh = a.c.head_dim;
+  const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, groups = 256 / lanes;
+  const int l = t % lanes, g = t / lanes;
+  float top = kNone, total = 0.f;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int c = g; c < n_chunks; c += groups) {
+    const int64_t at = (before + (int64_t)c * per_chunk + rb * a.c.heads + h) * unit_rows + in;
+    const float2 st = a.part_stat[at];
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (4 * l < dh) x = *reinterpret_cast<const f32x4*>(a.part_out + at * dh + 4 * l);
+    const float m = fmaxf(top, st.x), w0 = weight_of(top, m, a.c_log2), w1 = weight_of(st.x, m, a.c_log2);
+    top = m;
+    total = total * w0 + st.y * w1;
+    sum = sum * w0 + x * w1;
+  }
+  sums[t] = sum;
+  if (l == 0) stats[g] = make_float2(top, total);
+  __syncthreads();
+  if (g != 0 || 4 * l >= dh) return;
+  for (int o = 1; o < groups; ++o) {
+    const float2 st = stats[o];
+    const float m = fmaxf(top, st.x), w0 = weight_of(top, m, a.c_log2), w1 = weight_of(st.x, m, a.c_log2);
+    top = m;
+    total = total * w0 + st.y * w1;
+    sum = sum * w0 + sums[o * lanes + l] * w1;
+  }
+  const f32x4 x = sum * (total == 0.f ? 0.f : 1.f / total);
+  const int64_t to = b * a.out_batch + i * a.out_draft + (int64_t)hq * a.out_head + 4 * l;
+  if constexpr (F32) {
+    *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.out) + to) = x;
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
+    *reinterpret_cast<bf16x4_any*>(static_cast<__bf16*>(a.out) + to) =
+        bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+using namespace sn;
+
+struct Way {
+  int nt;         // blocks of 16 rows in a wave
+  int unit_rows;  // rows of a workgroup
+  int64_t units;  // at most
+  int64_t slots;  // units that may write parts
+  int64_t off_stat, bytes;
+};
+
+template <int D, bool E5M2, bool F32>
+void launch2(const AttendArgs& a, const Way& w, hipStream_t st) {
+  const dim3 g((uint32_t)w.units);
+  if (w.nt == 1) return attend_kernel<D, E5M2, F32, 1><<<g, 64 * waves_of(1), 0, st>>>(a);
+  if constexpr (!(D == 256 && F32)) {
+    if (w.nt == 2) return attend_kernel<D, E5M2, F32, 2><<<g, 64 * waves_of(2), 0, st>>>(a);
+    if constexpr (D != 256 && !F32) attend_kernel<D, E5M2, F32, 4><<<g, 64 * waves_of(4), 0, st>>>(a);
+  }
+}
+
+template <int D>
+void launch1(const AttendArgs& a, const Way& w, bool e5m2, bool f32, hipStream_t st) {
+  if (f32)
+    e5m2 ? launch2<D, true, true>(a, w, st) : launch2<D, false, true>(a, w, st);
+  else
+    e5m2 ? launch2<D, true, false>(a, w, st) : launch2<D, false, false>(a, w, st);
+}
+
+// Checks the description and fills in the kernel's arguments.
+int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bool need_memory) {
+  if (!p) return refuse(SN_ENULL, "p must not be NULL");
+  if (int rc = view_cache(cache, a.c, need_memory)) return rc;
+  if (p->dtype != SN_F32 && p->dtype != SN_BF16) return refuse(SN_EDTYPE, "queries must be SN_F32 or SN_BF16");
+  if (p->batch < 0 || p->batch > (1 << 20)) return refuse(SN_EINVAL, "batch must be in [0, 2^20]");
+  if (p->drafts < 1 || p->drafts > 64) return refuse(SN_EINVAL, "drafts must be in [1, 64]");
+  if (p->q_heads < 1 || p->q_heads > 65536 || p->q_heads % a.c.heads)
+    return refuse(SN_EINVAL, "q_heads must be a multiple of the cache's heads, 65536 at most");
+  if (p->table_cols < 0 || (int64_t)p->table_cols * a.c.page >= (int64_t(1) << 31) - kStep)
+    return refuse(SN_EINVAL, "table_cols must be >= 0, and table_cols * page below 2^31 - 32");
+  if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return refuse(SN_EINVAL, "scale must be finite and positive");
+  constexpr int64_t kMost = int64_t(1) << 40;
+  for (int64_t s : {p->q_batch, p->q_draft, p->q_head, p->out_batch, p->out_draft, p->out_head})
+    if (s < 0 || s > kMost) return refuse(SN_EINVAL, "strides must be >= 0 and below 2^40");
+  // rows of out must not overlap: each dimension steps over what those of smaller strides span
+  struct Dim {
+    int64_t stride, size;
+  } dims[3] = {{p->out_batch, p->batch}, {p->out_draft, p->drafts}, {p->out_head, p->q_heads}};
+  std::sort(dims, dims + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+  int64_t span = a.c.head_dim;
+  for (const Dim& d : dims) {
+    if (d.size <= 1) continue;
+    if (d.stride < span) return refuse(SN_EINVAL, "rows of out must not overlap");
+    span += (d.size - 1) * d.stride;
+  }
+  if (p->table_ld < 0 || p->table_ld > kMost || p->mask_batch < 0 || p->mask_batch > kMost)
+    return refuse(SN_EINVAL, "table_ld and mask_batch must be >= 0 and below 2^40");
+  a.q_batch = p->q_batch;
+  a.q_draft = p->q_draft;
+  a.q_head = p->q_head;
+  a.out_batch = p->out_batch;
+  a.out_draft = p->out_draft;
+  a.out_head = p->out_head;
+  a.table_ld = p->table_ld ? p->table_ld : p->table_cols;
+  a.mask_batch = p->mask_batch;
+  a.batch = p->batch;
+  a.drafts = p->drafts;
+  a.group = p->q_heads / a.c.heads;
+  a.rows = a.drafts * a.group;
+  a.max_places = p->table_cols * a.c.page;
+  a.c_log2 = p->scale * 1.44269504088896340736f;
+
+  const bool f32 = p->dtype == SN_F32;
+  const int most = a.c.head_dim > 128 ? (f32 ? 1 : 2) : f32 ? 2 : 4;
+  w.nt = a.rows <= 16 ? 1 : a.rows <= 32 ? std::min(2, most) : most;
+  const int waves = waves_of(w.nt), blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
+  a.row_waves = 1;
+  while (a.row_waves < waves && a.row_waves < blocks) a.row_waves *= 2;
+  w.unit_rows = 16 * w.nt * a.row_waves;
+  a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
+  a.target = 1024;
+  a.least = 8;
+  const int64_t per_chunk = (int64_t)a.c.heads * a.row_blocks;
+  // a sequence has a chunk for every `per` of its steps and one more at most, and there are `least` steps to a chunk
+  const int64_t steps = ((int64_t)a.max_places + kStep - 1) / kStep;
+  const int64_t longest = std::max<int64_t>(1, (steps + a.least - 1) / a.least);
+  w.units = std::min((int64_t)a.batch * longest * per_chunk, a.target + (int64_t)a.batch * per_chunk);
+  if (w.units * 64 * waves >= (int64_t(1) << 32) ||
+      (int64_t)a.batch * a.drafts * p->q_heads * 256 >= (int64_t(1) << 32))
+    return refuse(SN_EINVAL, "batch * drafts * q_heads is too large");
+  w.off_stat = w.bytes = 0;
+  if (longest > 1) {
+    w.off_stat = (w.units * w.unit_rows * a.c.head_dim * 4 + 255) / 256 * 256;
+    w.bytes = w.off_stat + (w.units * w.unit_rows * 8 + 255) / 256 * 256;
+  }
+  return SN_OK;
+}
+
+}  // namespace
+
+extern "C" SN_API int spectral_cache_attend_workspace_bytes(const sn_cache* cache, const sn_attend* p, int64_t* bytes) {
+  if (!bytes) return refuse(SN_ENULL, "bytes must not be NULL");
+  AttendArgs a{};
+  Way w{};
+  if (int rc = resolve(cache, p, a, w, false)) return rc;
+  *bytes = w.bytes;
+  return SN_OK;
+}
+
+extern "C" SN_API int spectral_cache_attend(const sn_cache* cache, const sn_attend* p, const void* q,
+                                            const int32_t* table, const int32_t* lengths, const int64_t* masks,
+                                            void* out, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+  AttendArgs a{};
+  Way w{};
+  if (int rc = resolve(cache, p, a, w, p && p->batch > 0)) return rc;
+  if (a.batch == 0) return SN_OK;
+  if (a.c.pages == 0) return refuse(SN_EINVAL, "the cache has no pages");
+  if (!q || !lengths || !out || (p->table_cols > 0 && !table))
+    return refuse(SN_ENULL, "q, table, lengths and out must not be NULL");
+  const int type = p->dtype == SN_F32 ? 4 : 2;
+  if (!aligned(q, type) || !aligned(out, type) || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(masks, 8))
+    return refuse(SN_EINVAL, "q, out, table, lengths and masks must be aligned to their type");
+  if (w.bytes > 0) {
+    if (!workspace) return refuse(SN_ENULL, "workspace must not be NULL");
+    if (workspace_bytes < w.bytes)
+      return refuse(SN_EINVAL, "workspace too small (spectral_cache_attend_workspace_bytes)");
+    if (!aligned(workspace, 256)) return refuse(SN_EINVAL, "workspace must be 256-byte aligned");
+  }
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (int rc = check_stream(st)) return rc;
+  a.q = q;
+  a.out = out;
+  a.table = table;
+  a.lengths = lengths;
+  a.masks = masks;
+  a.part_out = static_cast<float*>(workspace);
+  a.part_stat = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.off_stat);
+  const bool f32 = p->dtype == SN_F32, e5m2 = cache->format == SN_E5M2;
+  if (a.c.head_dim <= 64)
+    launch1<64>(a, w, e5m2, f32, st);
+  else if (a.c.head_dim <= 128)
+    launch1<128>(a, w, e5m2, f32, st);
+  else
+    launch1<256>(a, w, e5m2, f32, st);
+  if (int rc = sn::launched("attention")) return rc;
+  if (w.bytes > 0) {
+    const dim3 g((uint32_t)((int64_t)a.batch * a.drafts * p->q_heads));
+    f32 ? join_kernel<true><<<g, 256, 0, st>>>(a, w.unit_rows) : join_kernel<false><<<g, 256, 0, st>>>(a, w.unit_rows);
+    return sn::launched("join");
+  }
+  return SN_OK;
+}

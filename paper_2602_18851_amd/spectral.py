@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libspectral.so")
 
 SN_OK, SN_EINVAL, SN_ENULL, SN_EDTYPE, SN_EHIP, SN_ESTATE = 0, -1, -2, -3, -4, -5
-SN_F32, SN_BF16, SN_E4M3, SN_E5M2 = 0, 1, 2, 3
+SN_F32, SN_BF16, SN_E4M3, SN_E5M2, SN_I8 = 0, 1, 2, 3, 4
 SN_FLAG_VALU_K_SWEEP = 1
 SN_FLAG_GRAM = 2
 SN_FLAG_LAYER = 4
@@ -51,6 +51,14 @@ EXPORTED = (
     "spectral_matmul_fp8",
     "spectral_rotary_frequencies",
     "spectral_rotary",
+    "spectral_quantize_int8",
+    "spectral_matmul_int8_workspace_bytes",
+    "spectral_matmul_int8_kernel",
+    "spectral_matmul_int8",
+    "spectral_cache_write",
+    "spectral_cache_read",
+    "spectral_cache_attend_workspace_bytes",
+    "spectral_cache_attend",
 )
 
 
@@ -124,6 +132,56 @@ class sn_heads(ctypes.Structure):
     ]
 
 
+class sn_matmul_int8(ctypes.Structure):
+    _fields_ = [
+        ("m", ctypes.c_int64),
+        ("n", ctypes.c_int64),
+        ("k", ctypes.c_int64),
+        ("a_type", ctypes.c_int32),
+        ("c_type", ctypes.c_int32),
+        ("ld_a", ctypes.c_int64),
+        ("ld_b", ctypes.c_int64),
+        ("ld_c", ctypes.c_int64),
+        ("sa_row", ctypes.c_int64),
+        ("sb_row", ctypes.c_int64),
+    ]
+
+
+class sn_cache(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("pages", ctypes.c_int64),
+        ("heads", ctypes.c_int32),
+        ("page", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("format", ctypes.c_int32),
+        ("code_page", ctypes.c_int64),
+        ("scale_page", ctypes.c_int64),
+    ]
+
+
+class sn_attend(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("drafts", ctypes.c_int32),
+        ("q_heads", ctypes.c_int32),
+        ("table_cols", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("q_batch", ctypes.c_int64),
+        ("q_draft", ctypes.c_int64),
+        ("q_head", ctypes.c_int64),
+        ("out_batch", ctypes.c_int64),
+        ("out_draft", ctypes.c_int64),
+        ("out_head", ctypes.c_int64),
+        ("table_ld", ctypes.c_int64),
+        ("mask_batch", ctypes.c_int64),
+    ]
+
+
 class SpectralError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"spectral error {code}: {msg}")
@@ -194,6 +252,25 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.spectral_rotary_frequencies.restype = ctypes.c_int
     lib.spectral_rotary.argtypes = [ctypes.POINTER(sn_rotary), i32, i64, vp, i64, i32, vp, i32, vp]
     lib.spectral_rotary.restype = ctypes.c_int
+    lib.spectral_quantize_int8.argtypes = [vp, i64, i64, i64, i32, vp, i64, vp, vp]
+    lib.spectral_quantize_int8.restype = ctypes.c_int
+    lib.spectral_matmul_int8_workspace_bytes.argtypes = [ctypes.POINTER(sn_matmul_int8), ctypes.POINTER(i64)]
+    lib.spectral_matmul_int8_workspace_bytes.restype = ctypes.c_int
+    lib.spectral_matmul_int8_kernel.argtypes = [ctypes.POINTER(sn_matmul_int8), ctypes.POINTER(i32),
+                                                ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i32)]
+    lib.spectral_matmul_int8_kernel.restype = ctypes.c_int
+    lib.spectral_matmul_int8.argtypes = [ctypes.POINTER(sn_matmul_int8), vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.spectral_matmul_int8.restype = ctypes.c_int
+    for rows in (lib.spectral_cache_write, lib.spectral_cache_read):
+        rows.restype = ctypes.c_int
+    lib.spectral_cache_write.argtypes = [ctypes.POINTER(sn_cache), i32, i64, vp, i64, i64, vp, i64, i64, vp, vp]
+    lib.spectral_cache_read.argtypes = [ctypes.POINTER(sn_cache), i32, i64, vp, vp, i64, i64, vp, i64, i64, vp]
+    lib.spectral_cache_attend_workspace_bytes.argtypes = [ctypes.POINTER(sn_cache), ctypes.POINTER(sn_attend),
+                                                          ctypes.POINTER(i64)]
+    lib.spectral_cache_attend_workspace_bytes.restype = ctypes.c_int
+    lib.spectral_cache_attend.argtypes = [ctypes.POINTER(sn_cache), ctypes.POINTER(sn_attend), vp, vp, vp, vp, vp, vp,
+                                          i64, vp]
+    lib.spectral_cache_attend.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -382,6 +459,62 @@ def spectral_rotary(p: sn_rotary, dtype: int, n_tokens: int, positions: int, fir
     """heads: a ctypes array of n_heads sn_heads, or of their seven 64-bit fields in order."""
     _check(load_library().spectral_rotary(ctypes.byref(p), dtype, n_tokens, positions or None, first, inverse, heads,
                                           n_heads, stream or None))
+
+
+# ------------------------- 8-bit integers and the 8-bit cache, context-free
+
+
+def spectral_quantize_int8(x: int, rows: int, cols: int, ld_x: int, dtype: int, codes: int, ld: int, scale: int,
+                           stream: int = 0) -> None:
+    _check(load_library().spectral_quantize_int8(x or None, rows, cols, ld_x, dtype, codes or None, ld, scale or None,
+                                                 stream or None))
+
+
+def spectral_matmul_int8_workspace_bytes(p: sn_matmul_int8) -> int:
+    out = ctypes.c_int64(0)
+    _check(load_library().spectral_matmul_int8_workspace_bytes(ctypes.byref(p), ctypes.byref(out)))
+    return out.value
+
+
+def spectral_matmul_int8_kernel(p: sn_matmul_int8) -> tuple[str, int, int, int]:
+    """(name of the kernel, parts of the sum, workgroups, threads of each) of a product."""
+    kernel, parts, threads = ctypes.c_int32(), ctypes.c_int32(), ctypes.c_int32()
+    workgroups = ctypes.c_int64()
+    _check(load_library().spectral_matmul_int8_kernel(ctypes.byref(p), ctypes.byref(kernel), ctypes.byref(parts),
+                                                      ctypes.byref(workgroups), ctypes.byref(threads)))
+    return MATMUL_KERNELS[kernel.value], parts.value, workgroups.value, threads.value
+
+
+def spectral_matmul_int8(p: sn_matmul_int8, a: int, sa: int, b: int, sb: int, c: int, workspace: int,
+                         workspace_bytes: int, stream: int = 0) -> None:
+    _check(load_library().spectral_matmul_int8(ctypes.byref(p), a or None, sa or None, b or None, sb or None, c or None,
+                                               workspace or None, workspace_bytes, stream or None))
+
+
+def spectral_cache_write(cache: sn_cache, dtype: int, tokens: int, k: int, k_token: int, k_head: int, v: int,
+                         v_token: int, v_head: int, slots: int, stream: int = 0) -> None:
+    _check(load_library().spectral_cache_write(ctypes.byref(cache), dtype, tokens, k or None, k_token, k_head,
+                                               v or None, v_token, v_head, slots or None, stream or None))
+
+
+def spectral_cache_read(cache: sn_cache, dtype: int, tokens: int, slots: int, k: int, k_token: int, k_head: int, v: int,
+                        v_token: int, v_head: int, stream: int = 0) -> None:
+    _check(load_library().spectral_cache_read(ctypes.byref(cache), dtype, tokens, slots or None, k or None, k_token,
+                                              k_head, v or None, v_token, v_head, stream or None))
+
+
+def spectral_cache_attend_workspace_bytes(cache: sn_cache, p: sn_attend) -> int:
+    out = ctypes.c_int64(0)
+    _check(load_library().spectral_cache_attend_workspace_bytes(ctypes.byref(cache), ctypes.byref(p),
+                                                                ctypes.byref(out)))
+    return out.value
+
+
+def spectral_cache_attend(cache: sn_cache, p: sn_attend, q: int, table: int, lengths: int, masks: int, out: int,
+                          workspace: int, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load_library().spectral_cache_attend(ctypes.byref(cache), ctypes.byref(p), q or None, table or None,
+                                                lengths or None, masks or None, out or None, workspace or None,
+                                                workspace_bytes, stream or None))
 
 
 # ------------------------------------------- consumer-side calibration

@@ -1,0 +1,509 @@
+"""The 8-bit cache of keys and values and attention over it against the float64 oracle (oracle.cache)."""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as oracle, fp8_blocks
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # pragma: no cover - collected on CPU machines, skipped there
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_2602_18851_amd import Fp8Cache, Rotary, matmul_int8, quantize_int8  # noqa: E402
+
+TORCH = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2, "f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def rng(*key):
+    return np.random.default_rng([20261209, *key])
+
+
+def on_gpu(x, dtype):
+    return torch.from_numpy(np.asarray(x, dtype=np.float32)).to(TORCH[dtype]).cuda()
+
+
+def host(t):
+    return t.detach().cpu().double().numpy()
+
+
+def fmt_of(cache):
+    return "e4m3" if cache.k.dtype == TORCH["e4m3"] else "e5m2"
+
+
+def held(cache):
+    """Values of keys and values [pages, heads, page, d]."""
+    out = []
+    for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        with np.errstate(invalid="ignore"):
+            out.append(fp8_blocks.decode(codes.view(torch.uint8).cpu().numpy(), fmt_of(cache)) * host(scale)[..., None])
+    return out
+
+
+def spread(r, *shape):
+    return r.standard_normal(shape) * np.exp2(r.integers(-3, 4, (*shape[:-1], 1))) * np.exp2(r.integers(-2, 3, shape[-1]))
+
+
+# ------------------------------------------------------------------ write and read
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,heads,dh,page", [(1, 1, 16, 16), (5, 3, 64, 16), (37, 8, 128, 32), (70, 2, 80, 64), (9, 5, 256, 128),
+                                                  (33, 25, 96, 16), (20, 1, 48, 1024)])
+def test_rows_go_to_their_slots_and_back(fmt, dtype, tokens, heads, dh, page):
+    r = rng(tokens, heads, dh, page)
+    pages = tokens // page + 3
+    c = Fp8Cache.empty(pages, heads, page, dh, fmt)
+    for t in (c.k, c.v):
+        t.view(torch.uint8).fill_(0x55)
+    for t in (c.k_scale, c.v_scale):
+        t.fill_(-1.0)
+    k, v = (on_gpu(spread(r, tokens, heads, dh), dtype) for _ in range(2))
+    slots = r.permutation(pages * page)[:tokens]
+    c.write(k, v, torch.from_numpy(slots).cuda())
+    for x, codes, scale in ((k, c.k, c.k_scale), (v, c.v, c.v_scale)):
+        ref_codes = np.full((pages, heads, page, dh), fp8_blocks.decode(np.uint8([0x55]), fmt)[0])
+        ref_scale = np.full((pages, heads, page), -1.0)
+        cs, ss = oracle.rows(host(x), fmt)
+        ref_codes[slots // page, :, slots % page], ref_scale[slots // page, :, slots % page] = cs, ss
+        np.testing.assert_array_equal(fp8_blocks.decode(codes.view(torch.uint8).cpu().numpy(), fmt), ref_codes)
+        np.testing.assert_array_equal(host(scale), ref_scale)
+    at = torch.from_numpy(r.permutation(slots)).cuda()
+    at = torch.cat([at, at[:1]])  # a place may be read twice
+    for out in ("f32", "bf16"):
+        got = c.read(at, dtype=TORCH[out])
+        for g, full in zip(got, held(c)):
+            n = at.cpu().numpy()
+            # products of a code and a power of two: exact in either type
+            assert g.dtype == TORCH[out] and np.array_equal(host(g), full[n // page, :, n % page])
+
+
+def test_slots_outside_are_padding():
+    c = Fp8Cache.empty(3, 2, 16, 64)
+    k, v = (on_gpu(spread(rng(1, i), 6, 2, 64), "bf16") for i in range(2))
+    slots = torch.tensor([-1, 47, 48, 1 << 40, -(1 << 40), 5], device="cuda")
+    c.write(k, v, slots)
+    ref = Fp8Cache.empty(3, 2, 16, 64)
+    ref.write(k[[1, 5]], v[[1, 5]], slots[[1, 5]])
+    for a, b in ((c.k, ref.k), (c.v, ref.v)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert torch.equal(c.k_scale, ref.k_scale) and torch.equal(c.v_scale, ref.v_scale)
+    got = c.read(slots, out=tuple(torch.full_like(k, float("nan")) for _ in range(2)))
+    for g, r in zip(got, ref.read(slots[[1, 5]])):
+        assert (g[[0, 2, 3, 4]] == 0).all() and torch.equal(g[[1, 5]], r)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_rows_of_extremes(fmt):
+    """Zeros, the scale's lower limit, the largest numbers, infinities and NaN."""
+    x = np.zeros((7, 1, 64))
+    largest = fp8_blocks.FORMATS[fmt][2]
+    x[1, 0, :2], x[2, 0, :3], x[3, 0, :2] = (2.0 ** -130, -2.0 ** -140), (largest, 1.0, -3.3), (1.5e38, -1e30)
+    x[4, 0, 5], x[5, 0, 63] = np.inf, np.nan
+    x[6, 0] = np.nextafter(np.float32(largest), np.float32(np.inf))
+    c = Fp8Cache.empty(1, 1, 16, 64, fmt)
+    t = on_gpu(x, "f32")
+    c.write(t, t, torch.arange(7, device="cuda"))
+    with np.errstate(invalid="ignore"):
+        codes, scale = oracle.rows(host(t), fmt)
+    for cs, ss in ((c.k, c.k_scale), (c.v, c.v_scale)):
+        np.testing.assert_array_equal(fp8_blocks.decode(cs.view(torch.uint8).cpu().numpy()[0, 0, :7], fmt), codes[:, 0])
+        np.testing.assert_array_equal(host(ss)[0, 0, :7], scale[:, 0])
+
+
+def test_rows_of_any_strides_and_pages_apart():
+    """Keys and values as windows of one projection; a cache whose pages hold keys and values side by side."""
+    r = rng(3)
+    both = torch.zeros(4, 2, 3, 16, 80, dtype=torch.uint8, device="cuda").view(TORCH["e4m3"])
+    scales = torch.zeros(4, 2, 3, 16, device="cuda")
+    c = Fp8Cache(both[:, 0], scales[:, 0], both[:, 1], scales[:, 1])
+    qkv = on_gpu(spread(r, 20, 1, 7 * 80 + 5)[:, 0], "bf16")
+    k, v = qkv[:, 81:81 + 240].view(20, 3, 80), qkv[:, 321:321 + 240].view(20, 3, 80)
+    slots = torch.from_numpy(r.permutation(64)[:20]).cuda()
+    c.write(k, v, slots)
+    ref = Fp8Cache.empty(4, 3, 16, 80)
+    ref.write(k.contiguous(), v.contiguous(), slots)
+    for a, b in ((c.k, ref.k), (c.v, ref.v)):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.view(torch.uint8))
+    room = torch.full((2, 3, 20, 83), 7.0, device="cuda")  # tokens within heads
+    out = [room[i, :, :, 1:81].transpose(0, 1) for i in range(2)]
+    c.read(slots, out=out)
+    for a, b in zip(out, ref.read(slots, dtype=torch.float32)):
+        assert torch.equal(a, b)
+    assert (room[..., 0] == 7.0).all() and (room[..., 81:] == 7.0).all()
+    c.write(k.transpose(0, 1).contiguous().transpose(0, 1), v, slots)  # tokens within heads
+    assert torch.equal(c.k.contiguous().view(torch.uint8), ref.k.view(torch.uint8))
+    q = on_gpu(r.standard_normal((1, 2, 6, 80)), "bf16")
+    table, lengths = torch.tensor([[2, 0, 3, 1]], dtype=torch.int32, device="cuda"), torch.tensor([64], dtype=torch.int32, device="cuda")
+    assert torch.equal(c.attend(q, table, lengths), ref.attend(q, table, lengths))
+
+
+# ------------------------------------------------------------------ attention
+
+
+def setup(key, batch, drafts, heads, group, dh, page, lengths, fmt="e4m3", dtype="bf16", junk=True, spare=2):
+    """A cache with the sequences' places in pages of any order; all else of it is NaN."""
+    r = rng(11, *key)
+    need = [-(-n // page) for n in lengths]
+    pages = sum(need) + spare
+    cols = max(max(need), 1)
+    c = Fp8Cache.empty(pages, heads, page, dh, fmt)
+    if junk:
+        for t in (c.k, c.v):
+            t.view(torch.uint8).fill_(0x7F)
+        for t in (c.k_scale, c.v_scale):
+            t.fill_(float("nan"))
+    ids = r.permutation(pages)
+    table = np.full((batch, cols), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = ids[at:at + n]
+        at += n
+        if lengths[b]:
+            t = np.arange(lengths[b])
+            slots = torch.from_numpy(table[b, t // page].astype(np.int64) * page + t % page).cuda()
+            c.write(*(on_gpu(spread(r, lengths[b], heads, dh), "f32") for _ in range(2)), slots)
+    q = on_gpu(r.standard_normal((batch, drafts, heads * group, dh)) * 0.7, dtype)
+    return c, q, torch.from_numpy(table).cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+
+
+def trees(key, drafts, n=None):
+    r = rng(12, *key)
+    out = np.zeros((n or 1, drafts), np.uint64)
+    for m in out:
+        for i in range(drafts):
+            parent = int(r.integers(-1, i)) if i else -1
+            m[i] = (int(m[parent]) if parent >= 0 else 0) | (1 << i)
+    return out if n else out[0]
+
+
+def check(got, q, cache, table, lengths, masks=None, scale=None):
+    """The rounding errors of the sums q k over d elements, in the matrix cores' order (2^-23 each of the magnitudes' sum at
+    most, and float32 queries held to 2^-24), of the exponent (the factor and one product, 2^-23 of it, twice) and
+    of its power (2^-22) are errors of the weights, relative to them: `off`.  They enter a result once as its weights and
+    once as their sum.  Weights are held to 2^-16 (bf16) or 2^-24, sums over n places and some joins round n + 64 times."""
+    dtype = "f32" if q.dtype == torch.float32 else "bf16"
+    d = q.shape[3]
+    ref, mag, reach = oracle.attend(host(q), *held(cache), table.cpu().numpy(), lengths.cpu().numpy(),
+                                    None if masks is None else masks, scale)
+    n = int(lengths.max())
+    off = reach[..., None] * (d + 8) * 2.0 ** -23 + 2.0 ** -22
+    tol = mag * (2 * off * (1 + off) + (2.0 ** -16 if dtype == "bf16" else 2.0 ** -24) + 2 * (n + 64) * 2.0 ** -23)
+    tol += np.abs(ref) * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) + 1e-37
+    got = host(got)
+    assert (np.isnan(got) == np.isnan(ref)).all()
+    err = np.abs(got - ref)
+    fine = ~np.isnan(ref)
+    assert (err[fine] <= tol[fine]).all(), float((err[fine] / tol[fine]).max())
+
+
+def gpu_masks(m):
+    return torch.from_numpy(m.view(np.int64)).cuda()
+
+
+# batch, drafts, heads, group, d_h, page, lengths
+SHAPES = [
+    (1, 1, 1, 1, 16, 16, [1]), (1, 1, 2, 4, 64, 16, [33]), (3, 1, 2, 8, 128, 16, [1, 31, 200]), (2, 1, 3, 5, 80, 32, [64, 65]),
+    (2, 1, 2, 1, 96, 64, [100, 7]), (2, 1, 1, 16, 128, 128, [300, 129]), (1, 1, 2, 20, 64, 16, [500]), (1, 1, 1, 3, 256, 16, [77]),
+    (2, 2, 2, 4, 64, 16, [50, 2]), (2, 7, 1, 8, 128, 32, [90, 600]), (1, 64, 2, 1, 64, 16, [700]), (1, 33, 1, 5, 128, 16, [40]),
+    (2, 64, 1, 8, 128, 64, [64, 400]), (1, 20, 1, 3, 256, 16, [130]), (1, 64, 1, 4, 256, 32, [300]), (1, 64, 1, 5, 112, 16, [129]),
+    (1, 17, 1, 2, 48, 16, [1000]), (5, 3, 2, 2, 32, 16, [3, 4, 0, 1, 60]),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", "bf16"), ("e4m3", "f32"), ("e5m2", "bf16"), ("e5m2", "f32")])
+@pytest.mark.parametrize("tree", ["chain", "one", "each"])
+def test_attention(shape, fmt, dtype, tree):
+    batch, drafts = shape[:2]
+    c, q, table, lengths = setup(shape[:6], *shape, fmt=fmt, dtype=dtype)
+    masks = None if tree == "chain" else trees(shape[:6], drafts, batch if tree == "each" else None)
+    got = c.attend(q, table, lengths, tree=None if masks is None else gpu_masks(masks))
+    check(got, q, c, table, lengths, masks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,drafts,heads,group,dh,page,lengths", [
+    (1, 1, 1, 8, 128, 64, [9001]), (3, 1, 2, 4, 64, 16, [5000, 300, 2049]), (2, 5, 1, 8, 128, 32, [4100, 257]),
+    (70, 1, 1, 2, 64, 16, [200 + 13 * i for i in range(70)]), (1, 64, 1, 8, 128, 256, [3000]), (2, 2, 1, 4, 256, 64, [2500, 2])])
+def test_sequences_in_chunks(batch, drafts, heads, group, dh, page, lengths, dtype):
+    """Lengths at which workgroups share a sequence, beside short ones."""
+    c, q, table, lens = setup((batch, drafts, dh), batch, drafts, heads, group, dh, page, lengths, dtype=dtype)
+    got = c.attend(q, table, lens)
+    check(got, q, c, table, lens)
+    assert torch.equal(got, c.attend(q, table, lens))  # the same bits again
+
+
+def test_a_long_sequence():
+    """Equal keys, so that every weight is the same, and values that are whole numbers: the mean."""
+    n, page = 131071, 256
+    c = Fp8Cache.empty(512, 1, page, 64)
+    c.k_scale.fill_(1.0)
+    c.v_scale.fill_(1.0)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    c.v.copy_(torch.randint(-8, 9, c.v.shape, generator=g, device="cuda").float())
+    table = torch.randperm(512, generator=g, device="cuda").to(torch.int32)[None]
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    q = torch.randn(1, 1, 4, 64, generator=g, device="cuda")
+    got = c.attend(q, table, lengths)
+    v = c.v.float()[table[0].long()].view(-1, 64)[:n].double()
+    # weights of 1 are exact; sums of whole numbers below 2^24 too; a division
+    assert ((got.double() - v.mean(0)).abs() <= v.mean(0).abs() * 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_see_nothing(dtype):
+    c, q, table, lengths = setup((1,), 4, 3, 2, 2, 64, 16, [3, 40, 0, 3], dtype=dtype)
+    masks = np.zeros((4, 3), np.uint64)
+    masks[0, 1], masks[3] = 0b010, 0b111
+    got = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    check(got, q, c, table, lengths, masks)
+    assert (got[0, [0, 2]] == 0).all() and (got[2] == 0).all()
+
+
+def test_masks_of_64_tokens():
+    """The highest bit, and bits of later tokens."""
+    c, q, table, lengths = setup((2,), 1, 64, 1, 1, 64, 16, [90])
+    masks = (np.uint64(1) << np.arange(64, dtype=np.uint64))
+    masks[3] = np.uint64((1 << 64) - 1)
+    masks[63] = np.uint64(1 << 63)
+    check(c.attend(q, table, lengths, tree=gpu_masks(masks)), q, c, table, lengths, masks)
+    c, q, table, lengths = setup((3,), 2, 5, 1, 2, 64, 16, [90, 4])
+    masks = np.full((2, 5), (1 << 64) - 1, np.uint64)  # bits past the tokens say nothing
+    check(c.attend(q, table, lengths, tree=gpu_masks(masks)), q, c, table, lengths, masks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("what", ["written", "codes"])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_drafts_that_are_not_finite_reach_who_sees_them(dtype, what, fmt):
+    """A drafted token's row of NaN (or of one NaN code): NaN where it is seen, the finite result elsewhere."""
+    c, q, table, lengths = setup((4,), 1, 6, 1, 2, 64, 16, [45], fmt=fmt, dtype=dtype)
+    masks = np.array([0b1, 0b11, 0b101, 0b1011, 0b10101, 0b100011], np.uint64)
+    place = 45 - 6 + 1  # token 1: seen by itself, 3 and 5
+    page, at = int(table[0, place // 16]), place % 16
+    before = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    check(before, q, c, table, lengths, masks)
+    if what == "written":
+        bad = torch.full((1, 1, 64), float("nan"), device="cuda")
+        c.write(torch.zeros_like(bad), bad, torch.tensor([page * 16 + at], device="cuda"))
+    else:
+        c.v.view(torch.uint8)[page, 0, at, 17] = 0x7F
+    got = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    for i in range(6):
+        if masks[i] & np.uint64(2):
+            assert torch.isnan(got[0, i] if what == "written" else got[0, i, :, 17]).all()
+        else:
+            assert torch.equal(got[0, i], before[0, i])
+    if what == "codes":
+        assert torch.isfinite(got[0, :, :, :17]).all() and torch.isfinite(got[0, :, :, 18:]).all()
+    nan = torch.full((1, 1, 64), float("nan"), device="cuda")
+    c.write(nan, torch.zeros_like(nan), torch.tensor([page * 16 + at], device="cuda"))  # and of keys
+    got = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    for i in range(6):
+        if masks[i] & np.uint64(2):
+            assert torch.isnan(got[0, i]).all()
+        else:
+            assert torch.equal(got[0, i], before[0, i])
+
+
+def test_a_place_that_is_not_finite_and_seen_by_all():
+    c, q, table, lengths = setup((5,), 2, 2, 1, 2, 64, 16, [100, 100])
+    before = c.attend(q, table, lengths)
+    place = 40
+    nan = torch.full((1, 1, 64), float("nan"), device="cuda")
+    c.write(torch.zeros_like(nan), nan, torch.tensor([int(table[0, place // 16]) * 16 + place % 16], device="cuda"))
+    got = c.attend(q, table, lengths)
+    assert torch.isnan(got[0]).all() and torch.equal(got[1], before[1])
+
+
+def test_pages_that_are_not_there_are_not_seen():
+    c, q, table, lengths = setup((6,), 2, 2, 2, 2, 64, 16, [100, 90])
+    table[0, 2], table[1, 0], table[0, 6] = c.pages, -5, 1 << 30
+    check(c.attend(q, table, lengths), q, c, table, lengths)
+    table[1] = -1
+    got = c.attend(q, table, lengths)
+    assert (got[1] == 0).all()
+    # lengths past the table end with it, negative ones hold nothing
+    lengths = torch.tensor([1 << 30, -7], dtype=torch.int32, device="cuda")
+    table[0] = torch.arange(table.shape[1], device="cuda")
+    c.k.view(torch.uint8).fill_(0x30), c.v.view(torch.uint8).fill_(0x31), c.k_scale.fill_(1.0), c.v_scale.fill_(1.0)
+    check(c.attend(q, table, lengths), q, c, table, lengths)
+
+
+def test_scales_of_all_sizes():
+    """Rows that differ by many octaves, and rows of zeros, whose scale is the least."""
+    c, q, table, lengths = setup((7,), 1, 1, 1, 4, 64, 16, [80], dtype="f32")
+    c.v_scale.copy_(torch.exp2(torch.randint(-60, 60, c.v_scale.shape, device="cuda").float()))
+    c.k_scale.copy_(torch.exp2(torch.randint(-30, 0, c.k_scale.shape, device="cuda").float()))
+    check(c.attend(q, table, lengths), q, c, table, lengths)
+    zero = torch.zeros(5, 1, 64, device="cuda")
+    c.write(zero, zero, int(table[0, 1]) * 16 + torch.arange(5, device="cuda"))
+    check(c.attend(q, table, lengths), q, c, table, lengths)
+
+
+def test_logits_far_apart():
+    """Weights from 1 to none, and logits in the thousands."""
+    c, q, table, lengths = setup((8,), 1, 1, 2, 4, 128, 16, [300], dtype="f32")
+    for factor in (30.0, 1000.0):
+        check(c.attend(q * factor, table, lengths), q * factor, c, table, lengths)
+    check(c.attend(q, table, lengths, scale=0.03), q, c, table, lengths, scale=0.03)
+
+
+def test_queries_and_results_of_any_strides():
+    c, q, table, lengths = setup((9,), 3, 4, 2, 3, 64, 16, [50, 9, 80])
+    ref = c.attend(q, table, lengths)
+    room = torch.full((4, 6, 3, 67), 7.0, dtype=torch.bfloat16, device="cuda")  # tokens, heads, batch
+    qs = room[..., 2:66].permute(2, 0, 1, 3)
+    qs.copy_(q)
+    wide = torch.full((3, table.shape[1] + 3), 9, dtype=torch.int32, device="cuda")
+    wide[:, 1:1 + table.shape[1]] = table
+    out_room = torch.full((6, 3, 4, 65), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = out_room[..., :64].permute(1, 2, 0, 3)
+    got = c.attend(qs, wide[:, 1:1 + table.shape[1]], lengths, out=out)
+    assert got is out and torch.equal(out, ref) and (out_room[..., 64] == 7.0).all()
+    one = q[:1].expand(3, -1, -1, -1)  # the same queries for all
+    assert torch.equal(c.attend(one, table, lengths), c.attend(one.contiguous(), table, lengths))
+    masks = gpu_masks(trees((9,), 4))
+    assert torch.equal(c.attend(q, table, lengths, tree=masks), c.attend(q, table, lengths, tree=masks.expand(3, 4)))
+
+
+def test_a_chain_is_a_tree_of_one_branch():
+    c, q, table, lengths = setup((10,), 2, 9, 2, 4, 128, 16, [500, 30])
+    masks = gpu_masks((np.uint64(2) << np.arange(9, dtype=np.uint64)) - np.uint64(1))
+    assert torch.equal(c.attend(q, table, lengths), c.attend(q, table, lengths, tree=masks))
+
+
+def test_refusals():
+    c, q, table, lengths = setup((13,), 2, 3, 2, 2, 64, 16, [50, 40])
+    k = torch.zeros(4, 2, 64, device="cuda")
+    slots = torch.arange(4, device="cuda")
+    bad = [
+        lambda: Fp8Cache(c.k.float(), c.k_scale, c.v, c.v_scale), lambda: Fp8Cache(c.k[0], c.k_scale, c.v, c.v_scale),
+        lambda: Fp8Cache(c.k, c.k_scale, c.v[1:], c.v_scale), lambda: Fp8Cache(c.k, c.k_scale[:, :1], c.v, c.v_scale),
+        lambda: Fp8Cache(c.k, c.k_scale.double(), c.v, c.v_scale), lambda: Fp8Cache.empty(2, 2, 48, 64),
+        lambda: Fp8Cache.empty(2, 2, 16, 72), lambda: Fp8Cache.empty(2, 2, 16, 64, fmt="int8"),
+        lambda: Fp8Cache(c.k[:, :, :, :32], c.k_scale, c.v[:, :, :, :32], c.v_scale),
+        lambda: Fp8Cache(c.k[::2], c.k_scale[::2], c.v[::2], c.v_scale[::2].clone()) and
+        Fp8Cache(c.k[:2], c.k_scale[:2], c.v[:4:2], c.v_scale[:4:2]),
+        lambda: c.write(k, k[:3], slots), lambda: c.write(k, k.bfloat16(), slots), lambda: c.write(k.half(), k.half(), slots),
+        lambda: c.write(k, k, slots.int()), lambda: c.write(k, k, slots[:3]), lambda: c.write(k, k, slots.cpu()),
+        lambda: c.write(k.clone().requires_grad_(), k, slots), lambda: c.write(k[:, :, :32], k[:, :, :32], slots),
+        lambda: c.write(k.transpose(1, 2).contiguous().transpose(1, 2), k, slots), lambda: c.write(k[0], k[0], slots),
+        lambda: c.read(slots, dtype=torch.float16), lambda: c.read(slots.int()), lambda: c.read(slots[None]),
+        lambda: c.read(slots, out=(k, k[:3])), lambda: c.attend(q.half(), table, lengths), lambda: c.attend(q[0], table, lengths),
+        lambda: c.attend(q[:, :, :3], table, lengths), lambda: c.attend(q[:, :, :, :32], table, lengths),
+        lambda: c.attend(q[:, :0], table, lengths), lambda: c.attend(q.expand(2, 3, 4, 64).repeat(1, 22, 1, 1), table, lengths),
+        lambda: c.attend(q, table.long(), lengths), lambda: c.attend(q, table[:1], lengths), lambda: c.attend(q, table.t(), lengths),
+        lambda: c.attend(q, table, lengths.long()), lambda: c.attend(q, table, lengths[:1]), lambda: c.attend(q, table, lengths.cpu()),
+        lambda: c.attend(q, table, lengths, tree=torch.ones(2, device="cuda", dtype=torch.int64)),
+        lambda: c.attend(q, table, lengths, tree=torch.ones(3, device="cuda", dtype=torch.int32)),
+        lambda: c.attend(q.clone().requires_grad_(), table, lengths), lambda: c.attend(q, table, lengths, out=q.float()),
+        lambda: c.attend(q, table, lengths, out=q[:, :, :2])]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            print("call", i)
+    from paper_2602_18851_amd import SpectralError
+    with pytest.raises(SpectralError):
+        c.read(slots, out=(k[:1].expand(4, 2, 64), k))
+    with pytest.raises(SpectralError):
+        c.attend(q, table, lengths, out=q[:1].expand(2, -1, -1, -1))
+    for scale in (0.0, -1.0, float("nan")):
+        with pytest.raises(SpectralError):
+            c.attend(q, table, lengths, scale=scale)
+    assert c.attend(q[:0], table[:0], lengths[:0]).shape == (0, 3, 4, 64)
+    c.write(k[:0], k[:0], slots[:0])
+    assert c.read(slots[:0])[0].shape == (0, 2, 64)
+
+
+# ------------------------------------------------------- streams and graphs
+
+
+def test_calls_replay_from_a_graph():
+    """A generated token after another from one graph: its slot, lengths and inputs change between replays."""
+    heads, group, dh, page = 2, 4, 64, 16
+    c, q, table, lengths = setup((20,), 3, 1, heads, group, dh, page, [700, 40, 16])
+    eager, _, _, _ = setup((20,), 3, 1, heads, group, dh, page, [700, 40, 16])
+    k, v = (torch.zeros(3, heads, dh, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    slots = torch.full((3,), -1, dtype=torch.int64, device="cuda")
+    out, ws = torch.empty_like(q), torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    c.write(k, v, slots)
+    c.attend(q, table, lengths, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.write(k, v, slots)
+        c.attend(q, table, lengths, out=out, workspace=ws)
+    r = rng(21)
+    last = [int(n) for n in lengths]
+    for rep in range(4):
+        at = []
+        for b in range(3):  # the token takes the place of the last one but rep
+            place = last[b] - 1 - rep
+            at.append(int(table[b, place // page]) * page + place % page)
+        slots.copy_(torch.tensor(at))
+        lengths.copy_(torch.tensor([n - rep for n in last], dtype=torch.int32))
+        for t in (k, v, q):
+            t.copy_(on_gpu(r.standard_normal(t.shape), "bf16"))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.write(k, v, slots)
+        assert torch.equal(out, eager.attend(q, table, lengths))
+        assert torch.equal(c.k.view(torch.uint8), eager.k.view(torch.uint8))
+
+
+def test_two_streams_at_once():
+    sets = [setup((22, i), 2, 2, 2, 4, 128, 32, [3000, 1500]) for i in range(2)]
+    refs = [c.attend(*rest) for c, *rest in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(sets[i][0].attend(*sets[i][1:]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(g, refs[i]) for g in got[i])
+
+
+# ------------------------------------------------------------------ all together
+
+
+def test_a_prompt_and_drafted_tokens_through_a_layer():
+    """An attention layer in 8 bits: projections as 8-bit integers, rotary positions, the cache, and a tree of drafted tokens,
+    against the same steps with the oracle's attention."""
+    d, heads, group, dh, page = 256, 2, 2, 64, 16
+    r = rng(30)
+    hq = heads * group
+    w = {n: quantize_int8(on_gpu(r.standard_normal((rows, d)) * d ** -0.5, "bf16"))
+         for n, rows in (("q", hq * dh), ("k", heads * dh), ("v", heads * dh))}
+    wo = quantize_int8(on_gpu(r.standard_normal((d, hq * dh)) * d ** -0.5, "bf16"))
+    rot = Rotary(dh)
+    c = Fp8Cache.empty(8, heads, page, dh)
+    table = torch.tensor([[5, 2, 7, 0, 1, 3]], dtype=torch.int32, device="cuda")
+
+    def step(x, first, tree):
+        n = x.shape[0]
+        a = quantize_int8(x)
+        q, k, v = (matmul_int8(a, w[name]).view(n, -1, dh) for name in "qkv")
+        depth = torch.arange(first, first + n, device="cuda") if tree is None else \
+            first - 1 + torch.tensor([bin(int(m)).count("1") for m in tree], device="cuda")
+        q, k = rot.apply(q, k, positions=depth)
+        place = torch.arange(first, first + n, device="cuda")
+        c.write(k, v, table[0].long()[place // page] * page + place % page)
+        lengths = torch.tensor([first + n], dtype=torch.int32, device="cuda")
+        o = c.attend(q[None], table, lengths, tree=None if tree is None else gpu_masks(tree))
+        check(o, q[None], c, table, lengths, tree)
+        y = matmul_int8(o.view(n, hq * dh), wo)
+        assert torch.isfinite(y).all() and y.shape == (n, d)
+        return y
+
+    for i in range(0, 64, 32):  # a prompt in pieces of chains
+        step(on_gpu(r.standard_normal((32, d)), "bf16"), i, None)
+    step(on_gpu(r.standard_normal((1, d)), "bf16"), 64, None)
+    step(on_gpu(r.standard_normal((10, d)), "bf16"), 65, trees((30,), 10))
