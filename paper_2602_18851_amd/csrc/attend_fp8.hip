@@ -16,6 +16,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "cache_fp8.h"
 #include "device_util.h"
@@ -26,7 +27,9 @@ namespace {
 using namespace sn_dev;
 using sn::CacheView;
 
-constexpr int kStep = 32;  // places that a wave takes at a time
+constexpr int kStep = 32;   // places that a wave of attend_kernel takes at a time
+constexpr int kTile = 64;   // places that a workgroup of tree_kernel takes at a time
+constexpr int kTreeWaves = 8;
 
 struct AttendArgs {
   CacheView c;
@@ -39,7 +42,7 @@ struct AttendArgs {
   const int64_t* masks;  // or NULL: a drafted token sees those before it and itself
   int64_t mask_batch;
   int32_t batch, drafts, group, rows;  // rows = drafts * group, of a key head
-  int32_t max_places;
+  int32_t max_places, step;  // step: kStep or kTile
   int32_t row_waves, row_blocks;  // waves of a workgroup with rows of their own, and workgroups that share a key head's rows
   int32_t target, least;          // workgroups to aim at, and the least steps of one
   float c_log2;                   // scale * log2(e)
@@ -47,11 +50,13 @@ struct AttendArgs {
   float2* part_stat;              // maximum and sum of each row
 };
 
+constexpr float kNone = -__builtin_inff();
+
 // ---- how the places are shared out --------------------------------------
 //
 // Lengths are known on the device only, and every workgroup derives the same plan from them: all sequences'
-// steps of kStep places, over `target` workgroups, give the steps of one (`least` at least, which hide its start and end);
-// a sequence is cut into as many equal chunks as that asks for, one at least.  A unit, a chunk
+// steps, over `target` workgroups, give the steps of one (`least` at least, which hide its start and end);
+// a sequence is cut into as many equal chunks as come nearest to that, one at least.  A unit, a chunk
 // of one key head's rows, is one workgroup's.
 struct Split {
   int64_t per;  // steps that a unit may take
@@ -59,7 +64,7 @@ struct Split {
 
 __device__ __forceinline__ int steps_of(const AttendArgs& a, int b) {
   const int n = min(max(a.lengths[b], 0), a.max_places);
-  return (int)(((int64_t)n + kStep - 1) / kStep);
+  return (int)(((int64_t)n + a.step - 1) / a.step);
 }
 
 __device__ __forceinline__ Split plan(const AttendArgs& a, int lane) {
@@ -72,7 +77,50 @@ __device__ __forceinline__ Split plan(const AttendArgs& a, int lane) {
 }
 
 __device__ __forceinline__ int chunks_of(int steps, const Split& s) {
-  return max(1, (int)((steps + s.per - 1) / s.per));
+  return max(1, (int)((steps + s.per / 2) / s.per));
+}
+
+// The unit of this workgroup.
+struct Unit {
+  int b, h, rb, len, n_chunks, step0, step1;  // steps from step0 to step1 - 1 (none of a sequence without places)
+};
+
+__device__ __forceinline__ bool find_unit(const AttendArgs& a, int lane, Unit& u) {
+  const Split split = plan(a, lane);
+  const int per_chunk = a.c.heads * a.row_blocks;  // units of a chunk
+  int64_t left = blockIdx.x;                       // units before this one, less those of the sequences before
+  int b = -1;
+  for (int b0 = 0; b0 < a.batch; b0 += 64) {
+    int64_t mine = 0;
+    if (b0 + lane < a.batch) mine = (int64_t)chunks_of(steps_of(a, b0 + lane), split) * per_chunk;
+    int64_t sum = mine;  // of the lanes up to this one
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int64_t o = __shfl_up(sum, d);
+      if (lane >= d) sum += o;
+    }
+    const uint64_t there = __ballot(sum > left);
+    if (there) {
+      const int at = __builtin_ctzll(there);
+      b = b0 + at;
+      left -= __shfl(sum - mine, at);
+      break;
+    }
+    left -= __shfl(sum, 63);
+  }
+  if (b < 0) return false;
+  u.b = uni(b);
+  const int in_seq = uni((int)left);
+  const int chunk = in_seq / per_chunk, rest = in_seq % per_chunk;
+  u.h = rest % a.c.heads;
+  u.rb = rest / a.c.heads;
+  u.len = uni(min(max(a.lengths[u.b], 0), a.max_places));
+  const int steps = uni(steps_of(a, u.b));
+  u.n_chunks = uni(chunks_of(steps, split));
+  const int per = (steps + u.n_chunks - 1) / u.n_chunks;
+  u.step0 = min(steps, chunk * per);
+  u.step1 = min(steps, u.step0 + per);
+  return true;
 }
 
 // ---- arithmetic ------------------------------------------------------------
@@ -118,11 +166,20 @@ __device__ __forceinline__ float quarters_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-constexpr float kNone = -__builtin_inff();
 
 // exp2 of the distance to a running maximum; a row that has seen nothing has none.
 __device__ __forceinline__ float weight_of(float m, float to, float c) {
   return m == kNone ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
+}
+
+// Elements d .. d + 3 of row r of sequence b from their sums.
+template <typename T>
+__device__ __forceinline__ void store_row4(const AttendArgs& a, int b, int h, int r, int d, const f32x4& x) {
+  typedef T vec __attribute__((ext_vector_type(4)));
+  typedef vec vec_any __attribute__((aligned(sizeof(T))));
+  const int i = r / a.group, g = r % a.group;
+  const int64_t at = b * a.out_batch + i * a.out_draft + ((int64_t)h * a.group + g) * a.out_head + d;
+  *reinterpret_cast<vec_any*>(static_cast<T*>(a.out) + at) = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
 }
 
 // Waves of a workgroup, with NT blocks of 16 rows in a wave.
@@ -143,38 +200,10 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
   const int q = lane >> 4, s = lane & 15;
   const int dh = a.c.head_dim, T = a.drafts;
 
-  // which unit this is
-  const Split split = plan(a, lane);
-  const int per_chunk = a.c.heads * a.row_blocks;  // units of a chunk
-  int64_t left = blockIdx.x;                       // units before this one, less those of the sequences before
-  int b = -1;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int64_t mine = 0;
-    if (b0 + lane < a.batch) mine = (int64_t)chunks_of(steps_of(a, b0 + lane), split) * per_chunk;
-    int64_t sum = mine;  // of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
-    }
-    const uint64_t there = __ballot(sum > left);
-    if (there) {
-      const int at = __builtin_ctzll(there);
-      b = b0 + at;
-      left -= __shfl(sum - mine, at);
-      break;
-    }
-    left -= __shfl(sum, 63);
-  }
-  if (b < 0) return;  // whole workgroup: past the last unit
-  b = uni(b);
-  const int in_seq = uni((int)left);
-  const int chunk = in_seq / per_chunk, rest = in_seq % per_chunk;
-  const int h = rest % a.c.heads, rb = rest / a.c.heads;
-  const int len = uni(min(max(a.lengths[b], 0), a.max_places));
-  const int steps = uni(steps_of(a, b)), n_chunks = uni(chunks_of(steps, split));
-  const int per = (steps + n_chunks - 1) / n_chunks;
-  const int step0 = chunk * per, step1 = min(steps, step0 + per);
+  Unit unit;
+  if (!find_unit(a, lane, unit)) return;  // whole workgroup: past the last one
+  const int b = unit.b, h = unit.h, rb = unit.rb, len = unit.len, n_chunks = unit.n_chunks;
+  const int step0 = unit.step0, step1 = unit.step1;
 
   const int rw = wv % a.row_waves, part = wv / a.row_waves, parts = W / a.row_waves;
   const int row0 = (rb * a.row_waves + rw) * 16 * NT;  // this wave's rows
@@ -486,26 +515,318 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
       continue;
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int i = r / a.group, g = r % a.group;
-    const int64_t at = b * a.out_batch + i * a.out_draft + ((int64_t)h * a.group + g) * a.out_head;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (VB * (4 * q + e) < dh)
 #pragma unroll
-        for (int j = 0; j < VB; j += 4) {
-          const f32x4 x = f32x4{acc[n][j][e], acc[n][j + 1][e], acc[n][j + 2][e], acc[n][j + 3][e]} * inv;
-          const int64_t to = at + VB * (4 * q + e) + j;
-          if constexpr (F32) {
-            *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.out) + to) = x;
-          } else {
-            typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-            typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
-            *reinterpret_cast<bf16x4_any*>(static_cast<__bf16*>(a.out) + to) =
-                bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-          }
-        }
+        for (int j = 0; j < VB; j += 4)
+          store_row4<typename std::conditional<F32, float, __bf16>::type>(
+              a, b, h, r, VB * (4 * q + e) + j,
+              f32x4{acc[n][j][e], acc[n][j + 1][e], acc[n][j + 2][e], acc[n][j + 3][e]} * inv);
     }
   }
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, const f32x16& sum) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0);
+}
+
+// Many rows (trees of drafted tokens): the matrix cores and the exponentials bound the call.  8 waves of 32 rows share
+// tiles of kTile places, which they widen to bf16 together, once: K to LDS place by place, V turned, so that a lane's eight
+// places of P^T are 16 bytes of a row of V^T.  With 128 rows or less, PARTS 2: pairs of waves have the same rows and half
+// of a tile's places each.  In LDS, rows of 128 bytes with their chunks swapped as staged tiles have them (K in D / 64
+// parts of 64 elements).  Products of 32 x 32: lane 32 hi + s holds
+//   of K and Q: row s, elements 8 hi .. + 7 of every 16;
+//   of S^T and O^T: for row s of Q, rows 8 i + 4 hi .. + 3, i < 4, of every 32.
+template <int D, bool E5M2, int PARTS>
+__global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) {
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int NB = D == 256 ? 1 : kTile / 32 / PARTS;  // blocks of 32 places at a time, as many as registers allow
+  constexpr int kBytes = kTile * D * 2;  // of K or of V in LDS
+  constexpr int REGS = 16 * DB + 2;      // of a wave's result
+  constexpr int kMerge = PARTS == 1 ? 0 : kTreeWaves / 2 * REGS * 256;
+  __shared__ __attribute__((aligned(16))) uint8_t tiles[4 * kBytes > kMerge ? 4 * kBytes : kMerge];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int hi = lane >> 5, s = lane & 31;
+  const int dh = a.c.head_dim, T = a.drafts;
+  Unit unit;
+  if (!find_unit(a, lane, unit)) return;  // whole workgroup: past the last one
+  const int b = unit.b, h = unit.h, len = unit.len;
+  const int rw = wv % (kTreeWaves / PARTS), part = wv / (kTreeWaves / PARTS);
+  const int row = (unit.rb * (kTreeWaves / PARTS) + rw) * 32 + s;  // this lane's
+
+  bf16x8 qf[KS];
+  const int draft = min(row, a.rows - 1) / a.group, in_group = min(row, a.rows - 1) % a.group;
+  uint64_t sees = a.masks ? (uint64_t)a.masks[b * a.mask_batch + draft] : ((uint64_t)2 << draft) - 1;
+  sees &= ~(uint64_t)0 >> (64 - T);
+  {
+    const __bf16* q = static_cast<const __bf16*>(a.q) + b * a.q_batch + draft * a.q_draft +
+                      ((int64_t)h * a.group + in_group) * a.q_head;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      Eight<__bf16> v;
+      v.clear();
+      const int d = 16 * k + 8 * hi;
+      if (d < dh && row < a.rows) v.load(q + d, 0, 8);
+      qf[k] = __builtin_bit_cast(bf16x8, v.w[0]);
+    }
+  }
+
+  // this thread's part of a tile on its way to LDS: D / 8 codes of K of place 8 wv + lane / 8; 4 places from 8 wv + 4 (lane
+  // / 32) on of V, VW words each
+  constexpr int KB = D / 8 < 16 ? 8 : 16, KN = D / 8 / KB, VW = D == 256 ? 2 : 1;
+  uint32_t kc[KN][KB / 4], vc[4][VW];
+  float ks;
+  f32x4 vs;
+  int ids = -1;  // lane l: page of group l % 4 of tile l / 4 of the current 16
+  uint32_t there_next = 0;
+  const int v_at = 4 * VW * (D == 64 ? lane & 15 : lane & 31);  // first element of V
+  const bool v_mine = D != 64 || (lane & 31) < 16;
+  const int count = unit.step1 - unit.step0;
+  auto load = [&](int i) {  // tile i of this unit, in order
+    if ((i & 15) == 0) {
+      const int64_t place = ((int64_t)unit.step0 + i + (lane >> 2)) * kTile + 16 * (lane & 3);
+      int id = -1;
+      if (place < len) id = a.table[b * a.table_ld + (place >> a.c.page_shift)];
+      ids = id >= 0 && id < a.c.pages ? id : -1;
+    }
+    there_next = (uint32_t)(__ballot(ids >= 0) >> (4 * (i & 15))) & 15u;
+    const int id = __builtin_amdgcn_readlane(ids, 4 * (i & 15) + (wv >> 1));
+    const int place = (unit.step0 + i) * kTile + 8 * wv;
+    // a group without a page reads page 0, to no use
+    const int in = (h << a.c.page_shift) + (id >= 0 ? place & (a.c.page - 1) : 8 * (wv & 1));
+    const int64_t page = id >= 0 ? id : 0;
+    const uint8_t* kp = a.c.k + page * a.c.code_page + (int64_t)in * dh;
+    const uint8_t* vp = a.c.v + page * a.c.code_page + (int64_t)in * dh;
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+      const int d = (lane & 7) * (D / 8) + KB * n;
+#pragma unroll
+      for (int w = 0; w < KB / 4; ++w) kc[n][w] = 0;
+      if (d < dh) {
+        typedef uint32_t words __attribute__((ext_vector_type(KB / 4)));
+        const words x = *reinterpret_cast<const words*>(kp + (lane >> 3) * dh + d);
+#pragma unroll
+        for (int w = 0; w < KB / 4; ++w) kc[n][w] = x[w];
+      }
+    }
+    ks = a.c.k_scale[page * a.c.scale_page + in + (lane >> 3)];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma unroll
+      for (int w = 0; w < VW; ++w) vc[e][w] = 0;
+      if (v_mine && v_at < dh) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(vp + (4 * hi + e) * dh + v_at);
+        if constexpr (VW == 1) {
+          vc[e][0] = *p;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          vc[e][0] = x.x, vc[e][1] = x.y;
+        }
+      }
+    }
+    vs = *reinterpret_cast<const f32x4*>(a.c.v_scale + page * a.c.scale_page + in + 4 * hi);
+  };
+  auto widen = [&](int i) {  // to LDS
+    uint8_t* kt = tiles + (i & 1) * 2 * kBytes;
+    uint8_t* vt = kt + kBytes;
+    const int place = 8 * wv + (lane >> 3), swz = stage_swz(place);
+#pragma unroll
+    for (int n = 0; n < KN; ++n)
+#pragma unroll
+      for (int w = 0; w < KB / 4; w += 2) {
+        const int chunk = ((lane & 7) * (D / 8) + KB * n) / 8 + w / 2;  // of 8 elements
+        *reinterpret_cast<u32x4*>(kt + (chunk >> 3) * kTile * 128 + 128 * place + 16 * ((chunk & 7) ^ swz)) =
+            u32x4{widen2<E5M2, false>(kc[n][w], ks), widen2<E5M2, true>(kc[n][w], ks),
+                  widen2<E5M2, false>(kc[n][w + 1], ks), widen2<E5M2, true>(kc[n][w + 1], ks)};
+      }
+    // places 16 g + 4 x .. + 3 go to half x / 2 of chunk 2 g + x % 2: a lane's eight places of P^T
+    const int four = 2 * wv + hi, chunk = 2 * (four >> 2) + (four & 1), half = 8 * (four >> 1 & 1);
+    if (v_mine) {
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+        uint32_t x[4][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[e][0] = widen2<E5M2, false>(vc[e][w], vs[e]);
+          x[e][1] = widen2<E5M2, true>(vc[e][w], vs[e]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+          const int d = v_at + 4 * w + j;
+          *reinterpret_cast<uint2*>(vt + 128 * d + 16 * (chunk ^ stage_swz(d)) + half) =
+              make_uint2(__builtin_amdgcn_perm(x[1][j >> 1], x[0][j >> 1], sel),
+                         __builtin_amdgcn_perm(x[3][j >> 1], x[2][j >> 1], sel));
+        }
+      }
+    }
+  };
+
+  f32x16 acc[DB];
+  f32x16 zero;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+#pragma unroll
+  for (int j = 0; j < DB; ++j) acc[j] = zero;
+  float top = kNone, total = 0.f;  // total: of the places that this lane holds
+  const float c_log2 = a.c_log2;
+
+  auto process = [&](int i, uint32_t there, int first) {  // the tile's places from `first` on
+    const uint8_t* kt = tiles + (i & 1) * 2 * kBytes;
+    const uint8_t* vt = kt + kBytes;
+    const int place = (unit.step0 + i) * kTile;
+    const bool edge = there != 15u || place + kTile > len - T;
+    f32x16 st[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) st[n] = zero;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+        st[n] = multiply32(__builtin_bit_cast(bf16x8, stage_chunk(kt + (k >> 2) * kTile * 128, first + 32 * n + s,
+                                                                  2 * (k & 3) + hi)),
+                           qf[k], st[n]);
+    uint32_t seen[NB];  // bit 4 i + e: row 8 i + 4 hi + e
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+        seen[n] = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          // four places from drafted token j on: ones before the first, zeros past the last
+          const int at = first + 32 * n + 8 * x + 4 * hi, j = place + at - (len - T);
+          const int before = min(max(-j, 0), 4);
+          const uint32_t of_tree = (uint32_t)(sees >> min(max(j, 0), 63)) << before | ((1u << before) - 1u);
+          const uint32_t four = (there >> (at >> 4) & 1u) & (uint32_t)(j < 64) ? of_tree & 15u : 0u;
+          seen[n] |= four << (4 * x);
+        }
+        f32x16 of_seen;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) of_seen[e] = seen[n] >> e & 1u ? st[n][e] : kNone;
+        st[n] = of_seen;
+      }
+    }
+    float m = st[0][0];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, st[n][e]);
+    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), top);
+    if (__ballot(m > top)) {
+      const float w = weight_of(top, m, c_log2);
+      total *= w;
+#pragma unroll
+      for (int j = 0; j < DB; ++j) acc[j] *= w;
+      top = m;
+    }
+    const float base = m == kNone ? 0.f : m * c_log2;
+    bf16x8 pf[2 * NB][2];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(st[n][8 * g + e], c_log2, -base));
+          total += p[e];
+        }
+        split8<2>(p, pf[2 * n + g]);
+      }
+#pragma unroll
+    for (int j = 0; j < DB; ++j) {
+#pragma unroll
+      for (int g = 0; g < 2 * NB; ++g) {
+        u32x4 v = stage_chunk(vt, 32 * j + s, 2 * (first / 16 + g) + hi);
+        if (edge) {
+          // Values that are not finite reach only the rows that see them: here they count as zeros, and whoever sees
+          // one gets NaN.
+          uint32_t bad[4], any = 0;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            bad[x] = ((v[x] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v[x] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+            any |= bad[x];
+          }
+          if (__ballot(any != 0)) {
+            u32x4 ones, who;
+            const uint32_t eight = seen[g >> 1] >> (8 * (g & 1));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              v[x] &= ~bad[x];
+              ones[x] = bad[x] & 0x3f803f80u;  // 1 in bf16
+              who[x] = (eight >> (2 * x) & 1u ? 0x3f80u : 0u) | (eight >> (2 * x + 1) & 1u ? 0x3f800000u : 0u);
+            }
+            const f32x16 n_bad = multiply32(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, who), zero);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[j][e] = n_bad[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[j][e];
+          }
+        }
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, v);
+        acc[j] = multiply32(vf, pf[g][1], acc[j]);
+        acc[j] = multiply32(vf, pf[g][0], acc[j]);
+      }
+    }
+  };
+
+  // Tile i + 1 is on its way to registers while tile i is multiplied, and goes to the other place in LDS, which every
+  // wave has read when it has passed the barrier.
+  if (count > 0) {
+    load(0);
+    widen(0);
+  }
+#pragma unroll 1
+  for (int i = 0; i < count; ++i) {
+    __syncthreads();
+    const uint32_t there = there_next;
+    if (i + 1 < count) load(i + 1);
+#pragma unroll 1
+    for (int first = part * (kTile / PARTS); first < (part + 1) * (kTile / PARTS); first += 32 * NB) process(i, there, first);
+    if (i + 1 < count) widen(i + 1);
+  }
+
+  if constexpr (PARTS == 2) {
+    float(*at)[64] = reinterpret_cast<float(*)[64]>(tiles) + rw * REGS;
+    __syncthreads();  // all tiles read
+    if (part == 1) {
+      at[0][lane] = top;
+      at[1][lane] = total;
+#pragma unroll
+      for (int j = 0; j < DB; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) at[2 + 16 * j + e][lane] = acc[j][e];
+    }
+    __syncthreads();
+    if (part == 1) return;
+    const float other = at[0][lane], m = fmaxf(top, other);
+    const float w0 = weight_of(top, m, c_log2), w1 = weight_of(other, m, c_log2);
+    top = m;
+    total = total * w0 + at[1][lane] * w1;
+#pragma unroll
+    for (int j = 0; j < DB; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[j][e] = acc[j][e] * w0 + at[2 + 16 * j + e][lane] * w1;
+  }
+  const float sum = total + __shfl_xor(total, 32);
+  if (row >= a.rows) return;
+  const float inv = unit.n_chunks > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  const int64_t at = (int64_t)blockIdx.x * (32 * (kTreeWaves / PARTS)) + 32 * rw + s;
+  if (unit.n_chunks > 1 && hi == 0) a.part_stat[at] = make_float2(top, sum);
+#pragma unroll
+  for (int j = 0; j < DB; ++j)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int d = 32 * j + 8 * x + 4 * hi;
+      if (d >= dh) continue;
+      const f32x4 o = f32x4{acc[j][4 * x], acc[j][4 * x + 1], acc[j][4 * x + 2], acc[j][4 * x + 3]} * inv;
+      if (unit.n_chunks > 1)
+        *reinterpret_cast<f32x4*>(a.part_out + at * dh + d) = o;
+      else
+        store_row4<__bf16>(a, b, h, row, d, o);
+    }
 }
 
 // Joins the chunks of a row, in order: a workgroup a row, groups of lanes every so many chunks, 4 elements a lane.
@@ -553,15 +874,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) 
     sum = sum * w0 + sums[o * lanes + l] * w1;
   }
   const f32x4 x = sum * (total == 0.f ? 0.f : 1.f / total);
-  const int64_t to = b * a.out_batch + i * a.out_draft + (int64_t)hq * a.out_head + 4 * l;
-  if constexpr (F32) {
-    *reinterpret_cast<f32x4_any*>(static_cast<float*>(a.out) + to) = x;
-  } else {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    typedef bf16x4 bf16x4_any __attribute__((aligned(2)));
-    *reinterpret_cast<bf16x4_any*>(static_cast<__bf16*>(a.out) + to) =
-        bf16x4{(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-  }
+  store_row4<typename std::conditional<F32, float, __bf16>::type>(a, b, h, r, 4 * l, x);
 }
 
 // ------------------------------------------------------------------ host side
@@ -569,7 +882,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) 
 using namespace sn;
 
 struct Way {
-  int nt;         // blocks of 16 rows in a wave
+  bool tree;      // tree_kernel
+  int nt;         // blocks of 16 rows in a wave of attend_kernel
   int unit_rows;  // rows of a workgroup
   int64_t units;  // at most
   int64_t slots;  // units that may write parts
@@ -579,6 +893,11 @@ struct Way {
 template <int D, bool E5M2, bool F32>
 void launch2(const AttendArgs& a, const Way& w, hipStream_t st) {
   const dim3 g((uint32_t)w.units);
+  if constexpr (!F32) {
+    if (w.tree)
+      return a.row_waves == kTreeWaves ? tree_kernel<D, E5M2, 1><<<g, 64 * kTreeWaves, 0, st>>>(a)
+                                       : tree_kernel<D, E5M2, 2><<<g, 64 * kTreeWaves, 0, st>>>(a);
+  }
   if (w.nt == 1) return attend_kernel<D, E5M2, F32, 1><<<g, 64 * waves_of(1), 0, st>>>(a);
   if constexpr (!(D == 256 && F32)) {
     if (w.nt == 2) return attend_kernel<D, E5M2, F32, 2><<<g, 64 * waves_of(2), 0, st>>>(a);
@@ -603,8 +922,8 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
   if (p->drafts < 1 || p->drafts > 64) return refuse(SN_EINVAL, "drafts must be in [1, 64]");
   if (p->q_heads < 1 || p->q_heads > 65536 || p->q_heads % a.c.heads)
     return refuse(SN_EINVAL, "q_heads must be a multiple of the cache's heads, 65536 at most");
-  if (p->table_cols < 0 || (int64_t)p->table_cols * a.c.page >= (int64_t(1) << 31) - kStep)
-    return refuse(SN_EINVAL, "table_cols must be >= 0, and table_cols * page below 2^31 - 32");
+  if (p->table_cols < 0 || (int64_t)p->table_cols * a.c.page >= (int64_t(1) << 31) - kTile)
+    return refuse(SN_EINVAL, "table_cols must be >= 0, and table_cols * page below 2^31 - 64");
   if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return refuse(SN_EINVAL, "scale must be finite and positive");
   constexpr int64_t kMost = int64_t(1) << 40;
   for (int64_t s : {p->q_batch, p->q_draft, p->q_head, p->out_batch, p->out_draft, p->out_head})
@@ -638,19 +957,30 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
   a.c_log2 = p->scale * 1.44269504088896340736f;
 
   const bool f32 = p->dtype == SN_F32;
-  const int most = a.c.head_dim > 128 ? (f32 ? 1 : 2) : f32 ? 2 : 4;
-  w.nt = a.rows <= 16 ? 1 : a.rows <= 32 ? std::min(2, most) : most;
-  const int waves = waves_of(w.nt), blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
-  a.row_waves = 1;
-  while (a.row_waves < waves && a.row_waves < blocks) a.row_waves *= 2;
-  w.unit_rows = 16 * w.nt * a.row_waves;
+  w.tree = !f32 && a.rows > 64;
+  if (w.tree) {
+    a.step = kTile;
+    a.row_waves = a.rows > 128 ? kTreeWaves : kTreeWaves / 2;
+    w.unit_rows = 32 * a.row_waves;
+    a.target = 256;
+    a.least = 4;
+  } else {
+    const int most = a.c.head_dim > 128 ? (f32 ? 1 : 2) : f32 ? 2 : 4;
+    w.nt = a.rows <= 16 ? 1 : a.rows <= 32 ? std::min(2, most) : most;
+    const int waves = waves_of(w.nt), blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
+    a.step = kStep;
+    a.row_waves = 1;
+    while (a.row_waves < waves && a.row_waves < blocks) a.row_waves *= 2;
+    w.unit_rows = 16 * w.nt * a.row_waves;
+    a.target = 1024;
+    a.least = 8;
+  }
+  const int waves = w.tree ? kTreeWaves : waves_of(w.nt);
   a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
-  a.target = 1024;
-  a.least = 8;
   const int64_t per_chunk = (int64_t)a.c.heads * a.row_blocks;
-  // a sequence has a chunk for every `per` of its steps and one more at most, and there are `least` steps to a chunk
-  const int64_t steps = ((int64_t)a.max_places + kStep - 1) / kStep;
-  const int64_t longest = std::max<int64_t>(1, (steps + a.least - 1) / a.least);
+  // a sequence has a chunk for every `per` of its steps and one more at most, and `per` is `least` at least
+  const int64_t steps = ((int64_t)a.max_places + a.step - 1) / a.step;
+  const int64_t longest = std::max<int64_t>(1, (steps + a.least / 2) / a.least);
   w.units = std::min((int64_t)a.batch * longest * per_chunk, a.target + (int64_t)a.batch * per_chunk);
   if (w.units * 64 * waves >= (int64_t(1) << 32) ||
       (int64_t)a.batch * a.drafts * p->q_heads * 256 >= (int64_t(1) << 32))

@@ -166,6 +166,154 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tile_kernel(IntArgs a) {
   }
 }
 
+// Large products: tiles of 256 x 256 by 8 waves of 128 x 64, two per SIMD.  A step is
+// a block of 128 columns, two stages of 64 KB in LDS.  A wave takes 64 rows of each half (128 rows) of A and 64 rows of B,
+// so a step falls into two phases of 64 x 64 (32 products of 16 x 16 x 64):
+//   phase           0                    1
+//   reads           A0, B                A1
+//   multiplies      A0 B                 A1 B
+//   requests        A1 of step k + 1     A0, B of step k + 2
+// A phase is a memory part and a product part with a bare barrier after each, and
+// waves 4-7 run half a phase behind waves 0-3, so on every SIMD one wave multiplies
+// while the other reads.
+// Nothing is read or refilled too early:
+//   - before the barrier that ends a memory part every wave waits until what the next phase reads has landed. That
+//     was requested two phases before it: since then 8 loads, of the two phases after, are outstanding at most;
+//   - a memory part ends with its reads complete, a barrier before any wave
+//     requests into their place.
+// Requests past the last step read nothing (an empty range) and keep the count.
+constexpr int kBT = 256;
+constexpr int kBHalf = 128 * 128;
+constexpr int kBStage = 4 * kBHalf;  // A0, A1, B
+
+template <typename TC>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) big_kernel(IntArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t stage[2 * kBStage];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int per_xcd = gridDim.x / 8;
+  const int tile = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (tile >= a.tiles_m * a.tiles_n) return;  // whole workgroup
+  int64_t bm, bn;
+  place(tile, a.tiles_m, a.tiles_n, bm, bn);
+
+  // this wave stages rows 16 wv .. + 15 of every 128
+  const uint8_t* base[4];
+  uint32_t len[4];
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int64_t row = (h < 2 ? bm : bn) * kBT + 128 * (h & 1) + 16 * wv;
+    base[h] = h < 2 ? a.a + row * a.ld_a : a.b + row * a.ld_b;
+    len[h] = range_bytes(row, h < 2 ? a.m : a.n, 16, h < 2 ? a.ld_a : a.ld_b, a.k);
+  }
+  const uint32_t rb[2] = {(uint32_t)a.ld_a, (uint32_t)a.ld_b};
+  const int n_k = (int)((a.k + 127) / 128), n_full = (int)(a.k / 128);
+  const int sr = lane >> 3, p = lane & 7;
+  uint32_t voff[2][2];  // operand, row group of 8
+#pragma unroll
+  for (int o = 0; o < 2; ++o)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      voff[o][j] = (uint32_t)sr * rb[o] + 16u * (uint32_t)(p ^ stage_swz(16 * wv + 8 * j + sr));
+  auto issue = [&](int h, int k) {  // this wave's part of half tile h of step k
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base[h], k < n_k ? len[h] : 0u);
+    uint8_t* dst = stage + (k & 1) * kBStage + h * kBHalf + 2048 * wv;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst + 1024 * j), 16, voff[h >> 1][j],
+                                               8u * j * rb[h >> 1] + 128u * (uint32_t)k, 0, 0);
+  };
+  enum { A0 = 0, A1 = 1, B0 = 2, B1 = 3 };
+
+  const int wm = wv >> 2, wn = wv & 3;  // 64 rows of each A half from 64 wm, of B from 64 wn
+  i32x4 acc[8][4];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+  u32x4 fa[4][2], fb[4][2];  // [16 rows][half of the block's columns]
+  auto read = [&](u32x4 (&f)[4][2], int k, int row) {
+    const uint8_t* src = stage + (k & 1) * kBStage + 128 * row;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) f[r][c] = stage_chunk(src, 16 * r + s, 4 * c + q);
+  };
+  // zeroes columns >= k of operands of the ragged step
+  auto mask = [&](u32x4 (&f)[4][2]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int keep = (int)(a.k - (int64_t)n_full * 128) - 16 * (4 * c + q);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) keep_chunk(f[r][c], keep);
+    }
+  };
+  auto products = [&](int i0) {
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i0 + i][j] = multiply64(fb[j][c], fa[i][c], acc[i0 + i][j]);
+    __builtin_amdgcn_s_setprio(0);
+  };
+  auto request = [&](int k) {
+    issue(A0, k);
+    issue(B0, k);
+    issue(B1, k);
+  };
+  auto step = [&](int k, auto ragged_tag) {
+    constexpr bool RAGGED = decltype(ragged_tag)::value;
+    // phase 0
+    read(fa, k, 64 * wm);
+    read(fb, k, 256 + 64 * wn);
+    issue(A1, k + 1);
+    wait_loads<8>();
+    bare_barrier();
+    if constexpr (RAGGED) {
+      mask(fa);
+      mask(fb);
+    }
+    products(0);
+    bare_barrier();
+    // phase 1
+    read(fa, k, 128 + 64 * wm);
+    request(k + 2);
+    wait_loads<8>();
+    bare_barrier();
+    if constexpr (RAGGED) mask(fa);
+    products(4);
+    bare_barrier();
+  };
+  request(0);
+  issue(A1, 0);
+  request(1);
+  wait_loads<8>();  // what phase 0 of step 0 reads
+  bare_barrier();
+  if (wm == 1) bare_barrier();  // waves 4-7: half a phase behind
+#pragma unroll 1
+  for (int k = 0; k < n_full; ++k) step(k, std::false_type{});
+  if (n_full < n_k) step(n_full, std::true_type{});
+  if (wm == 0) bare_barrier();
+  wait_loads<0>();  // the last loads have left the LDS alone before the workgroup gives it up
+
+  // lane: row 128 (i / 4) + 64 wm + 16 (i % 4) + s, columns 64 wn + 16 j + 4 q .. + 3
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int64_t n = bn * kBT + 64 * wn + 16 * j + 4 * q;
+    if (n >= a.n) continue;
+    Scale sb[4];
+    column_scales(a, n, sb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t m = bm * kBT + 128 * (i >> 2) + 64 * wm + 16 * (i & 3) + s;
+      if (m < a.m) finish4<TC>(a, m, n, acc[i][j], scale_of(a.sa + m * a.sa_row), sb);
+    }
+  }
+}
+
 // Adds the parts of C.
 template <typename TC>
 __global__ void __launch_bounds__(256) join_kernel(IntArgs a) {
@@ -350,7 +498,9 @@ struct Run {
 
 void launch_tiles(const IntArgs& a, const Run& run, hipStream_t st) {
   const dim3 g((uint32_t)run.workgroups);
-  if (run.kernel == SN_MATMUL_TILE_8)
+  if (run.kernel == SN_MATMUL_BIG)
+    a.c_bf16 ? big_kernel<__bf16><<<g, 512, 0, st>>>(a) : big_kernel<float><<<g, 512, 0, st>>>(a);
+  else if (run.kernel == SN_MATMUL_TILE_8)
     a.c_bf16 ? tile_kernel<__bf16, 8><<<g, 512, 0, st>>>(a) : tile_kernel<float, 8><<<g, 512, 0, st>>>(a);
   else
     a.c_bf16 ? tile_kernel<__bf16, 4><<<g, 256, 0, st>>>(a) : tile_kernel<float, 4><<<g, 256, 0, st>>>(a);
@@ -442,6 +592,14 @@ int resolve(sn_matmul_int8& p, Plan& pl) {
   }
   pl.tiles_m = (int32_t)((p.m + kT - 1) / kT);
   pl.tiles_n = (int32_t)((p.n + kT - 1) / kT);
+  const int64_t large = ((p.m + kBT - 1) / kBT) * ((p.n + kBT - 1) / kBT);
+  if (large >= 256 && p.k > 0) {
+    pl.tiles_m = (int32_t)((p.m + kBT - 1) / kBT);
+    pl.tiles_n = (int32_t)((p.n + kBT - 1) / kBT);
+    pl.blocks_per_split = (int32_t)n_kb;
+    pl.run = Run{SN_MATMUL_BIG, 512, (large + 7) / 8 * 8};
+    return SN_OK;
+  }
   int64_t splits = 1;
   while (splits < 16 && 2 * splits * small <= 256 && 4 * splits <= n_kb) splits *= 2;
   pl.blocks_per_split = (int32_t)((n_kb + splits - 1) / splits);

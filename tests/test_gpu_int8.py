@@ -159,7 +159,7 @@ def test_every_kernel_is_tested():
     """The sizes above reach every kernel, and sums in parts."""
     seen = {spectral_matmul_int8_kernel(sn_matmul_int8(*size, SN_I8, CODE[out]))[:2] for size in PRODUCTS + LARGE + WIDE
             for out in ("f32", "bf16")}
-    assert {name for name, _ in seen} >= {"few_rows", "tile_4", "tile_8"} and any(parts > 1 for _, parts in seen)
+    assert {name for name, _ in seen} >= {"few_rows", "tile_4", "tile_8", "big"} and any(parts > 1 for _, parts in seen)
 
 
 WIDE = [(8200, 8300, k) for k in (1, 100, 128, 129, 256, 300, 512, 600)]
