@@ -502,7 +502,7 @@ typedef struct {
   int32_t batch;       /* 0 .. 2^20                                                  */
   int32_t drafts;      /* 1 .. 64 tokens of each sequence                            */
   int32_t q_heads;     /* a multiple of the cache's heads                            */
-  int32_t table_cols;  /* pages of the longest sequence; times page below 2^31 - 64  */
+  int32_t table_cols;  /* pages of the longest sequence; times page below 2^31 - 128 */
   float scale;         /* finite, positive                                           */
   int64_t q_batch, q_draft, q_head;
   int64_t out_batch, out_draft, out_head;

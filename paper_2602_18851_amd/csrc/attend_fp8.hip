@@ -21,6 +21,7 @@
 #include "cache_fp8.h"
 #include "device_util.h"
 #include "fp8_device.h"
+#include "tile_device.h"
 
 namespace {
 
@@ -28,7 +29,6 @@ using namespace sn_dev;
 using sn::CacheView;
 
 constexpr int kStep = 32;   // places that a wave of attend_kernel takes at a time
-constexpr int kTile = 64;   // places that a workgroup of tree_kernel takes at a time
 constexpr int kTreeWaves = 8;
 
 struct AttendArgs {
@@ -42,7 +42,7 @@ struct AttendArgs {
   const int64_t* masks;  // or NULL: a drafted token sees those before it and itself
   int64_t mask_batch;
   int32_t batch, drafts, group, rows;  // rows = drafts * group, of a key head
-  int32_t max_places, step;  // step: kStep or kTile
+  int32_t max_places, step;  // step: places that go together
   int32_t row_waves, row_blocks;  // waves of a workgroup with rows of their own, and workgroups that share a key head's rows
   int32_t target, least;          // workgroups to aim at, and the least steps of one
   float c_log2;                   // scale * log2(e)
@@ -127,21 +127,25 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int lane, Unit& u
 
 __device__ __forceinline__ uint32_t bits(__bf16 x) { return __builtin_bit_cast(uint16_t, x); }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 // The bf16 parts of eight values, the nearest first.
 template <int PARTS>
 __device__ __forceinline__ void split8(const float (&x)[8], bf16x8 (&part)[PARTS]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float rest = x[e];
+  for (int e = 0; e < 8; e += 2) {
+    f32x2 rest = {x[e], x[e + 1]};
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      part[p][e] = (__bf16)rest;
-      if (p + 1 < PARTS) rest -= (float)part[p][e];
+      const bf16x2 near = __builtin_convertvector(rest, bf16x2);
+      part[p][e] = near[0];
+      part[p][e + 1] = near[1];
+      const uint32_t w = __builtin_bit_cast(uint32_t, near);
+      if (p + 1 < PARTS) rest = f32x2{rest[0] - __uint_as_float(w << 16), rest[1] - __uint_as_float(w & 0xffff0000u)};
     }
   }
 }
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Codes 0, 1 or 2, 3 of a word, times 2^e of the scale, as bf16.
 template <bool E5M2, bool HIGH>
@@ -534,20 +538,34 @@ __device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, c
 }
 
 // Many rows (trees of drafted tokens): the matrix cores and the exponentials bound the call.  8 waves of 32 rows share
-// tiles of kTile places, which they widen to bf16 together, once: K to LDS place by place, V turned, so that a lane's eight
+// tiles of 8192 / D places, which they widen to bf16 together, once: K to LDS place by place, V turned, so that a lane's eight
 // places of P^T are 16 bytes of a row of V^T.  With 128 rows or less, PARTS 2: pairs of waves have the same rows and half
-// of a tile's places each.  In LDS, rows of 128 bytes with their chunks swapped as staged tiles have them (K in D / 64
-// parts of 64 elements).  Products of 32 x 32: lane 32 hi + s holds
+// of a tile's places each.  Products of 32 x 32: lane 32 hi + s holds
 //   of K and Q: row s, elements 8 hi .. + 7 of every 16;
 //   of S^T and O^T: for row s of Q, rows 8 i + 4 hi .. + 3, i < 4, of every 32.
+// A wave takes half a tile at a time, a step: with PARTS 1 one half after the other, with PARTS 2 its own.  A step falls into
+// a part on the matrix cores, O += P V of step k - 1 and S of step k, and one on the vector units, P of step k, with a bare
+// barrier after each, and waves 4-7 run one part behind waves 0-3: on every SIMD one wave multiplies while the other
+// exponentiates.  With the vector part goes a share of a tile to LDS, where K and V have two places each.  Counting
+// parts, waves 0-3 multiply step k in part 2 k, waves 4-7 in part 2 k + 1.  PARTS 1: K of tile i + 1 is first read in
+// part 4 i + 4, K of i - 1 last in 4 i - 1; V of tile i first in 4 i + 2, V of i - 2 last in 4 i - 3.  Waves 0-3 write V of tile i
+// with step 2 i and K of i + 1 with 2 i + 1, in parts 4 i + 1 and 4 i + 3; waves 4-7, a tile ahead, V of i + 1 and K of
+// i + 2 in the same steps, parts 4 i + 2 and 4 i + 4.  PARTS 2, both with each step: K of i + 1 and V of i are first
+// read in 2 i + 2, K of i - 1 and V of i - 2 last in 2 i - 1, and written in 2 i + 1 and 2 i.  Tiles past the last are
+// loaded and written too, to no use, so that no load in flight meets a branch: the compiler would wait for all of them there.
+constexpr int tile_of(int d) { return 8192 / d; }
+
 template <int D, bool E5M2, int PARTS>
 __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) {
-  constexpr int KS = D / 16, DB = D / 32;
-  constexpr int NB = D == 256 ? 1 : kTile / 32 / PARTS;  // blocks of 32 places at a time, as many as registers allow
+  constexpr int kTile = tile_of(D), kGroups = kTile / 16;
+  constexpr int KS = D / 16, DB = D / 32, NB = kTile / 64;
   constexpr int kBytes = kTile * D * 2;  // of K or of V in LDS
   constexpr int REGS = 16 * DB + 2;      // of a wave's result
   constexpr int kMerge = PARTS == 1 ? 0 : kTreeWaves / 2 * REGS * 256;
-  __shared__ __attribute__((aligned(16))) uint8_t tiles[4 * kBytes > kMerge ? 4 * kBytes : kMerge];
+  __shared__ __attribute__((aligned(16))) uint8_t tiles[4 * kBytes > kMerge ? 4 * kBytes : kMerge];  // K, K, V, V
+  // which values of a tile that not all rows see are not finite (in LDS they are zeros): of places 4 f .. + 3 and elements
+  // 4 g .. + 3, bit 4 place + element of word [f][g]
+  __shared__ uint16_t bad[2][kTile * D / 16];
   const int lane = threadIdx.x & 63;
   const int wv = uni((int)(threadIdx.x >> 6));
   const int hi = lane >> 5, s = lane & 31;
@@ -555,7 +573,7 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
   Unit unit;
   if (!find_unit(a, lane, unit)) return;  // whole workgroup: past the last one
   const int b = unit.b, h = unit.h, len = unit.len;
-  const int rw = wv % (kTreeWaves / PARTS), part = wv / (kTreeWaves / PARTS);
+  const int rw = wv % (kTreeWaves / PARTS), part = PARTS == 1 ? 0 : wv / (kTreeWaves / PARTS);
   const int row = (unit.rb * (kTreeWaves / PARTS) + rw) * 32 + s;  // this lane's
 
   bf16x8 qf[KS];
@@ -575,122 +593,158 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     }
   }
 
-  // this thread's part of a tile on its way to LDS: D / 8 codes of K of place 8 wv + lane / 8; 4 places from 8 wv + 4 (lane
-  // / 32) on of V, VW words each
-  constexpr int KB = D / 8 < 16 ? 8 : 16, KN = D / 8 / KB, VW = D == 256 ? 2 : 1;
-  uint32_t kc[KN][KB / 4], vc[4][VW];
+  // Pages: lane l holds that of group l % kGroups of tile l / kGroups of a window of tiles, the current one, the one
+  // before (of which V and P are still to come) and the next.
+  constexpr int kWindow = 64 / kGroups;
+  const int count = unit.step1 - unit.step0;
+  auto pages_of = [&](int window) {
+    const int64_t place = ((int64_t)unit.step0 + window * kWindow) * kTile + 16 * lane;
+    int id = -1;
+    if (place < len) id = a.table[b * a.table_ld + (place >> a.c.page_shift)];
+    return id >= 0 && id < a.c.pages ? id : -1;
+  };
+  int window = 0, ids_before = -1, ids = pages_of(0), ids_next = pages_of(1);
+  // this wave's share of a tile: kTile / 8 places, in one group
+  constexpr int kShare = kTile / 8;
+  auto locate = [&](int i, int64_t& page, int& in) {
+    const int at = kGroups * (i % kWindow) + wv * kShare / 16;
+    const int id = i / kWindow == window ? __builtin_amdgcn_readlane(ids, at) : __builtin_amdgcn_readlane(ids_before, at);
+    // a group without a page reads page 0, to no use
+    const int place = (int)((uint32_t)(unit.step0 + i) * kTile) + kShare * wv;
+    in = (h << a.c.page_shift) + (id >= 0 ? place & (a.c.page - 1) : kShare * wv & 15);
+    page = id >= 0 ? id : 0;
+  };
+  auto there_of = [&](int i) {  // bit g: group g of tile i has a page
+    const uint64_t all = i / kWindow == window ? __ballot(ids >= 0) : __ballot(ids_before >= 0);
+    return (uint32_t)(all >> (kGroups * (i % kWindow))) & ((1u << kGroups) - 1u);
+  };
+  auto edge_of = [&](int i) {  // whether not all rows see all of tile i
+    return there_of(i) != (1u << kGroups) - 1u || (int64_t)(unit.step0 + i + 1) * kTile > len - T;
+  };
+  // 16 codes of K of one place, 4 of V of each of 4 places, on their way to LDS
+  u32x4 kc;
+  uint32_t vc[4];
   float ks;
   f32x4 vs;
-  int ids = -1;  // lane l: page of group l % 4 of tile l / 4 of the current 16
-  uint32_t there_next = 0;
-  const int v_at = 4 * VW * (D == 64 ? lane & 15 : lane & 31);  // first element of V
-  const bool v_mine = D != 64 || (lane & 31) < 16;
-  const int count = unit.step1 - unit.step0;
-  auto load = [&](int i) {  // tile i of this unit, in order
-    if ((i & 15) == 0) {
-      const int64_t place = ((int64_t)unit.step0 + i + (lane >> 2)) * kTile + 16 * (lane & 3);
-      int id = -1;
-      if (place < len) id = a.table[b * a.table_ld + (place >> a.c.page_shift)];
-      ids = id >= 0 && id < a.c.pages ? id : -1;
+  constexpr int KL = D / 16, VL = D / 4;  // lanes of a place, of four places
+  const int k_place = lane / KL, k_at = 16 * (lane % KL), v_four = lane / VL, v_at = 4 * (lane % VL);
+  // byte offsets from the share's first place; elements from head_dim on are out of range and read zeros
+  constexpr uint32_t kNowhere = 0x80000000u;
+  const uint32_t k_off = k_at < dh ? (uint32_t)(k_place * dh + k_at) : kNowhere;
+  const uint32_t v_off = v_at < dh ? (uint32_t)(4 * v_four * dh + v_at) : kNowhere;
+  auto from = [](const void* p) { return make_rsrc(p, 0x7fffffffu); };
+  auto load_k = [&](int i) {  // in order
+    if (i / kWindow != window) {
+      ++window;
+      ids_before = ids;
+      ids = ids_next;
+      ids_next = pages_of(window + 1);
     }
-    there_next = (uint32_t)(__ballot(ids >= 0) >> (4 * (i & 15))) & 15u;
-    const int id = __builtin_amdgcn_readlane(ids, 4 * (i & 15) + (wv >> 1));
-    const int place = (unit.step0 + i) * kTile + 8 * wv;
-    // a group without a page reads page 0, to no use
-    const int in = (h << a.c.page_shift) + (id >= 0 ? place & (a.c.page - 1) : 8 * (wv & 1));
-    const int64_t page = id >= 0 ? id : 0;
-    const uint8_t* kp = a.c.k + page * a.c.code_page + (int64_t)in * dh;
-    const uint8_t* vp = a.c.v + page * a.c.code_page + (int64_t)in * dh;
+    int64_t page;
+    int in;
+    locate(i, page, in);
+    kc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                       from(a.c.k + page * a.c.code_page + (int64_t)in * dh), k_off, 0, 0));
+    ks = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from(a.c.k_scale + page * a.c.scale_page + in),
+                                                              4u * (uint32_t)k_place, 0, 0));
+  };
+  auto load_v = [&](int i) {
+    int64_t page;
+    int in;
+    locate(i, page, in);
+    const __amdgpu_buffer_rsrc_t r = from(a.c.v + page * a.c.code_page + (int64_t)in * dh);
 #pragma unroll
-    for (int n = 0; n < KN; ++n) {
-      const int d = (lane & 7) * (D / 8) + KB * n;
+    for (int e = 0; e < 4; ++e) vc[e] = __builtin_amdgcn_raw_buffer_load_b32(r, v_off, (uint32_t)(e * dh), 0);
+    vs = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                       from(a.c.v_scale + page * a.c.scale_page + in), 16u * (uint32_t)v_four, 0, 0));
+  };
+  // In LDS, rows of 128 bytes with their chunks of 16 swapped as staged tiles have them: K in parts of 64 elements, V^T in
+  // parts of 64 places.
+  auto k_chunk = [&](int i, int place, int chunk) {
+    return tiles + (i & 1) * kBytes + (chunk >> 3) * kTile * 128 + 128 * place + 16 * ((chunk & 7) ^ stage_swz(place));
+  };
+  auto v_chunk = [&](int i, int d, int chunk) {
+    return tiles + (2 + (i & 1)) * kBytes + (chunk >> 3) * D * 128 + 128 * d + 16 * ((chunk & 7) ^ stage_swz(d));
+  };
+  // Where this lane reads chunk 2 c + hi of 8 of row s of a block of 32 rows (the swaps repeat every 32 rows)
+  int at_chunk[4];
 #pragma unroll
-      for (int w = 0; w < KB / 4; ++w) kc[n][w] = 0;
-      if (d < dh) {
-        typedef uint32_t words __attribute__((ext_vector_type(KB / 4)));
-        const words x = *reinterpret_cast<const words*>(kp + (lane >> 3) * dh + d);
+  for (int c = 0; c < 4; ++c) at_chunk[c] = 128 * s + 16 * ((2 * c + hi) ^ stage_swz(s));
+  auto widen_k = [&](int i) {
 #pragma unroll
-        for (int w = 0; w < KB / 4; ++w) kc[n][w] = x[w];
-      }
-    }
-    ks = a.c.k_scale[page * a.c.scale_page + in + (lane >> 3)];
+    for (int w = 0; w < 4; w += 2)
+      *reinterpret_cast<u32x4*>(k_chunk(i, kShare * wv + k_place, k_at / 8 + w / 2)) =
+          u32x4{widen2<E5M2, false>(kc[w], ks), widen2<E5M2, true>(kc[w], ks), widen2<E5M2, false>(kc[w + 1], ks),
+                widen2<E5M2, true>(kc[w + 1], ks)};
+  };
+  auto widen_v = [&](int i) {
+    uint32_t x[4][2];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-#pragma unroll
-      for (int w = 0; w < VW; ++w) vc[e][w] = 0;
-      if (v_mine && v_at < dh) {
-        const uint32_t* p = reinterpret_cast<const uint32_t*>(vp + (4 * hi + e) * dh + v_at);
-        if constexpr (VW == 1) {
-          vc[e][0] = *p;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(p);
-          vc[e][0] = x.x, vc[e][1] = x.y;
-        }
-      }
+      x[e][0] = widen2<E5M2, false>(vc[e], vs[e]);
+      x[e][1] = widen2<E5M2, true>(vc[e], vs[e]);
     }
-    vs = *reinterpret_cast<const f32x4*>(a.c.v_scale + page * a.c.scale_page + in + 4 * hi);
+    if (edge_of(i)) {
+      uint32_t word = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t lo = (x[e][y] & 0x7f80u) == 0x7f80u, up = (x[e][y] & 0x7f800000u) == 0x7f800000u;
+          word |= (lo | up << 1) << (4 * e + 2 * y);
+          x[e][y] &= (lo ? 0u : 0xffffu) | (up ? 0u : 0xffff0000u);
+        }
+      bad[i & 1][(kShare / 4 * wv + v_four) * (D / 4) + v_at / 4] = (uint16_t)word;
+    }
+    // places 16 g + 4 y .. + 3 go to half y / 2 of chunk 2 g + y % 2: a lane's eight places of P^T
+    const int four = kShare / 4 * wv + v_four;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
+      *reinterpret_cast<uint2*>(v_chunk(i, v_at + j, 2 * (four >> 2) + (four & 1)) + 8 * (four >> 1 & 1)) =
+          make_uint2(__builtin_amdgcn_perm(x[1][j >> 1], x[0][j >> 1], sel),
+                     __builtin_amdgcn_perm(x[3][j >> 1], x[2][j >> 1], sel));
+    }
   };
-  auto widen = [&](int i) {  // to LDS
-    uint8_t* kt = tiles + (i & 1) * 2 * kBytes;
-    uint8_t* vt = kt + kBytes;
-    const int place = 8 * wv + (lane >> 3), swz = stage_swz(place);
-#pragma unroll
-    for (int n = 0; n < KN; ++n)
-#pragma unroll
-      for (int w = 0; w < KB / 4; w += 2) {
-        const int chunk = ((lane & 7) * (D / 8) + KB * n) / 8 + w / 2;  // of 8 elements
-        *reinterpret_cast<u32x4*>(kt + (chunk >> 3) * kTile * 128 + 128 * place + 16 * ((chunk & 7) ^ swz)) =
-            u32x4{widen2<E5M2, false>(kc[n][w], ks), widen2<E5M2, true>(kc[n][w], ks),
-                  widen2<E5M2, false>(kc[n][w + 1], ks), widen2<E5M2, true>(kc[n][w + 1], ks)};
-      }
-    // places 16 g + 4 x .. + 3 go to half x / 2 of chunk 2 g + x % 2: a lane's eight places of P^T
-    const int four = 2 * wv + hi, chunk = 2 * (four >> 2) + (four & 1), half = 8 * (four >> 1 & 1);
-    if (v_mine) {
-#pragma unroll
-      for (int w = 0; w < VW; ++w) {
-        uint32_t x[4][2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e][0] = widen2<E5M2, false>(vc[e][w], vs[e]);
-          x[e][1] = widen2<E5M2, true>(vc[e][w], vs[e]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
-          const int d = v_at + 4 * w + j;
-          *reinterpret_cast<uint2*>(vt + 128 * d + 16 * (chunk ^ stage_swz(d)) + half) =
-              make_uint2(__builtin_amdgcn_perm(x[1][j >> 1], x[0][j >> 1], sel),
-                         __builtin_amdgcn_perm(x[3][j >> 1], x[2][j >> 1], sel));
-        }
-      }
-    }
+  auto fill_k = [&](int i) {
+    widen_k(i);
+    load_k(i + 1);
+  };
+  auto fill_v = [&](int i) {
+    widen_v(i);
+    load_v(i + 1);
   };
 
-  f32x16 acc[DB];
-  f32x16 zero;
+  f32x16 acc[DB], zero;
 #pragma unroll
   for (int e = 0; e < 16; ++e) zero[e] = 0.f;
 #pragma unroll
   for (int j = 0; j < DB; ++j) acc[j] = zero;
   float top = kNone, total = 0.f;  // total: of the places that this lane holds
   const float c_log2 = a.c_log2;
+  f32x16 st[NB];
+  bf16x8 pf[2 * NB][2];
+  uint32_t seen[NB];  // bit 4 i + e: row 8 i + 4 hi + e
+  bool edge = false;  // of the tile whose P this wave holds
 
-  auto process = [&](int i, uint32_t there, int first) {  // the tile's places from `first` on
-    const uint8_t* kt = tiles + (i & 1) * 2 * kBytes;
-    const uint8_t* vt = kt + kBytes;
-    const int place = (unit.step0 + i) * kTile;
-    const bool edge = there != 15u || place + kTile > len - T;
-    f32x16 st[NB];
+  auto tile = [](int k) { return PARTS == 1 ? k >> 1 : k; };
+  auto half = [&](int k) { return PARTS == 1 ? k & 1 : part; };
+  auto scores = [&](int k) {
+    const uint8_t* kt = tiles + (tile(k) & 1) * kBytes + half(k) * 32 * NB * 128;
 #pragma unroll
     for (int n = 0; n < NB; ++n) st[n] = zero;
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
+    for (int c = 0; c < KS; ++c) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
-        st[n] = multiply32(__builtin_bit_cast(bf16x8, stage_chunk(kt + (k >> 2) * kTile * 128, first + 32 * n + s,
-                                                                  2 * (k & 3) + hi)),
-                           qf[k], st[n]);
-    uint32_t seen[NB];  // bit 4 i + e: row 8 i + 4 hi + e
+        st[n] = multiply32(*reinterpret_cast<const bf16x8*>(kt + ((c >> 2) * kTile + 32 * n) * 128 + at_chunk[c & 3]),
+                           qf[c], st[n]);
+    }
+  };
+  auto weights = [&](int k) {
+    const int i = tile(k), first = half(k) * 32 * NB, place = (unit.step0 + i) * kTile;
+    const uint32_t there = there_of(i);
+    edge = edge_of(i);
     if (edge) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -708,6 +762,7 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
 #pragma unroll
         for (int e = 0; e < 16; ++e) of_seen[e] = seen[n] >> e & 1u ? st[n][e] : kNone;
         st[n] = of_seen;
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     float m = st[0][0];
@@ -724,7 +779,6 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
       top = m;
     }
     const float base = m == kNone ? 0.f : m * c_log2;
-    bf16x8 pf[2 * NB][2];
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -736,56 +790,99 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
           total += p[e];
         }
         split8<2>(p, pf[2 * n + g]);
+        __builtin_amdgcn_sched_barrier(0);
       }
+  };
+  auto values = [&](int k) {
+    const int u = half(k);
+    const uint8_t* v = tiles + (2 + (tile(k) & 1)) * kBytes + (NB == 2 ? u * D * 128 : 0);
 #pragma unroll
-    for (int j = 0; j < DB; ++j) {
+    for (int g = 0; g < 2 * NB; ++g) {
+      const int at = at_chunk[g] ^ (NB == 1 ? 64 * u : 0);  // chunk 4 u + 2 g + hi
 #pragma unroll
-      for (int g = 0; g < 2 * NB; ++g) {
-        u32x4 v = stage_chunk(vt, 32 * j + s, 2 * (first / 16 + g) + hi);
-        if (edge) {
-          // Values that are not finite reach only the rows that see them: here they count as zeros, and whoever sees
-          // one gets NaN.
-          uint32_t bad[4], any = 0;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            bad[x] = ((v[x] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v[x] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-            any |= bad[x];
-          }
-          if (__ballot(any != 0)) {
-            u32x4 ones, who;
-            const uint32_t eight = seen[g >> 1] >> (8 * (g & 1));
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              v[x] &= ~bad[x];
-              ones[x] = bad[x] & 0x3f803f80u;  // 1 in bf16
-              who[x] = (eight >> (2 * x) & 1u ? 0x3f80u : 0u) | (eight >> (2 * x + 1) & 1u ? 0x3f800000u : 0u);
-            }
-            const f32x16 n_bad = multiply32(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, who), zero);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[j][e] = n_bad[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[j][e];
-          }
-        }
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, v);
+      for (int j = 0; j < DB; ++j) {
+        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(v + 32 * j * 128 + at);
         acc[j] = multiply32(vf, pf[g][1], acc[j]);
         acc[j] = multiply32(vf, pf[g][0], acc[j]);
       }
     }
   };
+  // Whoever sees a value that is not finite gets NaN (tiles that not all rows see; hardly ever any).
+  auto poison = [&](int k) {
+    const int i = tile(k), first = half(k) * 32 * NB;
+    uint32_t any = 0;
+    for (int n = lane; n < kTile * D / 32; n += 64) any |= reinterpret_cast<const uint32_t*>(bad[i & 1])[n];
+    if (__ballot(any != 0) == 0) return;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      const uint32_t other = (uint32_t)__shfl_xor((int)seen[n], 32);  // the other places of the row
+#pragma unroll 1
+      for (int y = 0; y < 8; ++y) {  // places 4 y .. + 3 of the 32
+        const uint32_t four = ((y & 1) == hi ? seen[n] : other) >> (4 * (y >> 1)) & 15u;
+        const uint32_t mask = (four & 1u ? 0x000fu : 0u) | (four & 2u ? 0x00f0u : 0u) | (four & 4u ? 0x0f00u : 0u) |
+                              (four & 8u ? 0xf000u : 0u);
+        const uint16_t* at = bad[i & 1] + (first / 4 + 8 * n + y) * (D / 4) + hi;
+#pragma unroll
+        for (int j = 0; j < DB; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            uint32_t hit = at[8 * j + 2 * x] & mask;
+            hit |= hit >> 8;
+            hit |= hit >> 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[j][4 * x + e] = hit >> e & 1u ? __uint_as_float(0x7fc00000u) : acc[j][4 * x + e];
+          }
+      }
+    }
+  };
+  auto meet = [&]() {
+    wait_loads<63>();  // what this wave has written to LDS
+    bare_barrier();
+  };
 
-  // Tile i + 1 is on its way to registers while tile i is multiplied, and goes to the other place in LDS, which every
-  // wave has read when it has passed the barrier.
   if (count > 0) {
-    load(0);
-    widen(0);
-  }
+    const int behind = wv >> 2;
+    load_k(0);
+    widen_k(0);
+    load_k(1);
+    load_v(0);
+    meet();
+    if (behind) {
+      fill_v(0);
+      fill_k(1);
+      meet();
+    }
+    scores(0);
+    meet();
+    auto multiply_part = [&](int k) {
+      __builtin_amdgcn_s_setprio(1);
+      values(k);
+      if (edge) poison(k);
+      scores(k + 1);
+      __builtin_amdgcn_s_setprio(0);
+      meet();
+    };
 #pragma unroll 1
-  for (int i = 0; i < count; ++i) {
-    __syncthreads();
-    const uint32_t there = there_next;
-    if (i + 1 < count) load(i + 1);
-#pragma unroll 1
-    for (int first = part * (kTile / PARTS); first < (part + 1) * (kTile / PARTS); first += 32 * NB) process(i, there, first);
-    if (i + 1 < count) widen(i + 1);
+    for (int i = 0; i < count; ++i) {
+      if constexpr (PARTS == 1) {
+        fill_v(i + behind);
+        weights(2 * i);
+        meet();
+        multiply_part(2 * i);
+        fill_k(i + 1 + behind);
+        weights(2 * i + 1);
+        meet();
+        multiply_part(2 * i + 1);
+      } else {
+        fill_v(i + behind);
+        fill_k(i + 1 + behind);
+        weights(i);
+        meet();
+        multiply_part(i);
+      }
+    }
+    if (!behind) meet();
   }
 
   if constexpr (PARTS == 2) {
@@ -893,7 +990,7 @@ struct Way {
 template <int D, bool E5M2, bool F32>
 void launch2(const AttendArgs& a, const Way& w, hipStream_t st) {
   const dim3 g((uint32_t)w.units);
-  if constexpr (!F32) {
+  if constexpr (!F32 && D != 256) {
     if (w.tree)
       return a.row_waves == kTreeWaves ? tree_kernel<D, E5M2, 1><<<g, 64 * kTreeWaves, 0, st>>>(a)
                                        : tree_kernel<D, E5M2, 2><<<g, 64 * kTreeWaves, 0, st>>>(a);
@@ -922,8 +1019,8 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
   if (p->drafts < 1 || p->drafts > 64) return refuse(SN_EINVAL, "drafts must be in [1, 64]");
   if (p->q_heads < 1 || p->q_heads > 65536 || p->q_heads % a.c.heads)
     return refuse(SN_EINVAL, "q_heads must be a multiple of the cache's heads, 65536 at most");
-  if (p->table_cols < 0 || (int64_t)p->table_cols * a.c.page >= (int64_t(1) << 31) - kTile)
-    return refuse(SN_EINVAL, "table_cols must be >= 0, and table_cols * page below 2^31 - 64");
+  if (p->table_cols < 0 || (int64_t)p->table_cols * a.c.page >= (int64_t(1) << 31) - 128)
+    return refuse(SN_EINVAL, "table_cols must be >= 0, and table_cols * page below 2^31 - 128");
   if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return refuse(SN_EINVAL, "scale must be finite and positive");
   constexpr int64_t kMost = int64_t(1) << 40;
   for (int64_t s : {p->q_batch, p->q_draft, p->q_head, p->out_batch, p->out_draft, p->out_head})
@@ -957,9 +1054,10 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
   a.c_log2 = p->scale * 1.44269504088896340736f;
 
   const bool f32 = p->dtype == SN_F32;
-  w.tree = !f32 && a.rows > 64;
+  const int wide = a.c.head_dim <= 64 ? 64 : a.c.head_dim <= 128 ? 128 : 256;
+  w.tree = !f32 && wide <= 128 && a.rows > 64;
   if (w.tree) {
-    a.step = kTile;
+    a.step = tile_of(wide);
     a.row_waves = a.rows > 128 ? kTreeWaves : kTreeWaves / 2;
     w.unit_rows = 32 * a.row_waves;
     a.target = 256;
