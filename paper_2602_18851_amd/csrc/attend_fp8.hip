@@ -44,6 +44,7 @@ struct AttendArgs {
   int32_t batch, drafts, group, rows;  // rows = drafts * group, of a key head
   int32_t max_places, step;  // step: places that go together
   int32_t row_waves, row_blocks;  // waves of a workgroup with rows of their own, and workgroups that share a key head's rows
+  int32_t strands;                // key heads times row_blocks
   int32_t target, least;          // workgroups to aim at, and the least steps of one
   float c_log2;                   // scale * log2(e)
   float* part_out;                // [unit][rows of a workgroup][head_dim], where a sequence is split
@@ -54,72 +55,85 @@ constexpr float kNone = -__builtin_inff();
 
 // ---- how the places are shared out --------------------------------------
 //
-// Lengths are known on the device only, and every workgroup derives the same plan from them: all sequences'
-// steps, over `target` workgroups, give the steps of one (`least` at least, which hide its start and end);
-// a sequence is cut into as many equal chunks as come nearest to that, one at least.  A unit, a chunk
-// of one key head's rows, is one workgroup's.
-struct Split {
-  int64_t per;  // steps that a unit may take
+// Lengths are known on the device only, and every workgroup derives the same plan from them: all sequences' steps (one
+// at least to a sequence), over `target` workgroups, give the steps of one (`least` at least, which hide its start and
+// end); a sequence is cut into as many equal chunks as come nearest to that, one at least.  A unit, a chunk of one
+// key head's rows, is one workgroup's.
+
+__device__ __forceinline__ int length_of(const AttendArgs& a, int b) { return min(max(a.lengths[b], 0), a.max_places); }
+
+// Steps of sequence b, none past the last one.
+__device__ __forceinline__ uint32_t steps_of(const AttendArgs& a, int b) {
+  return b < a.batch ? max(1u, ((uint32_t)length_of(a, b) + (uint32_t)a.step - 1) / (uint32_t)a.step) : 0u;
+}
+
+// Sums over the lanes up to and with each.
+__device__ __forceinline__ uint32_t scan64(uint32_t x) {
+#define SN_ADD(ctrl, rows) x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false)
+  SN_ADD(0x111, 0xf);  // from 1, 2, 4 and 8 lanes down in each row of 16
+  SN_ADD(0x112, 0xf);
+  SN_ADD(0x114, 0xf);
+  SN_ADD(0x118, 0xf);
+  SN_ADD(0x142, 0xa);  // from the last lane of the row below, and of the lower half
+  SN_ADD(0x143, 0xc);
+#undef SN_ADD
+  return x;
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// `steps` over chunks of about `per`.
+__device__ __forceinline__ uint32_t chunks_of(uint32_t steps, uint32_t per) {
+  return steps == 0 ? 0u : max(1u, (steps + per / 2) / per);
+}
+
+struct Plan {
+  uint32_t steps0;  // of sequence `lane`
+  uint32_t per;     // steps that a unit should have
 };
 
-__device__ __forceinline__ int steps_of(const AttendArgs& a, int b) {
-  const int n = min(max(a.lengths[b], 0), a.max_places);
-  return (int)(((int64_t)n + a.step - 1) / a.step);
-}
-
-__device__ __forceinline__ Split plan(const AttendArgs& a, int lane) {
-  int64_t all = 0;
-  for (int b = lane; b < a.batch; b += 64) all += steps_of(a, b);
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) all += __shfl_xor(all, d);
-  const int64_t per = (all * a.c.heads * a.row_blocks + a.target - 1) / a.target;
-  return Split{max(per, (int64_t)a.least)};
-}
-
-__device__ __forceinline__ int chunks_of(int steps, const Split& s) {
-  return max(1, (int)((steps + s.per / 2) / s.per));
+__device__ __forceinline__ Plan plan_of(const AttendArgs& a, int lane) {
+  Plan p;
+  p.steps0 = steps_of(a, lane);
+  uint32_t all = lane_of(scan64(p.steps0), 63);
+  for (int b0 = 64; b0 < a.batch; b0 += 64) all += lane_of(scan64(steps_of(a, b0 + lane)), 63);
+  p.per = max((all * (uint32_t)a.strands + (uint32_t)a.target - 1) / (uint32_t)a.target, (uint32_t)a.least);
+  return p;
 }
 
 // The unit of this workgroup.
 struct Unit {
-  int b, h, rb, len, n_chunks, step0, step1;  // steps from step0 to step1 - 1 (none of a sequence without places)
+  int b, h, rb, len, n_chunks, step0, step1;  // steps from step0 to step1 - 1
 };
 
 __device__ __forceinline__ bool find_unit(const AttendArgs& a, int lane, Unit& u) {
-  const Split split = plan(a, lane);
-  const int per_chunk = a.c.heads * a.row_blocks;  // units of a chunk
-  int64_t left = blockIdx.x;                       // units before this one, less those of the sequences before
+  const Plan p = plan_of(a, lane);
+  uint32_t base = 0, in = 0, steps = 0;
   int b = -1;
   for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    int64_t mine = 0;
-    if (b0 + lane < a.batch) mine = (int64_t)chunks_of(steps_of(a, b0 + lane), split) * per_chunk;
-    int64_t sum = mine;  // of the lanes up to this one
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
-    }
-    const uint64_t there = __ballot(sum > left);
+    const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
+    const uint32_t mine = chunks_of(n, p.per) * (uint32_t)a.strands, sum = scan64(mine);
+    const uint64_t there = __ballot(blockIdx.x < base + sum);
     if (there) {
       const int at = __builtin_ctzll(there);
       b = b0 + at;
-      left -= __shfl(sum - mine, at);
+      steps = lane_of(n, at);
+      in = blockIdx.x - (base + lane_of(sum, at) - lane_of(mine, at));
       break;
     }
-    left -= __shfl(sum, 63);
+    base += lane_of(sum, 63);
   }
   if (b < 0) return false;
+  const uint32_t chunk = in / (uint32_t)a.strands, strand = in % (uint32_t)a.strands, n = chunks_of(steps, p.per);
+  const uint32_t per = (steps + n - 1) / n;
   u.b = uni(b);
-  const int in_seq = uni((int)left);
-  const int chunk = in_seq / per_chunk, rest = in_seq % per_chunk;
-  u.h = rest % a.c.heads;
-  u.rb = rest / a.c.heads;
-  u.len = uni(min(max(a.lengths[u.b], 0), a.max_places));
-  const int steps = uni(steps_of(a, u.b));
-  u.n_chunks = uni(chunks_of(steps, split));
-  const int per = (steps + u.n_chunks - 1) / u.n_chunks;
-  u.step0 = min(steps, chunk * per);
-  u.step1 = min(steps, u.step0 + per);
+  u.h = uni((int)(strand % (uint32_t)a.c.heads));
+  u.rb = uni((int)(strand / (uint32_t)a.c.heads));
+  u.len = uni(length_of(a, b));
+  u.n_chunks = uni((int)n);
+  u.step0 = uni((int)min(steps, chunk * per));
+  u.step1 = uni((int)min(steps, chunk * per + per));
   return true;
 }
 
@@ -171,6 +185,10 @@ __device__ __forceinline__ float quarters_sum(float x) {
 }
 
 
+// A row's running maximum is raised, and its sums scaled, only when a logit is above it by a factor of 2^kSlack in weight: until
+// then weights are up to 2^kSlack, which float32 and bf16 hold as exactly.
+constexpr float kSlack = 8.f;
+
 // exp2 of the distance to a running maximum; a row that has seen nothing has none.
 __device__ __forceinline__ float weight_of(float m, float to, float c) {
   return m == kNone ? 0.f : __builtin_amdgcn_exp2f((m - to) * c);
@@ -186,8 +204,8 @@ __device__ __forceinline__ void store_row4(const AttendArgs& a, int b, int h, in
   *reinterpret_cast<vec_any*>(static_cast<T*>(a.out) + at) = vec{(T)x[0], (T)x[1], (T)x[2], (T)x[3]};
 }
 
-// Waves of a workgroup, with NT blocks of 16 rows in a wave.
-constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
+// Waves of a workgroup of attend_kernel.
+constexpr int kWaves = 4;
 
 // D: head_dim rounded up to 64, 128 or 256.  Lane q * 16 + s of a wave holds
 //   of K: places s of each of two groups of 16, bytes 16 q .. + 15 of every 64;
@@ -195,8 +213,8 @@ constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
 //   of S^T and P^T: those places of V for row s of each block;
 //   of O^T: for row s, D / 4 elements from D / 4 q on.
 template <int D, bool E5M2, bool F32, int NT>
-__global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 256 ? 1 : 2) attend_kernel(AttendArgs a) {
-  constexpr int W = waves_of(NT), KC = D / 64, VB = D / 16, QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
+__global__ void __launch_bounds__(64 * kWaves, NT * D * (F32 ? 2 : 1) > 256 ? 1 : 2) attend_kernel(AttendArgs a) {
+  constexpr int W = kWaves, KC = D / 64, VB = D / 16, QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
   constexpr int REGS = NT * (D / 4 + 2);  // of a wave's result: O, maximum, sum
   __shared__ float merge[W / 2][REGS][64];
   const int lane = threadIdx.x & 63;
@@ -245,62 +263,76 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
       }
   }
 
-  // One step's part of the cache in registers.
-  struct Tile {
-    u32x4 k[2][KC];
-    float ks[2];
-    uint32_t v[2][4][VB / 4];
-    f32x4 vs[2];
-    int place;       // its first
-    bool there[2];   // whether the table has a page for each group
-  };
-  int page_a = -1, page_b = -1;  // lane l: pages of this wave's step l of the current 64
+  // One step's part of the cache in registers.  Elements from head_dim on are out of range of a load and read zeros, and so
+  // does all of a step past the last.
+  u32x4 kc[2][KC];
+  float ks[2];
+  uint32_t vc[2][4][VB / 4];
+  f32x4 vs[2];
+  constexpr uint32_t kNowhere = 0x80000000u;
+  uint32_t k_off[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) k_off[c] = 64 * c + 16 * q < dh ? (uint32_t)(s * dh + 64 * c + 16 * q) : kNowhere;
+  const uint32_t v_off = VB * s < dh ? (uint32_t)(4 * q * dh + VB * s) : kNowhere;
   const int count = rows_there && step1 - step0 > part ? (step1 - step0 - part + parts - 1) / parts : 0;
-  auto load = [&](Tile& t, int i) {  // this wave's step i, in order
+  int page_a = -1, page_b = -1;  // lane l: pages of this wave's step l of the current 64
+  int ids[2];                    // of the step whose keys were requested last
+  auto place_of = [&](int i) { return (int)((uint32_t)(step0 + part + parts * i) * kStep); };
+  auto base_of = [&](int i, int g, int64_t& page) {
+    // a group without a page reads page 0, to no use
+    const int id = ids[g];
+    page = id >= 0 ? id : 0;
+    return (h << a.c.page_shift) + (id >= 0 ? (place_of(i) + 16 * g) & (a.c.page - 1) : 0);
+  };
+  auto load_k = [&](int i) {  // this wave's step i, in order
     if ((i & 63) == 0) {
-      auto page_of = [&](int place) {
-        const int id = place >= 0 && place < len ? a.table[b * a.table_ld + (place >> a.c.page_shift)] : -1;
+      auto page_of = [&](int64_t place) {
+        int id = -1;
+        if (place >= 0 && place < len) id = a.table[b * a.table_ld + (place >> a.c.page_shift)];
         return id >= 0 && id < a.c.pages ? id : -1;
       };
       const int64_t mine = (int64_t)(step0 + part) + (int64_t)parts * (i + lane);
-      const int place = mine < step1 ? (int)mine * kStep : -1;
-      page_a = page_of(place);
-      page_b = page_of(place < 0 ? -1 : place + 16);
+      page_a = page_of(mine < step1 ? mine * kStep : -1);
+      page_b = page_of(mine < step1 ? mine * kStep + 16 : -1);
     }
-    t.place = (step0 + part + parts * i) * kStep;
+    const uint32_t bytes = i < count ? 0x7fffffffu : 0u;
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const int id = __builtin_amdgcn_readlane(g ? page_b : page_a, i & 63);
-      t.there[g] = id >= 0;
-      // a group without a page reads page 0, to no use
-      const int in = (h << a.c.page_shift) + (id >= 0 ? (t.place + 16 * g) & (a.c.page - 1) : 0);
-      const int64_t page = id >= 0 ? id : 0;
-      const uint8_t* kp = a.c.k + page * a.c.code_page + (int64_t)in * dh;
-      const uint8_t* vp = a.c.v + page * a.c.code_page + (int64_t)in * dh;
-      const float* ksp = a.c.k_scale + page * a.c.scale_page + in;
-      const float* vsp = a.c.v_scale + page * a.c.scale_page + in;
+      ids[g] = __builtin_amdgcn_readlane(g ? page_b : page_a, i & 63);
+      int64_t page;
+      const int in = base_of(i, g, page);
+      const __amdgpu_buffer_rsrc_t r = make_rsrc(a.c.k + page * a.c.code_page + (int64_t)in * dh, bytes);
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        t.k[g][c] = u32x4{0, 0, 0, 0};
-        if (64 * c + 16 * q < dh) t.k[g][c] = *reinterpret_cast<const u32x4*>(kp + s * dh + 64 * c + 16 * q);
-      }
-      t.ks[g] = ksp[s];
+      for (int c = 0; c < KC; ++c)
+        kc[g][c] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, k_off[c], 0, 0));
+      ks[g] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+          make_rsrc(a.c.k_scale + page * a.c.scale_page + in, bytes), 4u * (uint32_t)s, 0, 0));
+    }
+  };
+  auto load_v = [&](int i) {  // after load_k(i)
+    const uint32_t bytes = i < count ? 0x7fffffffu : 0u;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      int64_t page;
+      const int in = base_of(i, g, page);
+      const __amdgpu_buffer_rsrc_t r = make_rsrc(a.c.v + page * a.c.code_page + (int64_t)in * dh, bytes);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
+        if constexpr (VB == 4) {
+          vc[g][e][0] = __builtin_amdgcn_raw_buffer_load_b32(r, v_off, (uint32_t)(e * dh), 0);
+        } else if constexpr (VB == 8) {
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, v_off, (uint32_t)(e * dh), 0));
+          vc[g][e][0] = x[0], vc[g][e][1] = x[1];
+        } else {
+          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, v_off, (uint32_t)(e * dh), 0));
 #pragma unroll
-        for (int w = 0; w < VB / 4; ++w) t.v[g][e][w] = 0;
-        if (VB * s < dh) {
-          typedef uint32_t words __attribute__((ext_vector_type(VB / 4)));
-          if constexpr (VB == 4) {
-            t.v[g][e][0] = *reinterpret_cast<const uint32_t*>(vp + (4 * q + e) * dh + VB * s);
-          } else {
-            const words x = *reinterpret_cast<const words*>(vp + (4 * q + e) * dh + VB * s);
-#pragma unroll
-            for (int w = 0; w < VB / 4; ++w) t.v[g][e][w] = x[w];
-          }
+          for (int w = 0; w < 4; ++w) vc[g][e][w] = x[w];
         }
       }
-      t.vs[g] = *reinterpret_cast<const f32x4*>(vsp + 4 * q);
+      vs[g] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                            make_rsrc(a.c.v_scale + page * a.c.scale_page + in, bytes),
+                                            16u * (uint32_t)q, 0, 0));
     }
   };
 
@@ -314,11 +346,11 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
     for (int j = 0; j < VB; ++j) acc[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float c_log2 = a.c_log2;
+  f32x4 st[NT][2];
+  bf16x8 pf[NT][PP];
+  uint32_t seen[NT];  // bit 4 g + e
 
-  auto process = [&](Tile& t) {
-    // all places of the step are seen by every row, unless it holds drafted tokens, the end, or lacks a page
-    const bool edge = !t.there[0] || !t.there[1] || t.place + kStep > len - T;
-    f32x4 st[NT][2];
+  auto scores = [&]() {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
 #pragma unroll
@@ -327,10 +359,10 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
       for (int c = 0; c < KC; ++c)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          __builtin_amdgcn_sched_barrier(0);
-          const uint32_t w0 = t.k[g][c][2 * u], w1 = t.k[g][c][2 * u + 1];
-          const u32x4 wide = {widen2<E5M2, false>(w0, t.ks[g]), widen2<E5M2, true>(w0, t.ks[g]),
-                              widen2<E5M2, false>(w1, t.ks[g]), widen2<E5M2, true>(w1, t.ks[g])};
+          if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);  // a few converted values at a time
+          const uint32_t w0 = kc[g][c][2 * u], w1 = kc[g][c][2 * u + 1];
+          const u32x4 wide = {widen2<E5M2, false>(w0, ks[g]), widen2<E5M2, true>(w0, ks[g]),
+                              widen2<E5M2, false>(w1, ks[g]), widen2<E5M2, true>(w1, ks[g])};
           const bf16x8 kf = __builtin_bit_cast(bf16x8, wide);
 #pragma unroll
           for (int n = 0; n < NT; ++n)
@@ -338,40 +370,41 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
             for (int p = QP - 1; p >= 0; --p) st[n][g] = multiply(kf, qf[n][c][u][p], st[n][g]);
         }
     }
-    uint32_t seen[NT];  // bit 4 g + e
-    if (edge) {
+  };
+  auto hide = [&](int place, bool there0, bool there1) {  // what a row does not see
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        seen[n] = 0;
+    for (int n = 0; n < NT; ++n) {
+      seen[n] = 0;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          // four places from drafted token j on: ones before the first, zeros past the last
-          const int j = t.place + 16 * g + 4 * q - (len - T);
-          const int before = min(max(-j, 0), 4);
-          const uint32_t of_tree = (uint32_t)(sees[n] >> min(max(j, 0), 63)) << before | ((1u << before) - 1u);
-          const uint32_t four = t.there[g] & (j < 64) ? of_tree & 15u : 0u;
-          seen[n] |= four << (4 * g);
-          f32x4 of_seen;
+      for (int g = 0; g < 2; ++g) {
+        // four places from drafted token j on: ones before the first, zeros past the last
+        const int j = place + 16 * g + 4 * q - (len - T);
+        const int before = min(max(-j, 0), 4);
+        const uint32_t of_tree = (uint32_t)(sees[n] >> min(max(j, 0), 63)) << before | ((1u << before) - 1u);
+        const uint32_t four = (g ? there1 : there0) & (j < 64) ? of_tree & 15u : 0u;
+        seen[n] |= four << (4 * g);
+        f32x4 of_seen;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) of_seen[e] = four >> e & 1u ? st[n][g][e] : kNone;
-          st[n][g] = of_seen;
-        }
+        for (int e = 0; e < 4; ++e) of_seen[e] = four >> e & 1u ? st[n][g][e] : kNone;
+        st[n][g] = of_seen;
       }
     }
-    bf16x8 pf[NT][PP];
+  };
+  auto weights = [&]() {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       float m = fmaxf(fmaxf(fmaxf(st[n][0][0], st[n][0][1]), fmaxf(st[n][0][2], st[n][0][3])),
                       fmaxf(fmaxf(st[n][1][0], st[n][1][1]), fmaxf(st[n][1][2], st[n][1][3])));
-      m = fmaxf(quarters_max(m), top[n]);
-      if (__ballot(m > top[n])) {
+      m = quarters_max(m);
+      if (__ballot((m - top[n]) * c_log2 > kSlack)) {
+        m = fmaxf(m, top[n]);
         const float w = weight_of(top[n], m, c_log2);
         total[n] *= w;
 #pragma unroll
         for (int j = 0; j < VB; ++j) acc[n][j] *= w;
         top[n] = m;
       }
-      const float base = m == kNone ? 0.f : m * c_log2;
+      const float base = top[n] == kNone ? 0.f : top[n] * c_log2;
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -380,89 +413,103 @@ __global__ void __launch_bounds__(64 * waves_of(NT), NT * D * (F32 ? 2 : 1) > 25
       }
       split8<PP>(p, pf[n]);
     }
-    // V, place by place, to pairs of places of one element each: place pairs 01 and 23 of both groups
-    auto values = [&](int w, u32x4 (&vt)[4]) {  // elements 4 w .. 4 w + 3
+  };
+  // V, place by place, to pairs of places of one element each: place pairs 01 and 23 of both groups, of elements 4 w .. + 3
+  auto widen = [&](int w, u32x4 (&vt)[4]) {
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < 2; ++g)
 #pragma unroll
-        for (int h2 = 0; h2 < 2; ++h2) {
-          uint32_t x[2][2];
+      for (int h2 = 0; h2 < 2; ++h2) {
+        uint32_t x[2][2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            x[e][0] = widen2<E5M2, false>(t.v[g][2 * h2 + e][w], t.vs[g][2 * h2 + e]);
-            x[e][1] = widen2<E5M2, true>(t.v[g][2 * h2 + e][w], t.vs[g][2 * h2 + e]);
-          }
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            vt[2 * u][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x05040100u);
-            vt[2 * u + 1][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x07060302u);
-          }
+        for (int e = 0; e < 2; ++e) {
+          x[e][0] = widen2<E5M2, false>(vc[g][2 * h2 + e][w], vs[g][2 * h2 + e]);
+          x[e][1] = widen2<E5M2, true>(vc[g][2 * h2 + e][w], vs[g][2 * h2 + e]);
         }
-    };
-    auto add = [&](int j, const u32x4& vt) {
-      const bf16x8 vf = __builtin_bit_cast(bf16x8, vt);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int p = PP - 1; p >= 0; --p) acc[n][j] = multiply(vf, pf[n][p], acc[n][j]);
-    };
+        for (int u = 0; u < 2; ++u) {
+          vt[2 * u][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x05040100u);
+          vt[2 * u + 1][2 * g + h2] = __builtin_amdgcn_perm(x[1][u], x[0][u], 0x07060302u);
+        }
+      }
+  };
+  // Values that are not finite reach only the rows that see them: in steps that not all rows see they count as zeros,
+  // and whoever sees one gets NaN afterwards.
+  auto bad_of = [](uint32_t v) {
+    return ((v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+  };
+  auto values = [&](bool edge) {
+    uint32_t any = 0;
 #pragma unroll
     for (int w = 0; w < VB / 4; ++w) {
-      __builtin_amdgcn_sched_barrier(0);  // a few converted values at a time
+      if constexpr (NT > 1) __builtin_amdgcn_sched_barrier(0);  // a few converted values at a time
       u32x4 vt[4];
-      values(w, vt);
+      widen(w, vt);
       if (edge) {
-        // Values that are not finite reach only the rows that see them: here they count as zeros, and whoever sees one
-        // gets NaN.
-        uint32_t bad[4][4], any = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const uint32_t v = vt[j][x];
-            const uint32_t lo = (v & 0x7f80u) == 0x7f80u ? 0xffffu : 0u;
-            const uint32_t hi = (v & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-            bad[j][x] = lo | hi;
-            any |= lo | hi;
+            const uint32_t bad = bad_of(vt[j][x]);
+            any |= bad;
+            vt[j][x] &= ~bad;
           }
-        if (__ballot(any != 0)) {
+      }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            u32x4 ones;
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              vt[j][x] &= ~bad[j][x];
-              ones[x] = bad[j][x] & 0x3f803f80u;  // 1 in bf16
-            }
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              u32x4 who;
+          for (int p = PP - 1; p >= 0; --p)
+            acc[n][4 * w + j] = multiply(__builtin_bit_cast(bf16x8, vt[j]), pf[n][p], acc[n][4 * w + j]);
+    }
+    if (edge && __ballot(any != 0)) {
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                who[x] = (seen[n] >> (2 * x) & 1 ? 0x3f80u : 0u) | (seen[n] >> (2 * x + 1) & 1 ? 0x3f800000u : 0u);
-              const f32x4 n_bad = multiply(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, who),
-                                           f32x4{0.f, 0.f, 0.f, 0.f});
+      for (int w = 0; w < VB / 4; ++w) {
+        u32x4 vt[4];
+        widen(w, vt);
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                acc[n][4 * w + j][e] = n_bad[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[n][4 * w + j][e];
-            }
+        for (int j = 0; j < 4; ++j) {
+          u32x4 ones;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) ones[x] = bad_of(vt[j][x]) & 0x3f803f80u;  // 1 in bf16
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            u32x4 who;
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              who[x] = (seen[n] >> (2 * x) & 1 ? 0x3f80u : 0u) | (seen[n] >> (2 * x + 1) & 1 ? 0x3f800000u : 0u);
+            const f32x4 n_bad = multiply(__builtin_bit_cast(bf16x8, ones), __builtin_bit_cast(bf16x8, who),
+                                         f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[n][4 * w + j][e] = n_bad[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[n][4 * w + j][e];
           }
         }
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) add(4 * w + j, vt[j]);
     }
   };
 
+  // The keys of the next step are on their way while this one's weights are formed and its values multiplied, the next values
+  // while the next scores are.
   if (count > 0) {
-    Tile now, next;
-    load(next, 0);
+    load_k(0);
+    __builtin_amdgcn_sched_barrier(0);  // requested in the order of the loop, or this would wait for all of them
+    load_v(0);
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
-      now = next;
-      if (i + 1 < count) load(next, i + 1);  // on its way while this one is processed
+      const bool there0 = ids[0] >= 0, there1 = ids[1] >= 0;
+      const int place = place_of(i);
+      scores();
+      load_k(i + 1);
+      // all places of the step are seen by every row, unless it holds drafted tokens, the end, or lacks a page
+      const bool edge = !there0 || !there1 || (int64_t)place + kStep > len - T;
+      if (edge) hide(place, there0, there1);
+      weights();
+      values(edge);
       __builtin_amdgcn_sched_barrier(0);
-      process(now);
+      load_v(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -547,12 +594,14 @@ __device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, c
 // a part on the matrix cores, O += P V of step k - 1 and S of step k, and one on the vector units, P of step k, with a bare
 // barrier after each, and waves 4-7 run one part behind waves 0-3: on every SIMD one wave multiplies while the other
 // exponentiates.  With the vector part goes a share of a tile to LDS, where K and V have two places each.  Counting
-// parts, waves 0-3 multiply step k in part 2 k, waves 4-7 in part 2 k + 1.  PARTS 1: K of tile i + 1 is first read in
-// part 4 i + 4, K of i - 1 last in 4 i - 1; V of tile i first in 4 i + 2, V of i - 2 last in 4 i - 3.  Waves 0-3 write V of tile i
-// with step 2 i and K of i + 1 with 2 i + 1, in parts 4 i + 1 and 4 i + 3; waves 4-7, a tile ahead, V of i + 1 and K of
-// i + 2 in the same steps, parts 4 i + 2 and 4 i + 4.  PARTS 2, both with each step: K of i + 1 and V of i are first
-// read in 2 i + 2, K of i - 1 and V of i - 2 last in 2 i - 1, and written in 2 i + 1 and 2 i.  Tiles past the last are
-// loaded and written too, to no use, so that no load in flight meets a branch: the compiler would wait for all of them there.
+// parts, waves 0-3 multiply step k in part 2 k, waves 4-7 in part 2 k + 1.
+//   PARTS 1: K of tile i + 1 is first read in part 4 i + 4, K of i - 1 last in 4 i - 1; V of i + 1 first at the end of 4 i
+//   + 5, V of i - 1 last in 4 i + 1.  All waves write K of i + 1 with step 2 i, in parts 4 i + 1 and 4 i + 2, and V of i + 1 with
+//   step 2 i + 1, in 4 i + 3 and 4 i + 4.
+//   PARTS 2, both with each step: K of i + 1 and V of i are first read in 2 i + 2, K of i - 1 and V of i - 2 last in 2 i - 1;
+//   waves 0-3 write them in 2 i + 1, waves 4-7, a tile ahead, in 2 i.
+// Tiles past the last are loaded and written too, to no use, so that no load in flight meets a branch: the compiler would
+// wait for all of them there.
 constexpr int tile_of(int d) { return 8192 / d; }
 
 template <int D, bool E5M2, int PARTS>
@@ -729,17 +778,35 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
 
   auto tile = [](int k) { return PARTS == 1 ? k >> 1 : k; };
   auto half = [&](int k) { return PARTS == 1 ? k & 1 : part; };
-  auto scores = [&](int k) {
+  // Operands from LDS: of V for eight products with each part of P, of K for eight
+  bf16x8 vf[8], kf[8];
+  auto read_values = [&](int k) {
+    const int u = half(k);
+    const uint8_t* v = tiles + (2 + (tile(k) & 1)) * kBytes + (NB == 2 ? u * D * 128 : 0);
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+      const int at = at_chunk[g] ^ (NB == 1 ? 64 * u : 0);  // chunk 4 u + 2 g + hi
+#pragma unroll
+      for (int j = 0; j < DB; ++j) vf[g * DB + j] = *reinterpret_cast<const bf16x8*>(v + 32 * j * 128 + at);
+    }
+  };
+  auto read_keys = [&](int k, int x) {  // four of them
     const uint8_t* kt = tiles + (tile(k) & 1) * kBytes + half(k) * 32 * NB * 128;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) st[n] = zero;
-#pragma unroll
-    for (int c = 0; c < KS; ++c) {
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-        st[n] = multiply32(*reinterpret_cast<const bf16x8*>(kt + ((c >> 2) * kTile + 32 * n) * 128 + at_chunk[c & 3]),
-                           qf[c], st[n]);
+    for (int y = x; y < x + 4; ++y) {
+      const int c = y / NB, n = y % NB;
+      kf[y] = *reinterpret_cast<const bf16x8*>(kt + ((c >> 2) * kTile + 32 * n) * 128 + at_chunk[c & 3]);
     }
+  };
+  auto multiply_values = [&](int x) {
+#pragma unroll
+    for (int y = x; y < x + 4; ++y) acc[y % DB] = multiply32(vf[y], pf[y / DB][1], acc[y % DB]);
+#pragma unroll
+    for (int y = x; y < x + 4; ++y) acc[y % DB] = multiply32(vf[y], pf[y / DB][0], acc[y % DB]);
+  };
+  auto multiply_keys = [&](int x) {
+#pragma unroll
+    for (int y = x; y < x + 4; ++y) st[y % NB] = multiply32(kf[y], qf[y / NB], y < NB ? zero : st[y % NB]);
   };
   auto weights = [&](int k) {
     const int i = tile(k), first = half(k) * 32 * NB, place = (unit.step0 + i) * kTile;
@@ -770,15 +837,16 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, st[n][e]);
-    m = fmaxf(fmaxf(m, __shfl_xor(m, 32)), top);
-    if (__ballot(m > top)) {
+    m = fmaxf(m, __shfl_xor(m, 32));
+    if (__ballot((m - top) * c_log2 > kSlack)) {
+      m = fmaxf(m, top);
       const float w = weight_of(top, m, c_log2);
       total *= w;
 #pragma unroll
       for (int j = 0; j < DB; ++j) acc[j] *= w;
       top = m;
     }
-    const float base = m == kNone ? 0.f : m * c_log2;
+    const float base = top == kNone ? 0.f : top * c_log2;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -792,20 +860,6 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
         split8<2>(p, pf[2 * n + g]);
         __builtin_amdgcn_sched_barrier(0);
       }
-  };
-  auto values = [&](int k) {
-    const int u = half(k);
-    const uint8_t* v = tiles + (2 + (tile(k) & 1)) * kBytes + (NB == 2 ? u * D * 128 : 0);
-#pragma unroll
-    for (int g = 0; g < 2 * NB; ++g) {
-      const int at = at_chunk[g] ^ (NB == 1 ? 64 * u : 0);  // chunk 4 u + 2 g + hi
-#pragma unroll
-      for (int j = 0; j < DB; ++j) {
-        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(v + 32 * j * 128 + at);
-        acc[j] = multiply32(vf, pf[g][1], acc[j]);
-        acc[j] = multiply32(vf, pf[g][0], acc[j]);
-      }
-    }
   };
   // Whoever sees a value that is not finite gets NaN (tiles that not all rows see; hardly ever any).
   auto poison = [&](int k) {
@@ -844,34 +898,52 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
   if (count > 0) {
     const int behind = wv >> 2;
     load_k(0);
+    load_v(0);
     widen_k(0);
     load_k(1);
-    load_v(0);
+    if constexpr (PARTS == 1) {
+      widen_v(0);
+      load_v(1);
+    }
     meet();
     if (behind) {
-      fill_v(0);
-      fill_k(1);
+      if constexpr (PARTS == 2) {
+        fill_v(0);
+        fill_k(1);
+      }
       meet();
     }
-    scores(0);
+    read_keys(0, 0);
+    read_keys(0, 4);
+    multiply_keys(0);
+    multiply_keys(4);
     meet();
     auto multiply_part = [&](int k) {
+      if constexpr (PARTS == 2) read_values(k);
       __builtin_amdgcn_s_setprio(1);
-      values(k);
+      multiply_values(0);
+      __builtin_amdgcn_sched_barrier(0);
+      read_keys(k + 1, 0);
+      multiply_values(4);
+      __builtin_amdgcn_sched_barrier(0);
+      read_keys(k + 1, 4);
       if (edge) poison(k);
-      scores(k + 1);
+      multiply_keys(0);
+      multiply_keys(4);
       __builtin_amdgcn_s_setprio(0);
       meet();
     };
 #pragma unroll 1
     for (int i = 0; i < count; ++i) {
       if constexpr (PARTS == 1) {
-        fill_v(i + behind);
+        fill_k(i + 1);
         weights(2 * i);
+        read_values(2 * i);
         meet();
         multiply_part(2 * i);
-        fill_k(i + 1 + behind);
+        fill_v(i + 1);
         weights(2 * i + 1);
+        read_values(2 * i + 1);
         meet();
         multiply_part(2 * i + 1);
       } else {
@@ -934,14 +1006,14 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) 
   const int lane = threadIdx.x & 63, t = threadIdx.x;
   const int heads_q = a.c.heads * a.group;
   const int row = blockIdx.x % (a.drafts * heads_q), b = blockIdx.x / (a.drafts * heads_q);
-  const Split split = plan(a, lane);
-  const int n_chunks = uni(chunks_of(steps_of(a, b), split));
-  if (n_chunks == 1) return;  // whole workgroup: written already
-  const int per_chunk = a.c.heads * a.row_blocks;
-  int64_t before = 0;  // units of the sequences before
-  for (int x = lane; x < b; x += 64) before += (int64_t)chunks_of(steps_of(a, x), split) * per_chunk;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
+  const Plan p = plan_of(a, lane);
+  const uint32_t n_chunks = uni((int)chunks_of(steps_of(a, b), p.per));
+  if (n_chunks <= 1) return;  // whole workgroup: written already
+  uint32_t before = 0;  // units of the sequences before
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
+    before += lane_of(scan64(b0 + lane < b ? chunks_of(n, p.per) * (uint32_t)a.strands : 0u), 63);
+  }
   const int i = row / heads_q, hq = row % heads_q, h = hq / a.group, r = i * a.group + hq % a.group;
   const int rb = r / unit_rows, in = r % unit_rows, dh = a.c.head_dim;
   const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, groups = 256 / lanes;
@@ -949,8 +1021,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) 
   float top = kNone, total = 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int c = g; c < n_chunks; c += groups) {
-    const int64_t at = (before + (int64_t)c * per_chunk + rb * a.c.heads + h) * unit_rows + in;
+  for (uint32_t c = g; c < n_chunks; c += groups) {
+    const int64_t at = ((int64_t)before + (int64_t)c * a.strands + rb * a.c.heads + h) * unit_rows + in;
     const float2 st = a.part_stat[at];
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
     if (4 * l < dh) x = *reinterpret_cast<const f32x4*>(a.part_out + at * dh + 4 * l);
@@ -995,10 +1067,9 @@ void launch2(const AttendArgs& a, const Way& w, hipStream_t st) {
       return a.row_waves == kTreeWaves ? tree_kernel<D, E5M2, 1><<<g, 64 * kTreeWaves, 0, st>>>(a)
                                        : tree_kernel<D, E5M2, 2><<<g, 64 * kTreeWaves, 0, st>>>(a);
   }
-  if (w.nt == 1) return attend_kernel<D, E5M2, F32, 1><<<g, 64 * waves_of(1), 0, st>>>(a);
+  if (w.nt == 1) return attend_kernel<D, E5M2, F32, 1><<<g, 64 * kWaves, 0, st>>>(a);
   if constexpr (!(D == 256 && F32)) {
-    if (w.nt == 2) return attend_kernel<D, E5M2, F32, 2><<<g, 64 * waves_of(2), 0, st>>>(a);
-    if constexpr (D != 256 && !F32) attend_kernel<D, E5M2, F32, 4><<<g, 64 * waves_of(4), 0, st>>>(a);
+    attend_kernel<D, E5M2, F32, 2><<<g, 64 * kWaves, 0, st>>>(a);
   }
 }
 
@@ -1063,9 +1134,8 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.target = 256;
     a.least = 4;
   } else {
-    const int most = a.c.head_dim > 128 ? (f32 ? 1 : 2) : f32 ? 2 : 4;
-    w.nt = a.rows <= 16 ? 1 : a.rows <= 32 ? std::min(2, most) : most;
-    const int waves = waves_of(w.nt), blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
+    w.nt = a.rows <= 16 || (a.c.head_dim > 128 && f32) ? 1 : 2;
+    const int waves = kWaves, blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
     a.step = kStep;
     a.row_waves = 1;
     while (a.row_waves < waves && a.row_waves < blocks) a.row_waves *= 2;
@@ -1073,13 +1143,16 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.target = 1024;
     a.least = 8;
   }
-  const int waves = w.tree ? kTreeWaves : waves_of(w.nt);
+  const int waves = w.tree ? kTreeWaves : kWaves;
   a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
-  const int64_t per_chunk = (int64_t)a.c.heads * a.row_blocks;
+  const int64_t strands = (int64_t)a.c.heads * a.row_blocks;
+  const int64_t steps = std::max<int64_t>(1, ((int64_t)a.max_places + a.step - 1) / a.step);
+  if (a.batch * steps * strands >= (int64_t(1) << 31))
+    return refuse(SN_EINVAL, "batch * table_cols * page * heads is too large");
+  a.strands = (int32_t)strands;
   // a sequence has a chunk for every `per` of its steps and one more at most, and `per` is `least` at least
-  const int64_t steps = ((int64_t)a.max_places + a.step - 1) / a.step;
   const int64_t longest = std::max<int64_t>(1, (steps + a.least / 2) / a.least);
-  w.units = std::min((int64_t)a.batch * longest * per_chunk, a.target + (int64_t)a.batch * per_chunk);
+  w.units = std::min((int64_t)a.batch * longest * strands, a.target + (int64_t)a.batch * strands);
   if (w.units * 64 * waves >= (int64_t(1) << 32) ||
       (int64_t)a.batch * a.drafts * p->q_heads * 256 >= (int64_t(1) << 32))
     return refuse(SN_EINVAL, "batch * drafts * q_heads is too large");
