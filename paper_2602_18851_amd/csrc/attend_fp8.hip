@@ -998,52 +998,99 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     }
 }
 
-// Joins the chunks of a row, in order: a workgroup a row, groups of lanes every so many chunks, 4 elements a lane.
+// Joins the chunks of rows.  Groups of lanes, 4 elements a lane, take every so many chunks, eight at a time, whose loads are
+// all on their way at once; the groups' results meet in LDS.  A workgroup takes some rows of a key head, so that the
+// workgroups of many rows that were not cut, which have nothing to do, are few (65536 rows: 43 us with one to
+// a workgroup, 4.7 with 64).
+constexpr int kAtOnce = 8;
+
 template <bool F32>
-__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows) {
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows, int rows_each) {
   __shared__ f32x4 sums[256];
   __shared__ float2 stats[16];
-  const int lane = threadIdx.x & 63, t = threadIdx.x;
-  const int heads_q = a.c.heads * a.group;
-  const int row = blockIdx.x % (a.drafts * heads_q), b = blockIdx.x / (a.drafts * heads_q);
+  const int t = threadIdx.x, lane = t & 63;
+  const int per_head = (a.rows + rows_each - 1) / rows_each;
+  const int part = blockIdx.x % per_head, h = blockIdx.x / per_head % a.c.heads, b = blockIdx.x / per_head / a.c.heads;
   const Plan p = plan_of(a, lane);
-  const uint32_t n_chunks = uni((int)chunks_of(steps_of(a, b), p.per));
+  const uint32_t steps = b < 64 ? lane_of(p.steps0, b) : (uint32_t)uni((int)steps_of(a, b));
+  const uint32_t n_chunks = chunks_of(steps, p.per);
   if (n_chunks <= 1) return;  // whole workgroup: written already
-  uint32_t before = 0;  // units of the sequences before
+  uint32_t before = 0;        // units of the sequences before
   for (int b0 = 0; b0 < b; b0 += 64) {
     const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
     before += lane_of(scan64(b0 + lane < b ? chunks_of(n, p.per) * (uint32_t)a.strands : 0u), 63);
   }
-  const int i = row / heads_q, hq = row % heads_q, h = hq / a.group, r = i * a.group + hq % a.group;
-  const int rb = r / unit_rows, in = r % unit_rows, dh = a.c.head_dim;
-  const int lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, groups = 256 / lanes;
-  const int l = t % lanes, g = t / lanes;
-  float top = kNone, total = 0.f;
-  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (uint32_t c = g; c < n_chunks; c += groups) {
-    const int64_t at = ((int64_t)before + (int64_t)c * a.strands + rb * a.c.heads + h) * unit_rows + in;
-    const float2 st = a.part_stat[at];
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (4 * l < dh) x = *reinterpret_cast<const f32x4*>(a.part_out + at * dh + 4 * l);
-    const float m = fmaxf(top, st.x), w0 = weight_of(top, m, a.c_log2), w1 = weight_of(st.x, m, a.c_log2);
-    top = m;
-    total = total * w0 + st.y * w1;
-    sum = sum * w0 + x * w1;
+  const int dh = a.c.head_dim, lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, groups = 256 / lanes;
+  const int l = t % lanes, g = t / lanes, d = min(4 * l, dh - 4);
+  const auto put = [&](int r, const f32x4& sum, float total) {
+    if (4 * l < dh)
+      store_row4<typename std::conditional<F32, float, __bf16>::type>(a, b, h, r, 4 * l,
+                                                                      sum * (total == 0.f ? 0.f : 1.f / total));
+  };
+  // One row: the chunks from c0 on, `step` apart.
+  float top, total;
+  f32x4 sum;
+  const auto add = [&](int r, uint32_t c0, uint32_t step) {
+    const int rb = r / unit_rows, in = r % unit_rows;
+    const int64_t first = ((int64_t)before + rb * a.c.heads + h) * unit_rows + in, apart = (int64_t)a.strands * unit_rows;
+    top = kNone;
+    total = 0.f;
+    sum = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (; c0 < n_chunks; c0 += kAtOnce * step) {
+      float2 st[kAtOnce];
+      f32x4 x[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t at = first + (int64_t)min(c0 + u * step, n_chunks - 1) * apart;
+        st[u] = a.part_stat[at];
+        x[u] = *reinterpret_cast<const f32x4*>(a.part_out + at * dh + d);
+      }
+      float m = top;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) m = fmaxf(m, st[u].x);
+      const float w0 = weight_of(top, m, a.c_log2);
+      total *= w0;
+      sum *= w0;
+      top = m;
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (c0 + u * step >= n_chunks) continue;
+        const float w = weight_of(st[u].x, m, a.c_log2);
+        total += st[u].y * w;
+        sum += x[u] * w;
+      }
+    }
+  };
+  if (n_chunks <= kAtOnce) {
+    // few chunks: a row to each group, and the rows of as many workgroups to the first of them
+    if (part % groups) return;
+    for (int r = part * rows_each + g; r < min(a.rows, (part + groups) * rows_each); r += groups) {
+      add(r, 0, 1);
+      put(r, sum, total);
+    }
+    return;
   }
-  sums[t] = sum;
-  if (l == 0) stats[g] = make_float2(top, total);
-  __syncthreads();
-  if (g != 0 || 4 * l >= dh) return;
-  for (int o = 1; o < groups; ++o) {
-    const float2 st = stats[o];
-    const float m = fmaxf(top, st.x), w0 = weight_of(top, m, a.c_log2), w1 = weight_of(st.x, m, a.c_log2);
-    top = m;
-    total = total * w0 + st.y * w1;
-    sum = sum * w0 + sums[o * lanes + l] * w1;
+  const int end = min(a.rows, (part + 1) * rows_each);
+  for (int r = part * rows_each; r < end; ++r) {
+    add(r, g, groups);
+    sums[t] = sum;
+    if (l == 0) stats[g] = make_float2(top, total);
+    __syncthreads();
+    if (g == 0) {
+      float m = top;
+      for (int o = 1; o < groups; ++o) m = fmaxf(m, stats[o].x);
+      float w = weight_of(top, m, a.c_log2);
+      total *= w;
+      sum *= w;
+      for (int o = 1; o < groups; ++o) {
+        w = weight_of(stats[o].x, m, a.c_log2);
+        total += stats[o].y * w;
+        sum += sums[o * lanes + l] * w;
+      }
+      put(r, sum, total);
+    }
+    if (r + 1 < end) __syncthreads();  // before the next row's
   }
-  const f32x4 x = sum * (total == 0.f ? 0.f : 1.f / total);
-  store_row4<typename std::conditional<F32, float, __bf16>::type>(a, b, h, r, 4 * l, x);
 }
 
 // ------------------------------------------------------------------ host side
@@ -1131,6 +1178,7 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.step = tile_of(wide);
     a.row_waves = a.rows > 128 ? kTreeWaves : kTreeWaves / 2;
     w.unit_rows = 32 * a.row_waves;
+    a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
     a.target = 256;
     a.least = 4;
   } else {
@@ -1140,11 +1188,13 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.row_waves = 1;
     while (a.row_waves < waves && a.row_waves < blocks) a.row_waves *= 2;
     w.unit_rows = 16 * w.nt * a.row_waves;
-    a.target = 1024;
+    a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
+    // Strands of few sequences have equal chunks: as many workgroups as run at once (131071 places: 59 us, with twice as many
+    // 63.7).  Chunks of many sequences' differ: twice as many even out (64 sequences of 200-8192 places: 73 us, 78.5).
+    a.target = (int64_t)a.batch * a.c.heads * a.row_blocks <= 256 ? 512 : 1024;
     a.least = 8;
   }
   const int waves = w.tree ? kTreeWaves : kWaves;
-  a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
   const int64_t strands = (int64_t)a.c.heads * a.row_blocks;
   const int64_t steps = std::max<int64_t>(1, ((int64_t)a.max_places + a.step - 1) / a.step);
   if (a.batch * steps * strands >= (int64_t(1) << 31))
@@ -1212,8 +1262,12 @@ extern "C" SN_API int spectral_cache_attend(const sn_cache* cache, const sn_atte
     launch1<256>(a, w, e5m2, f32, st);
   if (int rc = sn::launched("attention")) return rc;
   if (w.bytes > 0) {
-    const dim3 g((uint32_t)((int64_t)a.batch * a.drafts * p->q_heads));
-    f32 ? join_kernel<true><<<g, 256, 0, st>>>(a, w.unit_rows) : join_kernel<false><<<g, 256, 0, st>>>(a, w.unit_rows);
+    // about 512 workgroups
+    const int64_t all = (int64_t)a.batch * a.c.heads * a.rows;
+    const int rows_each = (int)std::min<int64_t>(a.rows, std::max<int64_t>(1, all / 512));
+    const dim3 g((uint32_t)((int64_t)a.batch * a.c.heads * ((a.rows + rows_each - 1) / rows_each)));
+    f32 ? join_kernel<true><<<g, 256, 0, st>>>(a, w.unit_rows, rows_each)
+        : join_kernel<false><<<g, 256, 0, st>>>(a, w.unit_rows, rows_each);
     return sn::launched("join");
   }
   return SN_OK;
