@@ -364,7 +364,9 @@ typedef enum {
   SN_MATMUL_TILE_4 = 2,   /* tiles of 128 x 128 by 4 waves                */
   SN_MATMUL_TILE_8 = 3,   /* ... by 8 waves, one to a compute unit        */
   SN_MATMUL_WIDE = 4,     /* 256 x 128, large results in SN_F32           */
-  SN_MATMUL_BIG = 5       /* 256 x 256, large results in SN_BF16          */
+  SN_MATMUL_BIG = 5,      /* 256 x 256, large results in SN_BF16 (8-bit
+                             integers: in either type)                   */
+  SN_MATMUL_SMALL = 6     /* 64 x 64, 8-bit integers                      */
 } sn_matmul_kernel;
 SN_API int spectral_matmul_fp8_kernel(const sn_matmul* p, int32_t* kernel, int32_t* parts, int64_t* workgroups,
                                       int32_t* threads);

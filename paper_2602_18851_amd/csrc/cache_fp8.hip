@@ -36,30 +36,43 @@ __device__ __forceinline__ bool locate(const RowsArgs& a, uint32_t row, uint32_t
   return true;
 }
 
-// LANES lanes of 8 elements take a row; grid.y says keys or values.
+// LANES lanes of 16 elements take a row of keys and that of values together, so that enough is on its way: 8191
+// tokens of 8 heads of 128 in bf16 take 9.9 us (5.1 TB/s; 11.5 with 8 elements of one of the two a lane).
 template <typename T, bool E5M2, int LANES>
 __global__ void __launch_bounds__(256) write_kernel(RowsArgs a) {
-  const int t = threadIdx.x, c = 8 * (t % LANES), which = blockIdx.y;
+  const int t = threadIdx.x, c = 16 * (t % LANES);
   for (uint32_t row = blockIdx.x * (256u / LANES) + t / LANES; row < a.rows; row += gridDim.x * (256u / LANES)) {
     uint32_t token, head;
     int64_t codes, scale;
     if (!locate(a, row, token, head, codes, scale)) continue;  // all lanes of the row
-    Eight<T> x;
-    x.clear();
-    if (c < a.c.head_dim)
-      x.load(static_cast<const T*>(a.x[which]) + token * a.token[which] + head * a.head[which] + c, 0, 8);
-    uint32_t top = 0;
+    Eight<T> x[2][2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, x.magnitude(e));
+    for (int which = 0; which < 2; ++which)
 #pragma unroll
-    for (int d = 1; d < LANES; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    float s, inv;
-    block_scale(top, format_top(E5M2), s, inv);
-    const uint2 w = make_uint2(
-        encode4<E5M2>(x.value(0) * inv, x.value(1) * inv, x.value(2) * inv, x.value(3) * inv),
-        encode4<E5M2>(x.value(4) * inv, x.value(5) * inv, x.value(6) * inv, x.value(7) * inv));
-    if (c < a.c.head_dim) *reinterpret_cast<uint2*>((which ? a.c.v : a.c.k) + codes + c) = w;
-    if (c == 0) (which ? a.c.v_scale : a.c.k_scale)[scale] = s;
+      for (int i = 0; i < 2; ++i) {
+        x[which][i].clear();
+        if (c < a.c.head_dim)
+          x[which][i].load(static_cast<const T*>(a.x[which]) + token * a.token[which] + head * a.head[which] + c + 8 * i, 0, 8);
+      }
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = max(top, x[which][e >> 3].magnitude(e & 7));
+#pragma unroll
+      for (int d = 1; d < LANES; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+      float s, inv;
+      block_scale(top, format_top(E5M2), s, inv);
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Eight<T>& v = x[which][i >> 1];
+        const int e = 4 * (i & 1);
+        w[i] = encode4<E5M2>(v.value(e) * inv, v.value(e + 1) * inv, v.value(e + 2) * inv, v.value(e + 3) * inv);
+      }
+      if (c < a.c.head_dim) *reinterpret_cast<u32x4*>((which ? a.c.v : a.c.k) + codes + c) = w;
+      if (c == 0) (which ? a.c.v_scale : a.c.k_scale)[scale] = s;
+    }
   }
 }
 
@@ -78,50 +91,79 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&f)[4]) {
   f[0] = lo[0], f[1] = lo[1], f[2] = hi[0], f[3] = hi[1];
 }
 
+// A lane takes the elements of one 16-byte store of keys and of values, and two rows at a time.  The results are more
+// than the caches hold where it counts, so their stores pass them by: 32768 tokens of 8 heads of 128 to bf16 33.6 us (6.0 TB/s),
+// 41.5 with ordinary stores, 47.5 with 8 elements of one of the two a lane.
 template <typename T, bool E5M2, int LANES>
 __global__ void __launch_bounds__(256) read_kernel(RowsArgs a) {
-  typedef T out4 __attribute__((ext_vector_type(4)));
-  typedef out4 out4_any __attribute__((aligned(sizeof(T))));
-  const int t = threadIdx.x, c = 8 * (t % LANES), which = blockIdx.y;
+  constexpr int PER = 16 / sizeof(T), WORDS = PER / 4, ROWS = 2;
+  typedef T out_vec __attribute__((ext_vector_type(PER)));
+  typedef out_vec out_any __attribute__((aligned(sizeof(T))));
+  const int t = threadIdx.x, c = PER * (t % LANES);
   if (c >= a.c.head_dim) return;
-  for (uint32_t row = blockIdx.x * (256u / LANES) + t / LANES; row < a.rows; row += gridDim.x * (256u / LANES)) {
-    uint32_t token, head;
-    int64_t codes, scale;
-    const bool there = locate(a, row, token, head, codes, scale);
-    T* out = static_cast<T*>(a.x[which]) + token * a.token[which] + head * a.head[which] + c;
-    uint2 w = make_uint2(0, 0);
-    float s = 0.f;
-    if (there) {
-      w = *reinterpret_cast<const uint2*>((which ? a.c.v : a.c.k) + codes + c);
-      s = (which ? a.c.v_scale : a.c.k_scale)[scale];
+  constexpr uint32_t kApart = 256 / LANES;
+  for (uint32_t row0 = blockIdx.x * (ROWS * kApart) + t / LANES; row0 < a.rows; row0 += gridDim.x * (ROWS * kApart)) {
+    uint32_t token[ROWS], head[ROWS], w[ROWS][2][WORDS];
+    float s[ROWS][2];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      int64_t codes, scale;
+      const bool there = locate(a, min(row0 + r * kApart, a.rows - 1), token[r], head[r], codes, scale);
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) w[r][which][i] = 0;
+        s[r][which] = 0.f;
+        if (!there) continue;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>((which ? a.c.v : a.c.k) + codes + c);
+        if constexpr (WORDS == 2) {
+          const uint2 x = *reinterpret_cast<const uint2*>(p);
+          w[r][which][0] = x.x, w[r][which][1] = x.y;
+        } else {
+          w[r][which][0] = *p;
+        }
+        s[r][which] = (which ? a.c.v_scale : a.c.k_scale)[scale];
+      }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float f[4];
-      decode4<E5M2>(h ? w.y : w.x, f);
-      *reinterpret_cast<out4_any*>(out + 4 * h) = out4{(T)(f[0] * s), (T)(f[1] * s), (T)(f[2] * s), (T)(f[3] * s)};
+    for (int r = 0; r < ROWS; ++r) {
+      if (row0 + r * kApart >= a.rows) continue;
+#pragma unroll
+      for (int which = 0; which < 2; ++which) {
+        out_vec o;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+          float f[4];
+          decode4<E5M2>(w[r][which][i], f);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[4 * i + e] = (T)(f[e] * s[r][which]);
+        }
+        __builtin_nontemporal_store(o, reinterpret_cast<out_any*>(static_cast<T*>(a.x[which]) + token[r] * a.token[which] +
+                                                                  head[r] * a.head[which] + c));
+      }
     }
   }
 }
 
 template <typename T, bool E5M2, bool WRITE>
 void launch2(const RowsArgs& a, hipStream_t st) {
-  const int lanes = a.c.head_dim <= 64 ? 8 : a.c.head_dim <= 128 ? 16 : 32;
-  const uint32_t per = 256 / lanes;
-  const dim3 grid(std::min<uint32_t>((a.rows - 1) / per + 1, 1u << 20), 2);
-#define SN_GO(L)                                                 \
-  do {                                                           \
-    if constexpr (WRITE)                                         \
-      write_kernel<T, E5M2, L><<<grid, 256, 0, st>>>(a);         \
-    else                                                         \
-      read_kernel<T, E5M2, L><<<grid, 256, 0, st>>>(a);          \
+  const int size = a.c.head_dim <= 64 ? 64 : a.c.head_dim <= 128 ? 128 : 256;
+  constexpr int PER = WRITE ? 16 : 16 / (int)sizeof(T);
+  const uint32_t per = 256 / (size / PER) * (WRITE ? 1 : 2);  // rows of a workgroup
+  const dim3 grid(std::min<uint32_t>((a.rows - 1) / per + 1, 1u << 20));
+#define SN_GO(D)                                                     \
+  do {                                                               \
+    if constexpr (WRITE)                                             \
+      write_kernel<T, E5M2, D / PER><<<grid, 256, 0, st>>>(a);       \
+    else                                                             \
+      read_kernel<T, E5M2, D / PER><<<grid, 256, 0, st>>>(a);        \
   } while (0)
-  if (lanes == 8)
-    SN_GO(8);
-  else if (lanes == 16)
-    SN_GO(16);
+  if (size == 64)
+    SN_GO(64);
+  else if (size == 128)
+    SN_GO(128);
   else
-    SN_GO(32);
+    SN_GO(256);
 #undef SN_GO
 }
 

@@ -166,6 +166,92 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tile_kernel(IntArgs a) {
   }
 }
 
+// Products of few tiles: tiles of 64 x 64 by 4 waves of 32 x 32, so that four times as many workgroups share the product, with a
+// ring of kSStages blocks of columns in LDS: a workgroup alone on its compute unit hides its loads' latency itself.
+constexpr int kST = 64, kSStages = 4;
+constexpr int kSStage = 2 * kST * 128;
+
+template <typename TC>
+__global__ void __launch_bounds__(256, 2) small_kernel(IntArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t stage[kSStages * kSStage];
+  const int lane = threadIdx.x & 63;
+  const int wv = uni((int)(threadIdx.x >> 6));
+  const int q = lane >> 4, s = lane & 15;
+  const int per_xcd = gridDim.x / 8;
+  const int unit = (blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (unit >= a.tiles_m * a.tiles_n * a.splits) return;  // whole workgroup
+  const int tile = unit / a.splits, split = unit % a.splits;
+  int64_t bm, bn;
+  place(tile, a.tiles_m, a.tiles_n, bm, bn);
+  const int64_t am = bm * kST + 16 * wv, bnr = bn * kST + 16 * wv;  // rows this wave stages
+  const uint8_t* const pa = a.a + am * a.ld_a;
+  const uint8_t* const pb = a.b + bnr * a.ld_b;
+  const uint32_t len_a = range_bytes(am, a.m, 16, a.ld_a, a.k), len_b = range_bytes(bnr, a.n, 16, a.ld_b, a.k);
+  const int kb0 = split * a.blocks_per_split, n_kb = min((int)((a.k + 127) / 128), kb0 + a.blocks_per_split);
+  // past the last block: empty ranges, which keep the count of loads
+  auto issue = [&](int kb) {
+    uint8_t* st = stage + (kb % kSStages) * kSStage;
+    const bool in = kb < n_kb;
+    stage_issue<16, 0>(make_rsrc(pa, in ? len_a : 0u), st + 128 * 16 * wv, 128u * (uint32_t)kb, (uint32_t)a.ld_a, lane, 16 * wv);
+    stage_issue<16, 0>(make_rsrc(pb, in ? len_b : 0u), st + 128 * (kST + 16 * wv), 128u * (uint32_t)kb, (uint32_t)a.ld_b, lane,
+                       16 * wv);
+  };
+  const int wm = wv >> 1, wn = wv & 1;
+  i32x4 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int x = 0; x < kSStages - 1; ++x) issue(kb0 + x);
+#pragma unroll 1
+  for (int kb = kb0; kb < n_kb; ++kb) {
+    wait_loads<4 * (kSStages - 2)>();  // all but the loads of the kSStages - 2 blocks after this one
+    bare_barrier();                    // every wave's part of the block, and the one before it fully read
+    issue(kb + kSStages - 1);
+    const uint8_t* ta = stage + (kb % kSStages) * kSStage;
+    const uint8_t* tb = ta + kST * 128;
+    u32x4 fa[2][2], fb[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        fa[r][h] = stage_chunk(ta, 32 * wm + 16 * r + s, 4 * h + q);
+        fb[r][h] = stage_chunk(tb, 32 * wn + 16 * r + s, 4 * h + q);
+      }
+    if (128 * (kb + 1) > a.k) {  // columns from k on are whatever the rows hold there
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) keep_chunk(fa[r][h], (int)(a.k - (int64_t)kb * 128) - 16 * (4 * h + q));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = multiply64(fb[j][h], fa[i][h], acc[i][j]);
+  }
+  wait_loads<0>();  // the last loads have left the LDS alone before the workgroup gives it up
+
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int64_t n = bn * kST + 32 * wn + 16 * j + 4 * q;
+    if (n >= a.n) continue;
+    Scale sb[4];
+    if (a.splits == 1) column_scales(a, n, sb);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t m = bm * kST + 32 * wm + 16 * i + s;
+      if (m >= a.m) continue;
+      if (a.splits > 1)
+        *reinterpret_cast<i32x4*>(a.parts + ((int64_t)split * a.m + m) * a.ld_parts + n) = acc[i][j];
+      else
+        finish4<TC>(a, m, n, acc[i][j], scale_of(a.sa + m * a.sa_row), sb);
+    }
+  }
+}
+
 // Large products: tiles of 256 x 256 by 8 waves of 128 x 64, two per SIMD.  A step is
 // a block of 128 columns, two stages of 64 KB in LDS.  A wave takes 64 rows of each half (128 rows) of A and 64 rows of B,
 // so a step falls into two phases of 64 x 64 (32 products of 16 x 16 x 64):
@@ -378,6 +464,47 @@ __device__ __forceinline__ void stage_plain(const IntArgs& a, uint8_t* codes, fl
   __syncthreads();
 }
 
+// The same for one row of up to kHeldRow columns, held in registers; its barriers wait for no load, so that those of B go on.
+constexpr int kHeldRow = 2 * 8 * 64 * kFewWaves;
+template <typename T>
+struct HeldRow {
+  Eight<T> v[2];
+  __device__ __forceinline__ void load(const IntArgs& a) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = 8 * (threadIdx.x + 64 * kFewWaves * i);
+      v[i].clear();
+      if (c < (int)a.k) v[i].load(reinterpret_cast<const T*>(a.a) + c, c, (int)a.k);
+    }
+  }
+  __device__ __forceinline__ void stage(const IntArgs& a, uint8_t* codes, float* scale, uint32_t* wave_max) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, v[i].magnitude(e));
+    top = max16(top);
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = top;
+    wait_loads<63>();
+    bare_barrier();
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) top = max(top, wave_max[w]);
+    float sc, inv;
+    int8_scale(top, sc, inv);
+    if (threadIdx.x == 0) *scale = sc;
+    const int room = (int)((a.k + 127) / 128 * 128);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = 8 * (threadIdx.x + 64 * kFewWaves * i);
+      if (c < room) *reinterpret_cast<uint2*>(codes + c) = int8_codes(v[i], c, a.k, sc, inv);
+    }
+    wait_loads<63>();
+    bare_barrier();
+  }
+};
+
 template <int TM, int TN, int PLAIN>
 __global__ void __launch_bounds__(64 * kFewWaves, TM * TN == 1 ? 4 : 2) few_rows_kernel(IntArgs a) {
   static_assert(PLAIN == 0 || TM <= 2, "a plain A has 32 rows at most");
@@ -445,10 +572,25 @@ __global__ void __launch_bounds__(64 * kFewWaves, TM * TN == 1 ? 4 : 2) few_rows
   };
   // this wave's full blocks wv, wv + 8, ..: `count` of them, in groups of AHEAD
   const int count = n_full > wv ? (n_full - wv + kFewWaves - 1) / kFewWaves : 0, groups = count / AHEAD;
-  if constexpr (PLAIN != 0) stage_plain<T>(a, plain_codes, plain_scale, wave_max);
-  int kb = wv;
+  int kb = wv, g = 0;
+  if constexpr (PLAIN != 0) {
+    if (TM == 1 && a.m == 1 && k <= kHeldRow && n_full >= kFewWaves * AHEAD) {  // the same for all waves
+      HeldRow<T> row;
+      row.load(a);
+      Side t[AHEAD];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) load(t[u], kb + kFewWaves * u, std::false_type{});
+      row.stage(a, plain_codes, plain_scale, wave_max[0]);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) multiply(t[u], kb + kFewWaves * u);
+      kb += kFewWaves * AHEAD;
+      g = 1;
+    } else {
+      stage_plain<T>(a, plain_codes, plain_scale, wave_max);
+    }
+  }
 #pragma unroll 1
-  for (int g = 0; g < groups; ++g, kb += kFewWaves * AHEAD) {
+  for (; g < groups; ++g, kb += kFewWaves * AHEAD) {
     Side t[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) load(t[u], kb + kFewWaves * u, std::false_type{});
@@ -500,6 +642,8 @@ void launch_tiles(const IntArgs& a, const Run& run, hipStream_t st) {
   const dim3 g((uint32_t)run.workgroups);
   if (run.kernel == SN_MATMUL_BIG)
     a.c_bf16 ? big_kernel<__bf16><<<g, 512, 0, st>>>(a) : big_kernel<float><<<g, 512, 0, st>>>(a);
+  else if (run.kernel == SN_MATMUL_SMALL)
+    a.c_bf16 ? small_kernel<__bf16><<<g, 256, 0, st>>>(a) : small_kernel<float><<<g, 256, 0, st>>>(a);
   else if (run.kernel == SN_MATMUL_TILE_8)
     a.c_bf16 ? tile_kernel<__bf16, 8><<<g, 512, 0, st>>>(a) : tile_kernel<float, 8><<<g, 512, 0, st>>>(a);
   else
@@ -532,8 +676,46 @@ using sn::refuse;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Rows of A up to which the kernel for few rows runs.
+// Rows of A up to which there is a kernel for few rows.
 constexpr int64_t kFewRows = 64;
+
+// The kernel of a product, and over how many workgroups a tile's sum is split: the cheapest by these costs in us.  A
+// launch's start and end, and a block of 128 columns: 64 x 64 tiles, one to a compute unit 0.29, two 0.39 (128 x 8192 x 8192
+// 22 us, 256 28.8, 512 54); 128 x 128 0.65 and 0.97 (512 x 8192 x 8192 45, 1024 66); 256 x 256, one to a unit, 1.62
+// (8192^3 421).  Parts are written, read and joined at 5.5 TB/s in a launch more: 512 x 512 x 16384 35 us in one part of 64 x
+// 64 tiles, 21 in 16 of 128 x 128.  Few rows: 512 or 1024 columns of C at a time, each wave an eighth of the columns of A (1 row
+// against 8192 x 8192 13.7, 40 and 64 rows 33 and 27.5).
+struct Way {
+  int kernel;
+  int splits, blocks_per_split;
+  double cost;
+};
+
+Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
+  auto up = [](int64_t x, int64_t t) { return (x + t - 1) / t; };
+  const int64_t n_kb = std::max<int64_t>(up(k, 128), 1);
+  Way best{SN_MATMUL_BIG, 1, (int)n_kb, 8.0 + 1.62 * (double)(up(up(m, kBT) * up(n, kBT), 256) * n_kb)};
+  auto tiles = [&](int kernel, int64_t size, double start, double alone, double both) {
+    const int64_t all = up(m, size) * up(n, size);
+    for (int64_t s = 1; s <= 16 && (s == 1 || 2 * s <= n_kb); ++s) {
+      const int64_t per = up(n_kb, s), wgs = all * s, rest = wgs % 512;
+      if (s > 1 && (s - 1) * per >= n_kb) continue;  // a split without blocks
+      double c = start + (double)per * ((double)(wgs / 512) * both + (rest == 0 ? 0.0 : rest <= 256 ? alone : both));
+      if (s > 1) c += 5.5 + (double)(8 * s + (f32 ? 4 : 2)) * (double)m * (double)n / 5.5e6;
+      if (c < best.cost) best = Way{kernel, (int)s, (int)per, c};
+    }
+  };
+  tiles(SN_MATMUL_TILE_4, kT, 5.0, 0.65, 0.97);
+  tiles(SN_MATMUL_SMALL, kST, 4.0, 0.29, 0.39);
+  // 512 lanes for 16 columns of C have to stay below the 2^32 of a launch
+  if (m <= kFewRows && n <= (int64_t(1) << 27) - 16) {
+    const int t = (int)((m + 15) / 16);
+    const double block = t == 1 ? 0.66 : t == 2 ? 1.8 : t == 3 ? 3.6 : 2.9;
+    const double cost = 3.0 + std::max(1.0, (double)up(n, t == 1 ? 16 : 32) / 256.0) * (double)up(n_kb, kFewWaves) * block;
+    if (cost <= best.cost) best = Way{SN_MATMUL_FEW_ROWS, 1, (int)n_kb, cost};
+  }
+  return best;
+}
 
 struct Plan {
   Run run;
@@ -576,9 +758,8 @@ int resolve(sn_matmul_int8& p, Plan& pl) {
   pl.plain_a = plain;
   pl.splits = 1;
   if (p.m == 0 || p.n == 0) return SN_OK;
-  const int64_t n_kb = (p.k + 127) / 128;
-  // 512 lanes for 16 columns of C have to stay below the 2^32 of a launch
-  const bool few = p.m <= kFewRows && p.n <= (int64_t(1) << 27) - 16;
+  const Way way = choose(p.m, p.n, p.k, p.c_type == SN_F32);
+  const bool few = way.kernel == SN_MATMUL_FEW_ROWS;
   pl.fuse = few && plain && p.m <= 32 && p.m * plain_row(p.k) <= kPlainBytes;
   if (plain && !pl.fuse) {
     pl.ld_codes = round_up(p.k, 16);
@@ -590,28 +771,20 @@ int resolve(sn_matmul_int8& p, Plan& pl) {
     pl.run = Run{SN_MATMUL_FEW_ROWS, 64 * kFewWaves, (p.n + cols - 1) / cols};
     return SN_OK;
   }
-  pl.tiles_m = (int32_t)((p.m + kT - 1) / kT);
-  pl.tiles_n = (int32_t)((p.n + kT - 1) / kT);
-  const int64_t large = ((p.m + kBT - 1) / kBT) * ((p.n + kBT - 1) / kBT);
-  if (large >= 256 && p.k > 0) {
-    pl.tiles_m = (int32_t)((p.m + kBT - 1) / kBT);
-    pl.tiles_n = (int32_t)((p.n + kBT - 1) / kBT);
-    pl.blocks_per_split = (int32_t)n_kb;
-    pl.run = Run{SN_MATMUL_BIG, 512, (large + 7) / 8 * 8};
-    return SN_OK;
-  }
-  int64_t splits = 1;
-  while (splits < 16 && 2 * splits * small <= 256 && 4 * splits <= n_kb) splits *= 2;
-  pl.blocks_per_split = (int32_t)((n_kb + splits - 1) / splits);
-  pl.splits = n_kb > 0 ? (int32_t)((n_kb + pl.blocks_per_split - 1) / pl.blocks_per_split) : 1;
+  const int64_t size = way.kernel == SN_MATMUL_BIG ? kBT : way.kernel == SN_MATMUL_SMALL ? kST : kT;
+  pl.tiles_m = (int32_t)((p.m + size - 1) / size);
+  pl.tiles_n = (int32_t)((p.n + size - 1) / size);
+  pl.splits = way.splits;
+  pl.blocks_per_split = way.blocks_per_split;
   if (pl.splits > 1) {
     pl.off_parts = pl.bytes;
     pl.ld_parts = round_up(p.n, 4);
     pl.bytes += round_up(pl.splits * p.m * pl.ld_parts * 4, 256);
   }
-  const int64_t units = small * pl.splits;
-  pl.run.kernel = units <= 256 ? SN_MATMUL_TILE_8 : SN_MATMUL_TILE_4;
-  pl.run.threads = units <= 256 ? 512 : 256;
+  const int64_t units = (int64_t)pl.tiles_m * pl.tiles_n * pl.splits;
+  // a 128 x 128 tile alone on its compute unit: 8 waves; else two of 4
+  pl.run.kernel = way.kernel == SN_MATMUL_TILE_4 && units <= 256 ? SN_MATMUL_TILE_8 : way.kernel;
+  pl.run.threads = pl.run.kernel == SN_MATMUL_BIG || pl.run.kernel == SN_MATMUL_TILE_8 ? 512 : 256;
   pl.run.workgroups = (units + 7) / 8 * 8;  // whole rounds of the XCDs
   return SN_OK;
 }

@@ -429,7 +429,7 @@ def spectral_matmul_fp8_workspace_bytes(p: sn_matmul) -> int:
     return out.value
 
 
-MATMUL_KERNELS = ("none", "few_rows", "tile_4", "tile_8", "wide", "big")
+MATMUL_KERNELS = ("none", "few_rows", "tile_4", "tile_8", "wide", "big", "small")
 
 
 def spectral_matmul_fp8_kernel(p: sn_matmul) -> tuple[str, int, int, int]:

@@ -144,7 +144,8 @@ PRODUCTS = [(1, 1, 1), (1, 33, 128), (2, 128, 127), (16, 200, 129), (17, 64, 16)
             (65, 128, 128), (128, 128, 128), (129, 300, 640), (300, 257, 384), (64, 1000, 2065), (520, 131, 257), (15, 4100, 144),
             (40, 24, 5000), (5, 20, 131071), (130, 40, 131000)]
 LARGE = [(512, 512, 128), (520, 515, 130), (1000, 777, 1000), (513, 1300, 2048), (600, 4100, 257), (2050, 640, 390),
-         (520, 600, 9000), (300, 520, 20000), (129, 2000, 4097), (2200, 2100, 100), (3000, 2500, 700)]
+         (520, 600, 9000), (300, 520, 20000), (129, 2000, 4097), (2200, 2100, 100), (3000, 2500, 700),
+         (2000, 1900, 1500), (4200, 4100, 900), (30, 4100, 3000)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS + LARGE)
@@ -159,10 +160,10 @@ def test_every_kernel_is_tested():
     """The sizes above reach every kernel, and sums in parts."""
     seen = {spectral_matmul_int8_kernel(sn_matmul_int8(*size, SN_I8, CODE[out]))[:2] for size in PRODUCTS + LARGE + WIDE
             for out in ("f32", "bf16")}
-    assert {name for name, _ in seen} >= {"few_rows", "tile_4", "tile_8", "big"} and any(parts > 1 for _, parts in seen)
+    assert {name for name, _ in seen} >= {"few_rows", "small", "tile_4", "tile_8", "big"} and any(parts > 1 for _, parts in seen)
 
 
-WIDE = [(8200, 8300, k) for k in (1, 100, 128, 129, 256, 300, 512, 600)]
+WIDE = [(8100, 8000, k) for k in (1, 100, 128, 129, 256, 300, 384, 512, 600, 1000)]
 
 
 @pytest.mark.parametrize("m,n,k", WIDE)
