@@ -682,7 +682,10 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
   const uint32_t k_off = k_at < dh ? (uint32_t)(k_place * dh + k_at) : kNowhere;
   const uint32_t v_off = v_at < dh ? (uint32_t)(4 * v_four * dh + v_at) : kNowhere;
   auto from = [](const void* p) { return make_rsrc(p, 0x7fffffffu); };
-  auto load_k = [&](int i) {  // in order
+  // Where tile i's keys (in order) and values are: scalar work, which goes with the matrix cores'.
+  const uint8_t *k_from, *v_from;
+  const float *ks_from, *vs_from;
+  auto find_k = [&](int i) {
     if (i / kWindow != window) {
       ++window;
       ids_before = ids;
@@ -692,20 +695,25 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     int64_t page;
     int in;
     locate(i, page, in);
-    kc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                       from(a.c.k + page * a.c.code_page + (int64_t)in * dh), k_off, 0, 0));
-    ks = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from(a.c.k_scale + page * a.c.scale_page + in),
-                                                              4u * (uint32_t)k_place, 0, 0));
+    k_from = a.c.k + page * a.c.code_page + (int64_t)in * dh;
+    ks_from = a.c.k_scale + page * a.c.scale_page + in;
   };
-  auto load_v = [&](int i) {
+  auto find_v = [&](int i) {
     int64_t page;
     int in;
     locate(i, page, in);
-    const __amdgpu_buffer_rsrc_t r = from(a.c.v + page * a.c.code_page + (int64_t)in * dh);
+    v_from = a.c.v + page * a.c.code_page + (int64_t)in * dh;
+    vs_from = a.c.v_scale + page * a.c.scale_page + in;
+  };
+  auto load_k = [&]() {
+    kc = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from(k_from), k_off, 0, 0));
+    ks = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(from(ks_from), 4u * (uint32_t)k_place, 0, 0));
+  };
+  auto load_v = [&]() {
+    const __amdgpu_buffer_rsrc_t r = from(v_from);
 #pragma unroll
     for (int e = 0; e < 4; ++e) vc[e] = __builtin_amdgcn_raw_buffer_load_b32(r, v_off, (uint32_t)(e * dh), 0);
-    vs = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                       from(a.c.v_scale + page * a.c.scale_page + in), 16u * (uint32_t)v_four, 0, 0));
+    vs = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from(vs_from), 16u * (uint32_t)v_four, 0, 0));
   };
   // In LDS, rows of 128 bytes with their chunks of 16 swapped as staged tiles have them: K in parts of 64 elements, V^T in
   // parts of 64 places.
@@ -755,13 +763,14 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
                      __builtin_amdgcn_perm(x[3][j >> 1], x[2][j >> 1], sel));
     }
   };
+  // Tile i to LDS, and the tile that was found last on its way
   auto fill_k = [&](int i) {
     widen_k(i);
-    load_k(i + 1);
+    load_k();
   };
   auto fill_v = [&](int i) {
     widen_v(i);
-    load_v(i + 1);
+    load_v();
   };
 
   f32x16 acc[DB], zero;
@@ -837,7 +846,11 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, st[n][e]);
-    m = fmaxf(m, __shfl_xor(m, 32));
+    {
+      // the other half's maximum
+      const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+      m = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+    }
     if (__ballot((m - top) * c_log2 > kSlack)) {
       m = fmaxf(m, top);
       const float w = weight_of(top, m, c_log2);
@@ -897,31 +910,40 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
 
   if (count > 0) {
     const int behind = wv >> 2;
-    load_k(0);
-    load_v(0);
+    find_k(0);
+    load_k();
+    find_v(0);
+    load_v();
     widen_k(0);
-    load_k(1);
+    find_k(1);
+    load_k();
     if constexpr (PARTS == 1) {
       widen_v(0);
-      load_v(1);
+      find_v(1);
+      load_v();
     }
     meet();
     if (behind) {
       if constexpr (PARTS == 2) {
+        find_v(1);
         fill_v(0);
+        find_k(2);
         fill_k(1);
       }
       meet();
     }
+    if constexpr (PARTS == 2) find_v(1 + behind);
+    find_k(2 + (PARTS == 2 ? behind : 0));
     read_keys(0, 0);
     read_keys(0, 4);
     multiply_keys(0);
     multiply_keys(4);
     meet();
-    auto multiply_part = [&](int k) {
+    auto multiply_part = [&](int k, auto find) {
+      __builtin_amdgcn_s_setprio(0);
       if constexpr (PARTS == 2) read_values(k);
-      __builtin_amdgcn_s_setprio(1);
       multiply_values(0);
+      find();
       __builtin_amdgcn_sched_barrier(0);
       read_keys(k + 1, 0);
       multiply_values(4);
@@ -930,7 +952,7 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
       if (edge) poison(k);
       multiply_keys(0);
       multiply_keys(4);
-      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_s_setprio(1);  // of the vector part: few of its instructions are ready at a time
       meet();
     };
 #pragma unroll 1
@@ -940,20 +962,24 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
         weights(2 * i);
         read_values(2 * i);
         meet();
-        multiply_part(2 * i);
+        multiply_part(2 * i, [&]() { find_v(i + 2); });
         fill_v(i + 1);
         weights(2 * i + 1);
         read_values(2 * i + 1);
         meet();
-        multiply_part(2 * i + 1);
+        multiply_part(2 * i + 1, [&]() { find_k(i + 3); });
       } else {
         fill_v(i + behind);
         fill_k(i + 1 + behind);
         weights(i);
         meet();
-        multiply_part(i);
+        multiply_part(i, [&]() {
+          find_k(i + 3 + behind);
+          find_v(i + 2 + behind);
+        });
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     if (!behind) meet();
   }
 
