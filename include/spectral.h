@@ -498,14 +498,16 @@ SN_API int spectral_cache_read(const sn_cache* cache, int32_t dtype, int64_t tok
  * largest; with SN_BF16 the weights to 2^-16.  Sums are float32.  The
  * same call gives the same bits.  Calls that can run at the same time need
  * workspaces of their own, graphs captured from them too; the workspace depends on the sizes
- * here, not on lengths, which a graph may change between replays.  batch = 0 does nothing. */
+ * here, not on lengths, which a graph may change between replays.  batch = 0 does nothing.  batch *
+ * table_cols * page * heads stays below 2^36 (with drafts * q_heads / heads above 64 or so: by
+ * their 64th or 256th part less). */
 typedef struct {
   int32_t dtype;       /* SN_F32 or SN_BF16, of q and out                            */
   int32_t batch;       /* 0 .. 2^20                                                  */
   int32_t drafts;      /* 1 .. 64 tokens of each sequence                            */
   int32_t q_heads;     /* a multiple of the cache's heads                            */
   int32_t table_cols;  /* pages of the longest sequence; times page below 2^31 - 128 */
-  float scale;         /* finite, positive                                           */
+  float scale;         /* positive, below 2e38                                       */
   int64_t q_batch, q_draft, q_head;
   int64_t out_batch, out_draft, out_head;
   int64_t table_ld, mask_batch;

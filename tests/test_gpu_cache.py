@@ -309,6 +309,47 @@ def test_drafts_that_are_not_finite_reach_who_sees_them(dtype, what, fmt):
             assert torch.equal(got[0, i], before[0, i])
 
 
+@pytest.mark.parametrize("drafts,group,dh", [(40, 2, 64), (40, 2, 128), (64, 4, 64), (64, 4, 128), (20, 6, 80), (30, 2, 64), (9, 2, 256)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_trees_with_drafts_that_are_not_finite(drafts, group, dh, fmt):
+    """Rows of NaN, one NaN code, pages that are not there, and tokens that see nothing, where the rows fill waves."""
+    c, q, table, lengths = setup((14, drafts, dh), 2, drafts, 1, group, dh, 16, [drafts + 61, drafts + 150], fmt=fmt)
+    masks = trees((14, drafts), drafts, 2)
+    masks[0, 5] = masks[1, 0] = 0
+    table[1, 3] = -1
+    before = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    check(before, q, c, table, lengths, masks)
+    bits = [int(m) >> 2 & 1 for m in masks[1]]  # who sees token 2 of the second sequence
+    place = 150 + 2
+    page, at = int(table[1, place // 16]), place % 16
+    c.v.view(torch.uint8)[page, 0, at, dh - 3] = 0x7F
+    got = c.attend(q, table, lengths, tree=gpu_masks(masks))
+    check(got, q, c, table, lengths, masks)
+    for i, sees in enumerate(bits):
+        assert torch.isnan(got[1, i, :, dh - 3]).all() == bool(sees)
+    other = torch.arange(dh, device="cuda") != dh - 3
+    assert torch.equal(got[..., other], before[..., other])
+    nan = torch.full((1, 1, dh), float("nan"), device="cuda")
+    for k, v in ((torch.zeros_like(nan), nan), (nan, torch.zeros_like(nan))):
+        c.write(k, v, torch.tensor([page * 16 + at], device="cuda"))
+        got = c.attend(q, table, lengths, tree=gpu_masks(masks))
+        for i, sees in enumerate(bits):
+            assert torch.isnan(got[1, i]).all() if sees else torch.equal(got[1, i], before[1, i])
+        assert torch.equal(got[0], before[0])
+
+
+@pytest.mark.parametrize("batch,drafts,group,dh,lengths", [
+    (66, 9, 8, 64, [20 + 3 * i for i in range(66)]), (3, 64, 3, 128, [70, 5000, 900]), (2, 64, 2, 64, [4000, 64]),
+    (130, 1, 2, 64, [1 + 7 * i for i in range(130)])])
+def test_many_rows_in_chunks(batch, drafts, group, dh, lengths):
+    """More than 64 sequences, and trees over sequences that workgroups share."""
+    c, q, table, lens = setup((15, batch, dh), batch, drafts, 1, group, dh, 32, lengths)
+    masks = trees((15, batch), drafts, batch)
+    got = c.attend(q, table, lens, tree=gpu_masks(masks))
+    check(got, q, c, table, lens, masks)
+    assert torch.equal(got, c.attend(q, table, lens, tree=gpu_masks(masks)))
+
+
 def test_a_place_that_is_not_finite_and_seen_by_all():
     c, q, table, lengths = setup((5,), 2, 2, 1, 2, 64, 16, [100, 100])
     before = c.attend(q, table, lengths)

@@ -173,7 +173,8 @@ BAD_CALLS = [
     (sp.SN_EINVAL, dict(drafts=0)), (sp.SN_EINVAL, dict(drafts=65)), (sp.SN_EINVAL, dict(q_heads=0)),
     (sp.SN_EINVAL, dict(q_heads=6)), (sp.SN_EINVAL, dict(q_heads=1 << 17)), (sp.SN_EINVAL, dict(table_cols=-1)),
     (sp.SN_EINVAL, dict(table_cols=(1 << 27) - 2)), (sp.SN_EINVAL, dict(scale=0.0)), (sp.SN_EINVAL, dict(scale=-1.0)),
-    (sp.SN_EINVAL, dict(scale=math.nan)), (sp.SN_EINVAL, dict(scale=math.inf)), (sp.SN_EINVAL, dict(q_batch=-1)),
+    (sp.SN_EINVAL, dict(scale=math.nan)), (sp.SN_EINVAL, dict(scale=math.inf)), (sp.SN_EINVAL, dict(scale=3e38)),
+    (sp.SN_EINVAL, dict(table_cols=1 << 26, batch=16)), (sp.SN_EINVAL, dict(q_batch=-1)),
     (sp.SN_EINVAL, dict(q_head=(1 << 40) + 1)), (sp.SN_EINVAL, dict(out_head=63)), (sp.SN_EINVAL, dict(out_draft=0)),
     (sp.SN_EINVAL, dict(out_batch=512)), (sp.SN_EINVAL, dict(out_draft=64)), (sp.SN_EINVAL, dict(table_ld=-1)),
     (sp.SN_EINVAL, dict(mask_batch=-1)), (sp.SN_EINVAL, dict(batch=1 << 20, q_heads=64, out_draft=4096, out_batch=8192))]
