@@ -207,6 +207,11 @@ __device__ __forceinline__ void store_row4(const AttendArgs& a, int b, int h, in
 // Waves of a workgroup of attend_kernel.
 constexpr int kWaves = 4;
 
+// Up to 64 rows of a key head (float32 queries and head_dim above 128: any number): bound by memory, so codes go straight
+// to registers.  Four waves of NT blocks of 16 rows; those with the same rows take every so many steps of the chunk, and
+// their results meet in LDS.  The keys of the next step are on their way while this one's weights are formed and its values
+// multiplied.  One token at the end of 131071 places, 8 key heads of 128 with 8 query heads each: 47-49 us (5.7 TB/s), and 10
+// for the join and its launch; with 8 waves to a workgroup, one on a compute unit in place of two, 81 us in all.
 // D: head_dim rounded up to 64, 128 or 256.  Lane q * 16 + s of a wave holds
 //   of K: places s of each of two groups of 16, bytes 16 q .. + 15 of every 64;
 //   of V: places 4 q .. 4 q + 3 of each group, D / 16 bytes from D / 16 s on;
@@ -601,7 +606,11 @@ __device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, c
 //   PARTS 2, both with each step: K of i + 1 and V of i are first read in 2 i + 2, K of i - 1 and V of i - 2 last in 2 i - 1;
 //   waves 0-3 write them in 2 i + 1, waves 4-7, a tile ahead, in 2 i.
 // Tiles past the last are loaded and written too, to no use, so that no load in flight meets a branch: the compiler would
-// wait for all of them there.
+// wait for all of them there (with branches 677 us in the case below, without 483).
+// 16 sequences of 64 tokens, 8 key heads of 128 with 8 query heads each, over 8000-8192 places: 385-412 us by the chip.  The matrix
+// products alone take 263 (1.55 PFLOP/s with P in two parts, at the clock that power leaves, the rate of a large bf16
+// product); one part of P 335, with twice the rounding error of the result's type.  Addresses are scalar work that
+// goes beside the matrix products (420 us with the vector part), whose waves have the lower priority.
 constexpr int tile_of(int d) { return 8192 / d; }
 
 template <int D, bool E5M2, int PARTS>
@@ -1130,7 +1139,6 @@ struct Way {
   int nt;         // blocks of 16 rows in a wave of attend_kernel
   int unit_rows;  // rows of a workgroup
   int64_t units;  // at most
-  int64_t slots;  // units that may write parts
   int64_t off_stat, bytes;
 };
 

@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tile_kernel(IntArgs a) {
 
 // Products of few tiles: tiles of 64 x 64 by 4 waves of 32 x 32, so that four times as many workgroups share the product, with a
 // ring of kSStages blocks of columns in LDS: a workgroup alone on its compute unit hides its loads' latency itself.
+// 1001 x 999 x 3001: 12 us, of which the host's part of a call is 9 (tiles of 128 x 128 in four parts: 20).
 constexpr int kST = 64, kSStages = 4;
 constexpr int kSStage = 2 * kST * 128;
 
@@ -268,6 +269,7 @@ __global__ void __launch_bounds__(256, 2) small_kernel(IntArgs a) {
 //   - a memory part ends with its reads complete, a barrier before any wave
 //     requests into their place.
 // Requests past the last step read nothing (an empty range) and keep the count.
+// 8192^3: 421-429 us (2.6 POP/s; tiles of 128 x 128 563), bound by power.
 constexpr int kBT = 256;
 constexpr int kBHalf = 128 * 128;
 constexpr int kBStage = 4 * kBHalf;  // A0, A1, B
@@ -418,7 +420,8 @@ __global__ void __launch_bounds__(256) join_kernel(IntArgs a) {
 // Few rows of A: every byte of B is used once or a few times, so B's rate from memory bounds the call, and B
 // goes straight to registers.  A workgroup takes 16 TN rows of B against all rows of A (16 TM), its 8 waves
 // every eighth block of columns each; their sums meet in LDS.  A plain A (PLAIN 1: bf16, 2: float32) that
-// fits LDS is quantised by every workgroup for itself, which saves a launch.
+// fits LDS is quantised by every workgroup for itself, which saves a launch.  One bf16 row against 8192 x 8192: 13.8 us
+// (4.9 TB/s); 16.4 when B was requested after the row was quantised.
 constexpr int kFewWaves = 8;
 constexpr int64_t kPlainBytes = 48 << 10;  // LDS for the codes of a plain A
 
