@@ -1215,9 +1215,10 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.row_waves = a.rows > 128 ? kTreeWaves : kTreeWaves / 2;
     w.unit_rows = 32 * a.row_waves;
     a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
-    // a chunk to each compute unit; with pairs of waves, shorter chunks even out (16 trees of 9 tokens, 72 rows, over 2000-8192
-    // places 100.5 -> 93 us; of 64 tokens 412 -> 480 with twice as many)
-    a.target = a.row_waves == kTreeWaves ? 256 : 512;
+    // A chunk to each compute unit.  With pairs of waves and strands of many sequences, whose chunks differ, shorter ones even out
+    // (16 trees of 9 tokens, 72 rows, over 2000-8192 places 93 us, 100.5 with 256; 3 of 12 over 2000-20000 53 and 47; of 64
+    // tokens, without pairs, 480 and 412).
+    a.target = a.row_waves == kTreeWaves || (int64_t)a.batch * a.c.heads * a.row_blocks <= 64 ? 256 : 512;
     a.least = 4;
   } else {
     w.nt = a.rows <= 16 || (a.c.head_dim > 128 && f32) ? 1 : 2;
