@@ -449,7 +449,8 @@ typedef struct {
   float* v_scale;
   int64_t pages;       /* >= 0, below 2^31                                           */
   int32_t heads;       /* 1 .. 65536                                                 */
-  int32_t page;        /* places of a page, a power of two, 16 .. 65536              */
+  int32_t page;        /* places of a page, a power of two, 16 .. 65536; heads * page
+                          below 2^31                                                 */
   int32_t head_dim;    /* a multiple of 16, 16 .. 256                                */
   int32_t format;      /* SN_E4M3 or SN_E5M2                                         */
   int64_t code_page;   /* elements from a page's codes to the next one's, and from its

@@ -224,6 +224,7 @@ int view_cache(const sn_cache* c, CacheView& view, bool need_memory) {
   if (c->heads < 1 || c->heads > 65536) return refuse(SN_EINVAL, "heads must be in [1, 65536]");
   if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1)))
     return refuse(SN_EINVAL, "page must be a power of two in [16, 65536]");
+  if ((int64_t)c->heads * c->page >= (int64_t(1) << 31)) return refuse(SN_EINVAL, "heads * page must stay below 2^31");
   if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16)
     return refuse(SN_EINVAL, "head_dim must be a multiple of 16 in [16, 256]");
   const int64_t scales = (int64_t)c->heads * c->page, codes = scales * c->head_dim;

@@ -48,6 +48,8 @@ class Fp8Cache:
                 raise ValueError(f"scales must be float32 tensors {list(k.shape[:3])} on the codes' device")
         if page < 16 or page & (page - 1) or page > 65536:
             raise ValueError("the page must be a power of two from 16 to 65536")
+        if not 1 <= heads <= 65536 or heads * page >= 1 << 31:
+            raise ValueError("heads must be in [1, 65536], and heads * page below 2^31")
         if dh % 16 or not 16 <= dh <= 256:
             raise ValueError("head_dim must be a multiple of 16 up to 256")
         far = []

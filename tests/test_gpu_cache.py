@@ -254,6 +254,27 @@ def test_a_long_sequence():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts", [1, 20])
+def test_pages_beyond_32_bits(drafts, dtype):
+    """A cache of more than 2^32 bytes of codes, its last pages in use: the bits of a small one."""
+    heads, page, dh = 8, 256, 128
+    pages = 17000
+    big = Fp8Cache.empty(pages, heads, page, dh)
+    small, q, table, lengths = setup((16, drafts), 2, drafts, heads, 8, dh, page, [1000, 300], dtype=dtype, junk=False)
+    far = torch.where(table >= 0, pages - 1 - table, table)
+    for b in range(2):
+        at = torch.arange(int(lengths[b]), device="cuda")
+        near = table[b].long()[at // page] * page + at % page
+        k, v = small.read(near, dtype=torch.float32)
+        slots = far[b].long()[at // page] * page + at % page
+        assert int(slots.max()) * heads * dh > 1 << 32
+        big.write(k, v, slots)
+        for x, y in zip(big.read(slots), small.read(near)):
+            assert torch.equal(x, y)
+    assert torch.equal(big.attend(q, far, lengths), small.attend(q, table, lengths))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_that_see_nothing(dtype):
     c, q, table, lengths = setup((1,), 4, 3, 2, 2, 64, 16, [3, 40, 0, 3], dtype=dtype)
     masks = np.zeros((4, 3), np.uint64)

@@ -252,6 +252,21 @@ def test_the_same_row_gives_the_same_bits_in_any_product():
         assert torch.equal(matmul_int8(quantize_int8(x[rows]), b, out_dtype=torch.float32), whole[rows])
 
 
+def test_matrices_beyond_32_bits():
+    """More than 2^32 elements: the bits of their last rows alone."""
+    rows, k = 40000, 110000
+    x = on_gpu(wide(rng(25), 1000, k), "bf16").repeat(rows // 1000, 1)
+    x[-3:] *= 2
+    m = quantize_int8(x)
+    last = quantize_int8(x[-200:].clone())
+    assert torch.equal(m.codes[-200:], last.codes) and torch.equal(m.scale[-200:], last.scale)
+    del x
+    b = matrix((25, 64), 64, k)
+    whole = matmul_int8(m, b, out_dtype=torch.float32)
+    assert torch.equal(whole[-200:], matmul_int8(last, b, out_dtype=torch.float32))
+    assert torch.equal(matmul_int8(b, m, out_dtype=torch.float32)[:, -200:], whole[-200:].t())  # as the other operand
+
+
 def test_products_of_nothing():
     a, b = quantize_int8(torch.zeros(3, 0, device="cuda")), quantize_int8(torch.zeros(100, 0, device="cuda"))
     assert (matmul_int8(a, b) == 0).all()

@@ -120,7 +120,7 @@ def cache(**kw):
 BAD_CACHES = [
     (sp.SN_EDTYPE, dict(format=sp.SN_F32)), (sp.SN_EINVAL, dict(pages=-1)), (sp.SN_EINVAL, dict(pages=1 << 31)),
     (sp.SN_EINVAL, dict(heads=0)), (sp.SN_EINVAL, dict(heads=65537)), (sp.SN_EINVAL, dict(page=8)),
-    (sp.SN_EINVAL, dict(page=48)), (sp.SN_EINVAL, dict(page=1 << 17)), (sp.SN_EINVAL, dict(head_dim=0)),
+    (sp.SN_EINVAL, dict(page=48)), (sp.SN_EINVAL, dict(page=1 << 17)), (sp.SN_EINVAL, dict(heads=32768, page=65536)), (sp.SN_EINVAL, dict(head_dim=0)),
     (sp.SN_EINVAL, dict(head_dim=72)), (sp.SN_EINVAL, dict(head_dim=272)), (sp.SN_EINVAL, dict(code_page=4080)),
     (sp.SN_EINVAL, dict(code_page=4104)), (sp.SN_EINVAL, dict(scale_page=60)), (sp.SN_EINVAL, dict(scale_page=66)),
     (sp.SN_EINVAL, dict(k=264)), (sp.SN_EINVAL, dict(v=264)), (sp.SN_EINVAL, dict(k_scale=260)),
