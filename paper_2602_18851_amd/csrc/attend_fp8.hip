@@ -218,7 +218,8 @@ constexpr int kWaves = 4;
 //   of S^T and P^T: those places of V for row s of each block;
 //   of O^T: for row s, D / 4 elements from D / 4 q on.
 template <int D, bool E5M2, bool F32, int NT>
-__global__ void __launch_bounds__(64 * kWaves, NT * D * (F32 ? 2 : 1) > 256 ? 1 : 2) attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(64 * kWaves, D == 256 || NT * D * (F32 ? 2 : 1) > 256 ? 1 : 2)
+attend_kernel(AttendArgs a) {
   constexpr int W = kWaves, KC = D / 64, VB = D / 16, QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
   constexpr int REGS = NT * (D / 4 + 2);  // of a wave's result: O, maximum, sum
   __shared__ float merge[W / 2][REGS][64];
@@ -1150,10 +1151,9 @@ void launch2(const AttendArgs& a, const Way& w, hipStream_t st) {
       return a.row_waves == kTreeWaves ? tree_kernel<D, E5M2, 1><<<g, 64 * kTreeWaves, 0, st>>>(a)
                                        : tree_kernel<D, E5M2, 2><<<g, 64 * kTreeWaves, 0, st>>>(a);
   }
-  if (w.nt == 1) return attend_kernel<D, E5M2, F32, 1><<<g, 64 * kWaves, 0, st>>>(a);
-  if constexpr (!(D == 256 && F32)) {
-    attend_kernel<D, E5M2, F32, 2><<<g, 64 * kWaves, 0, st>>>(a);
-  }
+  if constexpr (D != 256)
+    if (w.nt == 2) return attend_kernel<D, E5M2, F32, 2><<<g, 64 * kWaves, 0, st>>>(a);
+  attend_kernel<D, E5M2, F32, 1><<<g, 64 * kWaves, 0, st>>>(a);
 }
 
 template <int D>
@@ -1221,7 +1221,10 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.target = a.row_waves == kTreeWaves || (int64_t)a.batch * a.c.heads * a.row_blocks <= 64 ? 256 : 512;
     a.least = 4;
   } else {
-    w.nt = a.rows <= 16 || (a.c.head_dim > 128 && f32) ? 1 : 2;
+    // Sums of 256 elements fill the registers of a whole SIMD with 16 rows (8 sequences of 100-1500 places, 8 heads: 19.9 us;
+    // with two workgroups on a compute unit, half the registers and loads that wait, 23.0; 4 tokens each of 16 over
+    // 3500-4000: 54.7, with 32 rows a wave 61.8).
+    w.nt = a.rows <= 16 || wide == 256 ? 1 : 2;
     const int waves = kWaves, blocks = (a.rows + 16 * w.nt - 1) / (16 * w.nt);
     a.step = kStep;
     a.row_waves = 1;
@@ -1230,7 +1233,11 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
     a.row_blocks = (a.rows + w.unit_rows - 1) / w.unit_rows;
     // Strands of few sequences have equal chunks: as many workgroups as run at once (131071 places: 59 us, with twice as many
     // 63.7).  Chunks of many sequences' differ: twice as many even out (64 sequences of 200-8192 places: 73 us, 78.5).
-    a.target = (int64_t)a.batch * a.c.heads * a.row_blocks <= 256 ? 512 : 1024;
+    // Kernels of which one workgroup fits a compute unit: half as many for a single sequence (65536 places, 4 heads of 256:
+    // 43.5 us with 512, 33.9 with 256; f32, 4 tokens over 65536 places, 8 heads of 128: 58 and 49), the same for more, whose
+    // chunks differ (8 sequences of 500-4000 places, 8 tokens, 8 heads of 256: 64.4 us with 512, 75 with 256).
+    const bool alone = wide == 256 || (f32 && wide == 128 && w.nt == 2);
+    a.target = a.batch == 1 && alone ? 256 : (int64_t)a.batch * a.c.heads * a.row_blocks <= 256 ? 512 : 1024;
     a.least = 8;
   }
   const int waves = w.tree ? kTreeWaves : kWaves;

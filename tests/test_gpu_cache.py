@@ -227,7 +227,8 @@ def test_attention(shape, fmt, dtype, tree):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("batch,drafts,heads,group,dh,page,lengths", [
     (1, 1, 1, 8, 128, 64, [9001]), (3, 1, 2, 4, 64, 16, [5000, 300, 2049]), (2, 5, 1, 8, 128, 32, [4100, 257]),
-    (70, 1, 1, 2, 64, 16, [200 + 13 * i for i in range(70)]), (1, 64, 1, 8, 128, 256, [3000]), (2, 2, 1, 4, 256, 64, [2500, 2])])
+    (70, 1, 1, 2, 64, 16, [200 + 13 * i for i in range(70)]), (1, 64, 1, 8, 128, 256, [3000]), (2, 2, 1, 4, 256, 64, [2500, 2]),
+    (1, 6, 2, 5, 256, 32, [7001]), (3, 9, 1, 8, 208, 64, [3100, 1, 900]), (1, 3, 2, 8, 128, 64, [6000])])
 def test_sequences_in_chunks(batch, drafts, heads, group, dh, page, lengths, dtype):
     """Lengths at which workgroups share a sequence, beside short ones."""
     c, q, table, lens = setup((batch, drafts, dh), batch, drafts, heads, group, dh, page, lengths, dtype=dtype)
