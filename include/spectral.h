@@ -514,8 +514,8 @@ typedef struct {
   int64_t table_ld, mask_batch;
 } sn_attend;
 
-/* Device scratch (256-byte aligned) that the call needs, possibly 0.  Errors: SN_ENULL,
- * SN_EINVAL, SN_EDTYPE. */
+/* Device scratch (256-byte aligned) that the call needs, possibly 0: parts of results, and above 256 sequences
+ * how they are shared out.  Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE. */
 SN_API int spectral_cache_attend_workspace_bytes(const sn_cache* cache, const sn_attend* p, int64_t* bytes);
 
 /* Errors: SN_ENULL, SN_EINVAL, SN_EDTYPE, SN_ESTATE, SN_EHIP. */

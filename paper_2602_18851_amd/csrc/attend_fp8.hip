@@ -47,6 +47,7 @@ struct AttendArgs {
   int32_t strands;                // key heads times row_blocks
   int32_t target, least;          // workgroups to aim at, and the least steps of one
   float c_log2;                   // scale * log2(e)
+  uint32_t* plan;                 // [batch + 1] chunks of the sequences before each one, or NULL: every workgroup finds them
   float* part_out;                // [unit][rows of a workgroup][head_dim], where a sequence is split
   float2* part_stat;              // maximum and sum of each row
 };
@@ -58,7 +59,8 @@ constexpr float kNone = -__builtin_inff();
 // Lengths are known on the device only, and every workgroup derives the same plan from them: all sequences' steps (one
 // at least to a sequence), over `target` workgroups, give the steps of one (`least` at least, which hide its start and
 // end); a sequence is cut into as many equal chunks as come nearest to that, one at least.  A unit, a chunk of one
-// key head's rows, is one workgroup's.
+// key head's rows, is one workgroup's.  Of more than kScanned sequences plan_kernel forms the same plan once, and every
+// workgroup looks its chunk up: workgroups that scan all sequences grow with the square of their number.
 
 __device__ __forceinline__ int length_of(const AttendArgs& a, int b) { return min(max(a.lengths[b], 0), a.max_places); }
 
@@ -88,6 +90,11 @@ __device__ __forceinline__ uint32_t chunks_of(uint32_t steps, uint32_t per) {
   return steps == 0 ? 0u : max(1u, (steps + per / 2) / per);
 }
 
+// Steps that a unit should have, of all sequences'.
+__device__ __forceinline__ uint32_t per_of(const AttendArgs& a, uint32_t all) {
+  return max((all * (uint32_t)a.strands + (uint32_t)a.target - 1) / (uint32_t)a.target, (uint32_t)a.least);
+}
+
 struct Plan {
   uint32_t steps0;  // of sequence `lane`
   uint32_t per;     // steps that a unit should have
@@ -98,8 +105,63 @@ __device__ __forceinline__ Plan plan_of(const AttendArgs& a, int lane) {
   p.steps0 = steps_of(a, lane);
   uint32_t all = lane_of(scan64(p.steps0), 63);
   for (int b0 = 64; b0 < a.batch; b0 += 64) all += lane_of(scan64(steps_of(a, b0 + lane)), 63);
-  p.per = max((all * (uint32_t)a.strands + (uint32_t)a.target - 1) / (uint32_t)a.target, (uint32_t)a.least);
+  p.per = per_of(a, all);
   return p;
+}
+
+// The plan of many sequences, by one workgroup.  8 key heads of 128, 32-256 places each, one token: 512 sequences 70 us, 1024 137
+// and 4096 549, by workgroups that scan them all 88, 226 and 1994 (16384 of 256 places: 33.7 ms); 256 sequences 40 and 42, and
+// with one key head, where its launch counts, 13 and 10.5.
+constexpr int kScanned = 256;
+constexpr int kPlanWaves = 16, kPlanEach = 4;  // waves of its workgroup; sequences of a lane at a time
+
+__global__ void __launch_bounds__(64 * kPlanWaves) plan_kernel(AttendArgs a) {
+  __shared__ uint32_t sums[kPlanWaves];
+  const int t = threadIdx.x, lane = t & 63, wv = t >> 6;
+  // sums over the lanes up to and with each, and over all
+  auto scan = [&](uint32_t x, uint32_t& all) {
+    x = scan64(x);
+    __syncthreads();  // the sums before have been read
+    if (lane == 63) sums[wv] = x;
+    __syncthreads();
+    all = 0;
+    for (int w = 0; w < kPlanWaves; ++w) {
+      x += w < wv ? sums[w] : 0u;
+      all += sums[w];
+    }
+    return x;
+  };
+  uint32_t steps = 0, all;
+  for (int b = t; b < a.batch; b += 64 * kPlanWaves) steps += steps_of(a, b);
+  scan(steps, all);
+  const uint32_t per = per_of(a, all);
+  uint32_t base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += 64 * kPlanWaves * kPlanEach) {
+    const int b = b0 + kPlanEach * t;
+    uint32_t n[kPlanEach], mine = 0;
+#pragma unroll
+    for (int e = 0; e < kPlanEach; ++e) mine += n[e] = chunks_of(steps_of(a, b + e), per);
+    uint32_t at = base + scan(mine, all) - mine;
+#pragma unroll
+    for (int e = 0; e < kPlanEach; ++e) {
+      if (b + e < a.batch) a.plan[b + e] = at;
+      at += n[e];
+    }
+    base += all;
+  }
+  if (t == 0) a.plan[a.batch] = base;
+}
+
+// The sequence of chunk n of plan[batch]: each look of the 64 lanes leaves a 64th of the sequences.
+__device__ __forceinline__ int sequence_of(const AttendArgs& a, uint32_t n, int lane) {
+  int lo = 0, hi = a.batch;  // plan[lo] <= n < plan[hi]
+  while (hi - lo > 1) {
+    const int apart = (hi - lo + 63) / 64, at = lo + (lane + 1) * apart;
+    const uint64_t up_to = __ballot(at < hi && a.plan[min(at, hi)] <= n);
+    lo += __builtin_popcountll(up_to) * apart;
+    hi = min(hi, lo + apart);
+  }
+  return lo;
 }
 
 // The unit of this workgroup.
@@ -108,24 +170,36 @@ struct Unit {
 };
 
 __device__ __forceinline__ bool find_unit(const AttendArgs& a, int lane, Unit& u) {
-  const Plan p = plan_of(a, lane);
-  uint32_t base = 0, in = 0, steps = 0;
+  uint32_t in = 0, steps = 0, n = 0;  // in: units of the sequence before this one; n: its chunks
   int b = -1;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
-    const uint32_t mine = chunks_of(n, p.per) * (uint32_t)a.strands, sum = scan64(mine);
-    const uint64_t there = __ballot(blockIdx.x < base + sum);
-    if (there) {
-      const int at = __builtin_ctzll(there);
-      b = b0 + at;
-      steps = lane_of(n, at);
-      in = blockIdx.x - (base + lane_of(sum, at) - lane_of(mine, at));
-      break;
+  if (a.plan) {
+    const uint32_t at = blockIdx.x / (uint32_t)a.strands;
+    if (at >= a.plan[a.batch]) return false;
+    b = sequence_of(a, at, lane);
+    const uint32_t before = a.plan[b];
+    steps = steps_of(a, b);
+    n = a.plan[b + 1] - before;
+    in = blockIdx.x - before * (uint32_t)a.strands;
+  } else {
+    const Plan p = plan_of(a, lane);
+    uint32_t base = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+      const uint32_t s = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
+      const uint32_t mine = chunks_of(s, p.per) * (uint32_t)a.strands, sum = scan64(mine);
+      const uint64_t there = __ballot(blockIdx.x < base + sum);
+      if (there) {
+        const int at = __builtin_ctzll(there);
+        b = b0 + at;
+        steps = lane_of(s, at);
+        n = chunks_of(steps, p.per);
+        in = blockIdx.x - (base + lane_of(sum, at) - lane_of(mine, at));
+        break;
+      }
+      base += lane_of(sum, 63);
     }
-    base += lane_of(sum, 63);
+    if (b < 0) return false;
   }
-  if (b < 0) return false;
-  const uint32_t chunk = in / (uint32_t)a.strands, strand = in % (uint32_t)a.strands, n = chunks_of(steps, p.per);
+  const uint32_t chunk = in / (uint32_t)a.strands, strand = in % (uint32_t)a.strands;
   const uint32_t per = (steps + n - 1) / n;
   u.b = uni(b);
   u.h = uni((int)(strand % (uint32_t)a.c.heads));
@@ -1047,14 +1121,20 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int unit_rows, 
   const int t = threadIdx.x, lane = t & 63;
   const int per_head = (a.rows + rows_each - 1) / rows_each;
   const int part = blockIdx.x % per_head, h = blockIdx.x / per_head % a.c.heads, b = blockIdx.x / per_head / a.c.heads;
-  const Plan p = plan_of(a, lane);
-  const uint32_t steps = b < 64 ? lane_of(p.steps0, b) : (uint32_t)uni((int)steps_of(a, b));
-  const uint32_t n_chunks = chunks_of(steps, p.per);
-  if (n_chunks <= 1) return;  // whole workgroup: written already
-  uint32_t before = 0;        // units of the sequences before
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
-    before += lane_of(scan64(b0 + lane < b ? chunks_of(n, p.per) * (uint32_t)a.strands : 0u), 63);
+  uint32_t n_chunks, before = 0;  // before: units of the sequences before
+  if (a.plan) {
+    n_chunks = a.plan[b + 1] - a.plan[b];
+    if (n_chunks <= 1) return;  // whole workgroup: written already
+    before = a.plan[b] * (uint32_t)a.strands;
+  } else {
+    const Plan p = plan_of(a, lane);
+    const uint32_t steps = b < 64 ? lane_of(p.steps0, b) : (uint32_t)uni((int)steps_of(a, b));
+    n_chunks = chunks_of(steps, p.per);
+    if (n_chunks <= 1) return;  // whole workgroup: written already
+    for (int b0 = 0; b0 < b; b0 += 64) {
+      const uint32_t n = b0 == 0 ? p.steps0 : steps_of(a, b0 + lane);
+      before += lane_of(scan64(b0 + lane < b ? chunks_of(n, p.per) * (uint32_t)a.strands : 0u), 63);
+    }
   }
   const int dh = a.c.head_dim, lanes = dh <= 64 ? 16 : dh <= 128 ? 32 : 64, groups = 256 / lanes;
   const int l = t % lanes, g = t / lanes, d = min(4 * l, dh - 4);
@@ -1140,7 +1220,8 @@ struct Way {
   int nt;         // blocks of 16 rows in a wave of attend_kernel
   int unit_rows;  // rows of a workgroup
   int64_t units;  // at most
-  int64_t off_stat, bytes;
+  bool cut;       // whether a sequence may have several chunks
+  int64_t off_stat, off_plan, bytes;
 };
 
 template <int D, bool E5M2, bool F32>
@@ -1252,10 +1333,15 @@ int resolve(const sn_cache* cache, const sn_attend* p, AttendArgs& a, Way& w, bo
   if (w.units * 64 * waves >= (int64_t(1) << 32) ||
       (int64_t)a.batch * a.drafts * p->q_heads * 256 >= (int64_t(1) << 32))
     return refuse(SN_EINVAL, "batch * drafts * q_heads is too large");
-  w.off_stat = w.bytes = 0;
-  if (longest > 1) {
+  w.off_stat = w.off_plan = w.bytes = 0;
+  w.cut = longest > 1;
+  if (w.cut) {
     w.off_stat = (w.units * w.unit_rows * a.c.head_dim * 4 + 255) / 256 * 256;
     w.bytes = w.off_stat + (w.units * w.unit_rows * 8 + 255) / 256 * 256;
+  }
+  if (a.batch > kScanned) {
+    w.off_plan = w.bytes;
+    w.bytes += (((int64_t)a.batch + 1) * 4 + 255) / 256 * 256;
   }
   return SN_OK;
 }
@@ -1299,6 +1385,11 @@ extern "C" SN_API int spectral_cache_attend(const sn_cache* cache, const sn_atte
   a.masks = masks;
   a.part_out = static_cast<float*>(workspace);
   a.part_stat = reinterpret_cast<float2*>(static_cast<char*>(workspace) + w.off_stat);
+  if (a.batch > kScanned) {
+    a.plan = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + w.off_plan);
+    plan_kernel<<<1, 64 * kPlanWaves, 0, st>>>(a);
+    if (int rc = sn::launched("plan")) return rc;
+  }
   const bool f32 = p->dtype == SN_F32, e5m2 = cache->format == SN_E5M2;
   if (a.c.head_dim <= 64)
     launch1<64>(a, w, e5m2, f32, st);
@@ -1307,7 +1398,7 @@ extern "C" SN_API int spectral_cache_attend(const sn_cache* cache, const sn_atte
   else
     launch1<256>(a, w, e5m2, f32, st);
   if (int rc = sn::launched("attention")) return rc;
-  if (w.bytes > 0) {
+  if (w.cut) {
     // about 512 workgroups
     const int64_t all = (int64_t)a.batch * a.c.heads * a.rows;
     const int rows_each = (int)std::min<int64_t>(a.rows, std::max<int64_t>(1, all / 512));

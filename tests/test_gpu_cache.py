@@ -372,6 +372,47 @@ def test_many_rows_in_chunks(batch, drafts, group, dh, lengths):
     assert torch.equal(got, c.attend(q, table, lens, tree=gpu_masks(masks)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,drafts,group,dh,page", [(257, 1, 2, 64, 16), (700, 1, 8, 128, 32), (5000, 1, 1, 16, 16),
+                                                        (300, 9, 8, 64, 32), (600, 17, 8, 128, 16), (4161, 2, 2, 48, 64)])
+def test_more_sequences_than_are_scanned(batch, drafts, group, dh, page, dtype):
+    """Short sequences, one chunk each, have the bits of calls of 64 sequences; long ones among them are cut."""
+    heads, long = 2, 3000
+    c, _, rows, _ = setup((17, batch, dh), 2, 1, heads, group, dh, page, [long, 256], dtype=dtype)
+    r = rng(18, batch)
+    lens = r.integers(0, 257, batch)
+    which = np.ones(batch, int)
+    far = np.array([0, batch // 2, batch - 1])
+    lens[far], which[far] = long, 0
+    table = rows[torch.from_numpy(which).cuda()].contiguous()
+    lengths = torch.from_numpy(lens.astype(np.int32)).cuda()
+    q = on_gpu(r.standard_normal((batch, drafts, heads * group, dh)) * 0.7, dtype)
+    got = c.attend(q, table, lengths)
+    assert torch.equal(got, c.attend(q, table, lengths))
+    at = torch.from_numpy(far).cuda()
+    check(got[at], q[at], c, table[at], lengths[at])
+    near = torch.from_numpy(np.delete(np.arange(batch), far)).cuda()
+    for some in near.split(64):
+        assert torch.equal(got[some], c.attend(q[some], table[some, :256 // page], lengths[some]))
+
+
+def test_the_time_of_many_sequences_grows_as_they_do():
+    """Four times the sequences take about four times as long: 16 times when every workgroup looked at every sequence."""
+    c, _, rows, _ = setup((19,), 1, 1, 1, 1, 16, 16, [64])
+    times = []
+    for batch in (8192, 32768):
+        table, lengths = rows.expand(batch, -1).contiguous(), torch.full((batch,), 64, dtype=torch.int32, device="cuda")
+        q = on_gpu(rng(19, batch).standard_normal((batch, 1, 1, 16)), "bf16")
+        for _ in range(5):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            c.attend(q, table, lengths)
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+    assert min(times[5:]) < 9 * min(times[:5]), times
+
+
 def test_a_place_that_is_not_finite_and_seen_by_all():
     c, q, table, lengths = setup((5,), 2, 2, 1, 2, 64, 16, [100, 100])
     before = c.attend(q, table, lengths)
@@ -517,6 +558,28 @@ def test_calls_replay_from_a_graph():
         eager.write(k, v, slots)
         assert torch.equal(out, eager.attend(q, table, lengths))
         assert torch.equal(c.k.view(torch.uint8), eager.k.view(torch.uint8))
+
+
+def test_many_sequences_replay_from_a_graph():
+    """Their shares are formed anew at every replay, from the lengths of then."""
+    c, _, rows, _ = setup((24,), 1, 1, 2, 2, 64, 16, [2000])
+    r = rng(24)
+    table = rows.expand(300, -1).contiguous()
+    lengths = torch.zeros(300, dtype=torch.int32, device="cuda")
+    q = on_gpu(r.standard_normal((300, 1, 4, 64)), "bf16")
+    out, ws = torch.empty_like(q), torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    c.attend(q, table, lengths, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(q, table, lengths, out=out, workspace=ws)
+    for rep in range(4):
+        lengths.copy_(torch.from_numpy(np.where(r.random(300) < 0.05 * rep, 2000, r.integers(0, 300, 300)).astype(np.int32)))
+        ws.fill_(0xA5)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, c.attend(q, table, lengths))
 
 
 def test_two_streams_at_once():

@@ -213,6 +213,12 @@ def test_attention_workspace_is_bounded(lib):  # noqa: F811
     assert 0 < far < 1 << 28
 
 
+def test_many_sequences_have_a_plan_in_the_workspace(lib):  # noqa: F811
+    """Above 256 sequences the shares are found once, in 4 bytes for each sequence and 4 more, not by every workgroup."""
+    need = {b: sp.spectral_cache_attend_workspace_bytes(cache(), attend(batch=b, drafts=1, table_cols=1)) for b in (256, 257, 1 << 20)}
+    assert need == {256: 0, 257: 258 * 4 + 248, 1 << 20: 4 * (1 << 20) + 256}
+
+
 def test_python_refuses_tensors_of_the_host(lib):  # noqa: F811
     import torch
 
