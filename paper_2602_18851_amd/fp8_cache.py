@@ -2,7 +2,7 @@
 
 ``Fp8Cache`` checks torch tensors and passes them to spectral_cache_write, spectral_cache_read and spectral_cache_attend
 (include/spectral.h) on the current stream of the cache's device.  Autograd does not record the calls: a tensor that requires
-gradients is refused unless these are off.
+gradients, the cache's own and a given result among them, is refused unless these are off.
 """
 
 from __future__ import annotations
@@ -78,6 +78,10 @@ class Fp8Cache:
         scale = torch.zeros((2, pages, heads, page), dtype=torch.float32, device=device)
         return cls(codes[0], scale[0], codes[1], scale[1])
 
+    def _no_gradients(self) -> None:
+        if self.k_scale.requires_grad or self.v_scale.requires_grad or self.k.requires_grad or self.v.requires_grad:
+            refuse_autograd("a tensor of the cache")
+
     def _slots(self, slots: torch.Tensor, n: int) -> int:
         if slots.dtype != torch.int64 or tuple(slots.shape) != (n,) or slots.device != self.device \
                 or not slots.is_contiguous():
@@ -102,6 +106,7 @@ class Fp8Cache:
         / scale rounded to nearest even; a row that holds an infinity or a NaN becomes NaN.  Tokens whose slot is not in
         [0, pages * page) are padding and not written; the other slots must differ."""
         n = k.shape[0] if k.dim() == 3 else -1
+        self._no_gradients()
         on_stream_of(self.device, spectral_cache_write, self._c, _DTYPES.get(k.dtype, -1), n,
                      *self._rows(k, "k", k.dtype, n), *self._rows(v, "v", k.dtype, n), self._slots(slots, n))
 
@@ -110,6 +115,7 @@ class Fp8Cache:
         bfloat16); zeros for slots outside.  out: a pair of tensors of one type, any token and head strides without
         overlaps; new ones of dtype if None."""
         n = slots.shape[0] if slots.dim() == 1 else -1
+        self._no_gradients()
         if out is None:
             if dtype not in _DTYPES:
                 raise ValueError("dtype must be torch.float32 or torch.bfloat16")
@@ -138,6 +144,7 @@ class Fp8Cache:
             raise ValueError(f"q must be a float32 or bfloat16 tensor [batch, tokens, query heads, {dh}] on {dev}")
         if q.requires_grad:
             refuse_autograd("q")
+        self._no_gradients()
         batch, n, hq, _ = q.shape
         if not 1 <= n <= 64 or hq == 0 or hq % self.heads:
             raise ValueError(f"q must have 1 to 64 tokens and a multiple of {self.heads} heads")
@@ -172,6 +179,8 @@ class Fp8Cache:
             o_strides = out.stride()
             if o_strides[3] != 1:
                 raise ValueError("heads must be contiguous")
+            if out.requires_grad:
+                refuse_autograd("out")
         if batch == 0:
             return out
         if self.pages == 0:

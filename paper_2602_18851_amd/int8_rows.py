@@ -2,7 +2,8 @@
 
 ``quantize_int8`` and ``matmul_int8`` check torch tensors and pass them to spectral_quantize_int8 and
 spectral_matmul_int8 (include/spectral.h) on the current stream of the tensors' device.  Autograd does not record them:
-a tensor that requires gradients is refused unless these are off (torch.no_grad, or inside an autograd.Function).
+a tensor that requires gradients, a matrix's scale and a given result among them, is refused unless these are off
+(torch.no_grad, or inside an autograd.Function).
 """
 
 from __future__ import annotations
@@ -12,7 +13,7 @@ import functools
 import torch
 
 from .fp8_blocks import _PLAIN, _plain
-from .launch import on_stream_of
+from .launch import on_stream_of, refuse_autograd
 from .spectral import (SN_BF16, SN_F32, SN_I8, SN_STRIDE_ZERO, sn_matmul_int8, spectral_matmul_int8,
                        spectral_matmul_int8_workspace_bytes, spectral_quantize_int8)
 
@@ -91,7 +92,11 @@ def matmul_int8(a, b: Int8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: 
     run at the same time need their own."""
     if not isinstance(b, Int8Matrix):
         raise ValueError("b must be an Int8Matrix")
+    if b.scale.requires_grad:
+        refuse_autograd("b.scale")
     if isinstance(a, Int8Matrix):
+        if a.scale.requires_grad:
+            refuse_autograd("a.scale")
         codes, ld_a, m, k, sa, sa_row = a.codes, a.ld, a.rows, a.cols, a.scale.data_ptr(), _scale_stride(a)
     else:
         codes, ld_a, sa, sa_row = a, _plain(a, "a"), 0, 0
@@ -114,6 +119,8 @@ def matmul_int8(a, b: Int8Matrix, out_dtype: torch.dtype = torch.bfloat16, out: 
             raise ValueError("out must be row-major")
         if m <= 1:
             ld_c = n
+        if out.requires_grad:
+            refuse_autograd("out")
     if m == 0 or n == 0:
         return out
     kinds = (m, n, k, _TYPES[codes.dtype], _TYPES[out.dtype])

@@ -523,6 +523,34 @@ def test_refusals():
     assert c.read(slots[:0])[0].shape == (0, 2, 64)
 
 
+@pytest.mark.parametrize("which", ["k", "k_scale", "v", "v_scale"])
+def test_a_cache_that_requires_gradients_is_refused(which):
+    c, q, table, lengths = setup((25,), 2, 3, 2, 2, 64, 16, [50, 40])
+    ref = c.attend(q, table, lengths)
+    k, slots = torch.ones(4, 2, 64, device="cuda"), torch.arange(4, device="cuda") + c.pages * 16  # padding
+    getattr(c, which).requires_grad_()
+    for call in (lambda: c.write(k, k, slots), lambda: c.read(slots), lambda: c.attend(q, table, lengths)):
+        with pytest.raises(ValueError, match="gradients"):
+            call()
+        with torch.no_grad():
+            call()
+    with torch.no_grad():
+        assert torch.equal(c.attend(q, table, lengths), ref)
+
+
+def test_results_that_require_gradients_are_refused():
+    c, q, table, lengths = setup((26,), 2, 3, 2, 2, 64, 16, [50, 40], dtype="f32")
+    out = torch.zeros_like(q).requires_grad_()
+    with pytest.raises(ValueError, match="gradients"):
+        c.attend(q, table, lengths, out=out)
+    assert (out == 0).all()
+    with torch.no_grad():
+        assert torch.equal(c.attend(q, table, lengths, out=out), c.attend(q, table, lengths))
+    k, slots = torch.zeros(4, 2, 64, device="cuda"), torch.arange(4, device="cuda")
+    with pytest.raises(ValueError, match="gradients"):
+        c.read(slots, out=(k, k.clone().requires_grad_()))
+
+
 # ------------------------------------------------------- streams and graphs
 
 

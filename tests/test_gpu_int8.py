@@ -292,6 +292,21 @@ def test_refusals():
         quantize_int8(x.clone().requires_grad_())
 
 
+@pytest.mark.parametrize("which", ["a", "b", "out"])
+def test_scales_and_results_that_require_gradients_are_refused(which):
+    a, b = (quantize_int8(on_gpu(wide(rng(26, i), n, 40), "f32")) for i, n in enumerate((4, 6)))
+    ref = matmul_int8(a, b, out_dtype=torch.float32)
+    out = torch.zeros(4, 6, device="cuda", requires_grad=which == "out")
+    m = {"a": a, "b": b}.get(which)
+    if m is not None:
+        m.scale.requires_grad_()
+    with pytest.raises(ValueError, match="gradients"):
+        matmul_int8(a, b, out=out)
+    assert (out == 0).all()
+    with torch.no_grad():
+        assert torch.equal(matmul_int8(a, b, out=out), ref)
+
+
 # ------------------------------------------------------- streams and graphs
 
 
