@@ -488,7 +488,11 @@ SN_API int spectral_cache_read(const sn_cache* cache, int32_t dtype, int64_t tok
  * A token that sees nothing gets zeros.  A place whose page is not in [0, pages)
  * is not seen.  Query head h reads head h / (q_heads / heads) of the cache.  What a
  * place holds that a token does not see, NaN and infinities too, does not
- * reach its result; a row that is not finite makes NaN of who sees it.
+ * reach its result.  A NaN that it sees, as spectral_cache_write makes of a row that is
+ * not finite, does: of a key it makes the whole result NaN, of a value its element.
+ * Infinities are codes of SN_E5M2 that spectral_cache_write never stores.  Of a value that is seen
+ * they make its element NaN or an infinity; of a key the whole result NaN or, where the
+ * logit is minus infinity, a weight of zero.
  *   q        device, element e of head h of drafted token i of sequence b at
  *            b * q_batch + i * q_draft + h * q_head + e; out the same.
  *   table    device int32 [batch][table_ld] (0: table_cols), page numbers.

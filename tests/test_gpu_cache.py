@@ -423,6 +423,50 @@ def test_a_place_that_is_not_finite_and_seen_by_all():
     assert torch.isnan(got[0]).all() and torch.equal(got[1], before[1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts,group,dh", [(1, 4, 64), (3, 2, 128), (40, 2, 128), (64, 4, 64), (20, 2, 256)])
+@pytest.mark.parametrize("where", ["all", "drafted"])
+@pytest.mark.parametrize("code", [0x7C, 0xFC])
+def test_infinities_in_a_cache_written_elsewhere(drafts, group, dh, dtype, where, code):
+    """An infinite code, which E5M2 has, at a place that all see or one that only some see: no finite element of who sees it as a
+    value; as a key NaN, or the result without that place where its logit is minus infinity; nothing of the others changes."""
+    c, q, table, lengths = setup((27, drafts, dh), 1, drafts, 1, group, dh, 16, [drafts + 100], fmt="e5m2", dtype=dtype)
+    masks = trees((27, drafts), drafts)
+    tree = gpu_masks(masks)
+    place = 37 if where == "all" else 100 + drafts // 2
+    sees = np.array([where == "all" or bool(int(m) >> (drafts // 2) & 1) for m in masks])
+    sees = torch.from_numpy(sees).cuda()[:, None].expand(drafts, group)
+    page, at = int(table[0, place // 16]), place % 16
+    before = c.attend(q, table, lengths, tree=tree)[0]
+    check(before[None], q, c, table, lengths, masks)
+    kept = c.v.view(torch.uint8)[page, 0, at, 5].clone()
+    c.v.view(torch.uint8)[page, 0, at, 5] = code
+    got = c.attend(q, table, lengths, tree=tree)[0]
+    assert torch.equal(torch.isfinite(got[..., 5]), ~sees)
+    other = torch.arange(dh, device="cuda") != 5
+    assert torch.equal(got[..., other], before[..., other]) and torch.equal(got[~sees], before[~sees])
+    c.v.view(torch.uint8)[page, 0, at, 5] = kept
+    c.k.view(torch.uint8)[page, 0, at, 5] = code
+    got = c.attend(q, table, lengths, tree=tree)[0]
+    assert torch.equal(got[~sees], before[~sees])
+    nan = torch.isnan(got).all(dim=-1)
+    up = (q[0, :, :, 5] > 0) == (code == 0x7C)  # the logit is plus infinity
+    assert nan[sees & up].all() and not torch.isnan(got[~nan]).any()
+    if bool((sees & ~nan).any()):  # the sums of `check` over the other places
+        keys, values = c.read(table[0].long().repeat_interleave(16) * 16 + torch.arange(16, device="cuda").repeat(table.shape[1]),
+                              dtype=torch.float32)
+        n, t = int(lengths[0]), drafts
+        k, v = keys[:n, 0].double().cpu(), values[:n, 0].double().cpu()
+        for i, g in torch.nonzero(sees & ~nan).tolist()[:6]:
+            see = [p for p in range(n) if p != place and (p < n - t or int(masks[i]) >> (p - n + t) & 1)]
+            w = torch.softmax(k[see] @ q[0, i, g].double().cpu() * dh ** -0.5, dim=0)
+            reach = float((k[see].abs() @ q[0, i, g].double().cpu().abs()).max()) * dh ** -0.5
+            off = reach * (dh + 8) * 2.0 ** -23 + 2.0 ** -22
+            ref, mag = w @ v[see], w @ v[see].abs()
+            tol = mag * (2 * off * (1 + off) + 2.0 ** -16 + 2 * (n + 64) * 2.0 ** -23) + ref.abs() * 2.0 ** -8
+            assert ((got[i, g].double().cpu() - ref).abs() <= tol).all()
+
+
 def test_pages_that_are_not_there_are_not_seen():
     c, q, table, lengths = setup((6,), 2, 2, 2, 2, 64, 16, [100, 90])
     table[0, 2], table[1, 0], table[0, 6] = c.pages, -5, 1 << 30
