@@ -441,7 +441,9 @@ SN_API int spectral_matmul_int8(const sn_matmul_int8* p, const void* a, const fl
  * Places of tokens, in pages: codes [pages][heads][page][head_dim] and float32
  * scales [pages][heads][page], of keys and of values.  A row, the head_dim elements
  * of one place and head, has one scale, a power of two from 2^-126 on (or NaN):
- * element e is code[e] * scale.  Slot n is place n % page of page n / page. */
+ * element e is code[e] * scale.  Slot n is place n % page of page n / page.
+ * Other scales are not looked for: spectral_cache_read multiplies by whatever is there,
+ * spectral_cache_attend takes its power of two alone, and 1.5 is 1 to it. */
 typedef struct {
   void* k;             /* codes of keys, 16-byte aligned                             */
   float* k_scale;      /* their scales, 16-byte aligned                              */

@@ -31,7 +31,8 @@ def _workspace_bytes(heads, page, head_dim, fmt, dtype, batch, drafts, q_heads, 
 class Fp8Cache:
     """Keys and values of tokens in pages: ``k`` and ``v`` codes [pages, heads, page, head_dim] (torch.float8_e4m3fn or
     float8_e5m2), ``k_scale`` and ``v_scale`` float32 [pages, heads, page]: element e of a row is code[e] * scale, the scale
-    a power of two from 2^-126 on, or NaN.  page is a power of two from 16 on, head_dim a multiple of 16 up to 256.  A
+    a power of two from 2^-126 on, or NaN, as ``write`` makes them (others are not looked for: ``read`` multiplies by them,
+    ``attend`` takes their power of two alone).  page is a power of two from 16 on, head_dim a multiple of 16 up to 256.  A
     page is contiguous; pages may lie apart (the codes' pages of keys and of values equally far, and their scales').  Slot n
     is place n % page of page n // page."""
 

@@ -492,6 +492,19 @@ def test_scales_of_all_sizes():
     check(c.attend(q, table, lengths), q, c, table, lengths)
 
 
+@pytest.mark.parametrize("drafts,dtype", [(1, "bf16"), (1, "f32"), (40, "bf16")])
+def test_scales_between_powers_of_two(drafts, dtype):
+    """Of a cache written elsewhere: reading multiplies by them, attention takes the power of two."""
+    c, q, table, lengths = setup((28, drafts), 1, drafts, 1, 4, 64, 16, [drafts + 70], dtype=dtype, junk=False)
+    ref, slots = c.attend(q, table, lengths), torch.arange(c.pages * 16, device="cuda")
+    k, v = c.read(slots, dtype=torch.float32)
+    for t in (c.k_scale, c.v_scale):
+        t.mul_(1.5)
+    for got, x in zip(c.read(slots, dtype=torch.float32), (k, v)):
+        assert torch.equal(got, x * 1.5)  # codes of 4 bits: exact
+    assert torch.equal(c.attend(q, table, lengths), ref)
+
+
 def test_logits_far_apart():
     """Weights from 1 to none, and logits in the thousands."""
     c, q, table, lengths = setup((8,), 1, 1, 2, 4, 128, 16, [300], dtype="f32")
