@@ -697,8 +697,8 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
   constexpr int kMerge = PARTS == 1 ? 0 : kTreeWaves / 2 * REGS * 256;
   __shared__ __attribute__((aligned(16))) uint8_t tiles[4 * kBytes > kMerge ? 4 * kBytes : kMerge];  // K, K, V, V
   // which values of a tile that not all rows see are not finite (in LDS they are zeros): of places 4 f .. + 3 and elements
-  // 4 g .. + 3, bit 4 place + element of word [f][g]
-  __shared__ uint16_t bad[2][kTile * D / 16];
+  // 4 g .. + 3, bit 4 place + element of word [f][g]; looked through two words at a time
+  __shared__ __attribute__((aligned(4))) uint16_t bad[2][kTile * D / 16];
   const int lane = threadIdx.x & 63;
   const int wv = uni((int)(threadIdx.x >> 6));
   const int hi = lane >> 5, s = lane & 31;
