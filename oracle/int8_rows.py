@@ -32,9 +32,3 @@ def quantize(x) -> tuple[np.ndarray, np.ndarray]:
             rest = q - low
             codes[r, c] = low + (1 if rest > Fraction(1, 2) or (rest == Fraction(1, 2) and low % 2) else 0)
     return codes, scale
-
-
-def product(a, sa, b, sb) -> np.ndarray:
-    """sA sB times the whole sums, the sums exact, in float64 (2^-52 off)."""
-    sums = np.asarray(a, dtype=np.float64) @ np.asarray(b, dtype=np.float64).T
-    return sums * np.asarray(sa, dtype=np.float64)[:, None] * np.asarray(sb, dtype=np.float64)[None, :]

@@ -213,8 +213,6 @@ __device__ __forceinline__ bool find_unit(const AttendArgs& a, int lane, Unit& u
 
 // ---- arithmetic ------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t bits(__bf16 x) { return __builtin_bit_cast(uint16_t, x); }
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -257,7 +255,6 @@ __device__ __forceinline__ float quarters_sum(float x) {
   x += __shfl_xor(x, 16);
   return x + __shfl_xor(x, 32);
 }
-
 
 // A row's running maximum is raised, and its sums scaled, only when a logit is above it by a factor of 2^kSlack in weight: until
 // then weights are up to 2^kSlack, which float32 and bf16 hold as exactly.

@@ -667,7 +667,6 @@ void launch_few(const IntArgs& a, const Run& run, int plain, hipStream_t st) {
   switch (t) {
     case 1: return few_rows_kernel<1, 1, 0><<<g, W, 0, st>>>(a);
     case 2: return few_rows_kernel<2, 2, 0><<<g, W, 0, st>>>(a);
-    case 3: return few_rows_kernel<3, 2, 0><<<g, W, 0, st>>>(a);
     default: return few_rows_kernel<4, 2, 0><<<g, W, 0, st>>>(a);
   }
 }
@@ -679,15 +678,16 @@ using sn::refuse;
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Rows of A up to which there is a kernel for few rows.
-constexpr int64_t kFewRows = 64;
+// Whether there is a kernel for so few rows: 33 to 48 (40 rows 33 us against 8192 x 8192) are never
+// cheaper than the tiles of 64 x 64 (16.7).
+constexpr bool few_rows(int64_t m) { return m <= 32 || (m > 48 && m <= 64); }
 
 // The kernel of a product, and over how many workgroups a tile's sum is split: the cheapest by these costs in us.  A
 // launch's start and end, and a block of 128 columns: 64 x 64 tiles, one to a compute unit 0.29, two 0.39 (128 x 8192 x 8192
 // 22 us, 256 28.8, 512 54); 128 x 128 0.65 and 0.97 (512 x 8192 x 8192 45, 1024 66); 256 x 256, one to a unit, 1.62
 // (8192^3 421).  Parts are written, read and joined at 5.5 TB/s in a launch more: 512 x 512 x 16384 35 us in one part of 64 x
 // 64 tiles, 21 in 16 of 128 x 128.  Few rows: 512 or 1024 columns of C at a time, each wave an eighth of the columns of A (1 row
-// against 8192 x 8192 13.7, 40 and 64 rows 33 and 27.5).
+// against 8192 x 8192 13.7, 64 rows 27.5).
 struct Way {
   int kernel;
   int splits, blocks_per_split;
@@ -711,9 +711,9 @@ Way choose(int64_t m, int64_t n, int64_t k, bool f32) {
   tiles(SN_MATMUL_TILE_4, kT, 5.0, 0.65, 0.97);
   tiles(SN_MATMUL_SMALL, kST, 4.0, 0.29, 0.39);
   // 512 lanes for 16 columns of C have to stay below the 2^32 of a launch
-  if (m <= kFewRows && n <= (int64_t(1) << 27) - 16) {
+  if (few_rows(m) && n <= (int64_t(1) << 27) - 16) {
     const int t = (int)((m + 15) / 16);
-    const double block = t == 1 ? 0.66 : t == 2 ? 1.8 : t == 3 ? 3.6 : 2.9;
+    const double block = t == 1 ? 0.66 : t == 2 ? 1.8 : 2.9;
     const double cost = 3.0 + std::max(1.0, (double)up(n, t == 1 ? 16 : 32) / 256.0) * (double)up(n_kb, kFewWaves) * block;
     if (cost <= best.cost) best = Way{SN_MATMUL_FEW_ROWS, 1, (int)n_kb, cost};
   }

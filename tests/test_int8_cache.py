@@ -107,6 +107,17 @@ def test_products_of_nothing(lib):  # noqa: F811
         assert sp.spectral_matmul_int8_kernel(desc(**kw)) == ("none", 0, 0, 0)
 
 
+def test_rows_of_the_kernel_for_few(lib):  # noqa: F811
+    """33 to 48 rows never run it; the rows on either side do somewhere."""
+    def ways(m):
+        return {sp.spectral_matmul_int8_kernel(desc(m=m, n=n, k=k, c_type=c))[0] for n in (1, 500, 8192, 100000, 1 << 27)
+                for k in (1, 128, 1000, 1024, 1025, 8192, 131071) for c in (sp.SN_F32, sp.SN_BF16)}
+    for m in (1, 16, 17, 32, 49, 64):
+        assert "few_rows" in ways(m), m
+    for m in (33, 40, 48, 65):
+        assert "few_rows" not in ways(m), m
+
+
 # ------------------------------------------------------------------ refusals of the cache
 
 
