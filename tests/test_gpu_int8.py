@@ -178,6 +178,50 @@ def test_large_tiles_of_few_blocks(m, n, k, out):
     assert torch.equal(matmul_int8(*mats, out_dtype=TORCH[out]), ref.to(TORCH[out]))
 
 
+# sums in parts of every kind of tile, the last part's last block ragged, and few rows in blocks of 16 to 64
+SPLIT = [(66, 5451, 9963), (300, 4096, 14301), (65, 5458, 7692), (70, 4506, 9750), (130, 1000, 5001), (300, 2000, 7001)]
+FEW = [(16, 4000, 1000), (17, 4000, 500), (32, 8192, 1001), (49, 8000, 900), (50, 515, 1024), (64, 8192, 1000)]
+
+
+@pytest.mark.parametrize("m,n,k", SPLIT + FEW)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_products_in_parts_and_of_few_rows(m, n, k, out):
+    a, b = matrix((27, m, k), m, k), matrix((28, n, k), n, k, "strided")
+    assert same(matmul_int8(a, b, out_dtype=TORCH[out]), expected(a, b, out))
+
+
+def test_every_kernel_is_tested_in_parts():
+    for out in ("f32", "bf16"):
+        seen = {}
+        for size in SPLIT + FEW:
+            name, parts, _, _ = spectral_matmul_int8_kernel(sn_matmul_int8(*size, SN_I8, CODE[out]))
+            seen.setdefault((name, parts > 1), set()).add(-(-size[0] // 16))
+        assert {("tile_4", True), ("tile_8", True), ("small", True)} <= set(seen), seen
+        assert seen["few_rows", False] >= {1, 2, 4}, seen  # blocks of 16 rows
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(31, 8192, 1530), (32, 8192, 1400), (17, 4000, 2700), (300, 4096, 14301), (65, 5458, 7692)])
+def test_plain_operands_of_every_kernel(dtype, m, n, k):
+    """Rows whose codes fill the LDS of the kernel for few, and tiles whose sums are in parts."""
+    x = on_gpu(wide(rng(29, m, k), m, k), dtype)
+    b = matrix((30, n, k), n, k)
+    got = matmul_int8(x, b, out_dtype=torch.float32)
+    assert same(got, expected(quantize_int8(x), b, "f32"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("base", [32, 496, 2032, 8192])
+def test_rows_of_every_length_past_a_whole_one(dtype, base):
+    """1 to 16 columns past the last whole load."""
+    for cols in range(base + 1, base + 17):
+        x = on_gpu(wide(rng(31, cols), 3, cols), dtype)
+        check_quantized(quantize_int8(x), host(x))
+        room = torch.full((3, cols + 5), float("nan"), dtype=TORCH[dtype], device="cuda")
+        room[:, 3:3 + cols] = x
+        check_quantized(quantize_int8(room[:, 3:3 + cols]), host(x))
+
+
 @pytest.mark.parametrize("layout", ["strided", "one"])
 @pytest.mark.parametrize("m,n,k", [(5, 300, 700), (300, 260, 700), (1, 1, 100), (2100, 2200, 130), (70, 300, 6000)])
 def test_scales_of_any_strides(layout, m, n, k):
