@@ -372,6 +372,58 @@ def test_many_rows_in_chunks(batch, drafts, group, dh, lengths):
     assert torch.equal(got, c.attend(q, table, lens, tree=gpu_masks(masks)))
 
 
+LONG_CHUNKS = [
+    # trees, with pairs of waves and without: chunks of 20 tiles of 128 places in windows of 8, of 35 of 64 in windows of 16
+    (256, 9, 8, 64, 16, 5120, "bf16"), (128, 17, 8, 64, 32, 5120, "bf16"),
+    (256, 9, 8, 128, 64, 4480, "bf16"), (128, 17, 8, 128, 16, 4480, "bf16"),
+    # whole sequences of 70 and 20 tiles, whose shares are looked up
+    (512, 9, 8, 128, 16, 4480, "bf16"), (272, 17, 8, 64, 16, 2560, "bf16"),
+    # 137 to 140 steps a wave, with four, two and one of them to the same rows; pages are looked up 64 steps at a time
+    (512, 1, 8, 128, 64, 35200, "bf16"), (512, 1, 4, 64, 16, 35200, "f32"), (256, 3, 8, 256, 16, 17920, "bf16"),
+    (512, 8, 8, 64, 32, 17920, "bf16"), (256, 16, 8, 128, 16, 8960, "f32")]
+
+
+@pytest.mark.parametrize("batch,drafts,group,dh,page,length,dtype", LONG_CHUNKS)
+def test_long_chunks(batch, drafts, group, dh, page, length, dtype):
+    """So many sequences, copies of two, that a workgroup walks through several windows of page numbers, with pages that are not
+    there and a ragged end past the first window.  All copies have the same bits."""
+    c, q, table, lengths = setup((29, batch, dh), 2, drafts, 1, group, dh, page, [length, length - 333], dtype=dtype)
+    for b, at in ((0, 0.2), (0, 0.37), (0, 0.8), (1, 0.43), (1, 0.97)):  # parts of the sequence
+        table[b, int(at * length) // page] = -1
+    masks = trees((29, drafts), drafts, 2)
+    copy = torch.from_numpy(np.concatenate([[0, 1], rng(29, batch).integers(0, 2, batch - 2)])).cuda()
+    got = c.attend(q[copy], table[copy], lengths[copy], tree=gpu_masks(masks)[copy])
+    check(got[:2], q, c, table, lengths, masks)
+    assert torch.equal(got, got[:2][copy])
+
+
+@pytest.mark.parametrize("batch,drafts,group,dh,page,length,dtype", LONG_CHUNKS)
+def test_every_place_of_long_chunks_counts_once(batch, drafts, group, dh, page, length, dtype):
+    """Keys of zeros, so that every weight is 1, and values that are whole numbers: the mean over the places that are seen, of
+    exact sums below 2^24.  Rounded are the count's reciprocal, the product with it, and the result."""
+    c, q, table, lengths = setup((30, batch, dh), 2, drafts, 1, group, dh, page, [length, length - 333], dtype=dtype, junk=False)
+    c.k.view(torch.uint8).zero_()
+    c.k_scale.fill_(1.0), c.v_scale.fill_(1.0)
+    r = rng(30, batch, dh)
+    c.v.copy_(torch.from_numpy(r.integers(-16, 17, tuple(c.v.shape)).astype(np.float32)).cuda())
+    for b, at in ((0, 0.2), (0, 0.37), (0, 0.8), (1, 0.43), (1, 0.97)):
+        table[b, int(at * length) // page] = -1
+    masks = trees((30, drafts), drafts, 2)
+    copy = torch.from_numpy(np.concatenate([[0, 1], r.integers(0, 2, batch - 2)])).cuda()
+    got = c.attend(q[copy], table[copy], lengths[copy], tree=gpu_masks(masks)[copy])
+    assert torch.equal(got, got[:2][copy])
+    v = host(c.v.float())[:, 0]
+    for b in range(2):
+        n, ids = int(lengths[b]), table[b].cpu().numpy()
+        place = np.arange(n)
+        id_of = ids[place // page]
+        rows = np.where((id_of >= 0)[:, None], v[id_of, place % page], 0.0)
+        sees = np.concatenate([np.ones((drafts, n - drafts)), masks[b][:, None] >> np.arange(drafts, dtype=np.uint64) & np.uint64(1)], axis=1)
+        sees = sees * (id_of >= 0)
+        ref = (sees @ rows / sees.sum(axis=1, keepdims=True))[:, None, :]
+        assert (np.abs(host(got[b]) - ref) <= np.abs(ref) * (2.0 ** -8 * (dtype == "bf16") + 2.0 ** -22)).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("batch,drafts,group,dh,page", [(257, 1, 2, 64, 16), (700, 1, 8, 128, 32), (5000, 1, 1, 16, 16),
                                                         (300, 9, 8, 64, 32), (600, 17, 8, 128, 16), (4161, 2, 2, 48, 64)])
