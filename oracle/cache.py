@@ -55,3 +55,23 @@ def attend(q, k, v, table, lengths, masks=None, scale=None):
                     mag[b, i, h] = w @ np.abs(vs)
                     reach[b, i, h] = scale * (np.abs(ks) @ np.abs(q[b, i, h])).max()
     return out, mag, reach
+
+
+def weights(q, n, scale):
+    """softmax(scale q) over each row's first n elements, zeros after them: attention where place j has the key and the value
+    1 in element j.  q [rows, d], n [rows].  Returns (weights, the largest |scale q| of each row)."""
+    q = np.asarray(q, dtype=np.float64)
+    there = np.arange(q.shape[1]) < np.asarray(n)[:, None]
+    s = np.where(there, scale * q, -np.inf)
+    w = np.exp(s - s.max(axis=1, keepdims=True))
+    return w / w.sum(axis=1, keepdims=True), np.abs(np.where(there, scale * q, 0.0)).max(axis=1)
+
+
+def weights_off(reach, bf16=False):
+    """How far such weights may be off, relative to themselves, of up to 32 places.  Logits: parts of q whose sum is q to 2^-26, two
+    additions in the matrix cores (2^-23 each), the factor scale log2(e) (three roundings), the exponent's and the maximum's
+    rounding: less than 4.5 2^-23 of `reach`.  Its power 2^-23.  Both for the weight and for the sum of the weights, which takes ten
+    additions more (2^-24 each); three parts of a weight, added (2^-23 twice); the sum's reciprocal and the product with it.
+    For a bf16 result weights are two parts (2^-18), and sums of more rows take 26 additions more."""
+    off = (9.0 * reach + 11.0) * 2.0 ** -23
+    return off + 13.0 * 2.0 ** -23 + 2.0 ** -18 if bf16 else off

@@ -565,6 +565,33 @@ def test_logits_far_apart():
     check(c.attend(q, table, lengths, scale=0.03), q, c, table, lengths, scale=0.03)
 
 
+@pytest.mark.parametrize("size", [0.5, 30.0])
+@pytest.mark.parametrize("drafts,group,dh,dtype", [
+    (1, 1, 64, "f32"), (1, 8, 128, "f32"), (1, 16, 256, "f32"), (5, 8, 64, "f32"), (8, 8, 128, "f32"), (20, 8, 128, "f32"),
+    (3, 8, 256, "f32"), (2, 4, 32, "f32"), (1, 8, 128, "bf16"), (5, 8, 64, "bf16"), (8, 8, 128, "bf16"), (4, 8, 256, "bf16"),
+    (9, 8, 64, "bf16"), (9, 8, 128, "bf16"), (20, 8, 64, "bf16"), (20, 8, 128, "bf16")])
+def test_weights_are_held_to_their_bits(drafts, group, dh, dtype, size):
+    """32 places whose keys and values are the unit vectors, so that a result is its row's weights: within the bound of the parts
+    that queries and weights are held in, which one part less exceeds."""
+    n, scale, heads, batch = 32, 0.125, 2, 40
+    c = Fp8Cache.empty(2, heads, 16, dh)
+    unit = torch.eye(n, dh, device="cuda")[:, None].expand(n, heads, dh)
+    c.write(unit, unit, torch.arange(n, device="cuda"))
+    assert (c.k_scale[:, :, :] == 2.0 ** -8).all()  # 1 / 448 and up: exact
+    table = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda").expand(batch, 2).contiguous()
+    lengths = torch.full((batch,), n, dtype=torch.int32, device="cuda")
+    q = on_gpu(rng(31, drafts, dh).uniform(-1, 1, (batch, drafts, heads * group, dh)) * size / scale, dtype)
+    got = host(c.attend(q, table, lengths, scale=scale)).reshape(-1, dh)
+    seen = np.broadcast_to(n - drafts + 1 + np.arange(drafts)[None, :, None], q.shape[:3]).reshape(-1)
+    ref, reach = oracle.weights(host(q).reshape(-1, dh), seen, scale)
+    assert (got[ref == 0] == 0).all()
+    off = oracle.weights_off(reach, bf16=dtype == "bf16")[:, None]
+    low, high = (on_gpu(ref * (1 + sign * off), "f32") for sign in (-1, 1))
+    if dtype == "bf16":  # the result's own rounding
+        low, high = low.bfloat16(), high.bfloat16()
+    assert ((host(low) <= got) & (got <= host(high))).all(), float(np.abs(got / np.where(ref > 0, ref, 1) - 1)[ref > 0].max())
+
+
 def test_queries_and_results_of_any_strides():
     c, q, table, lengths = setup((9,), 3, 4, 2, 3, 64, 16, [50, 9, 80])
     ref = c.attend(q, table, lengths)

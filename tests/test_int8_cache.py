@@ -50,6 +50,66 @@ def test_oracle_attends():
     np.testing.assert_allclose(out[0, 0, 0], (np.arange(1, 5) / 10) @ v[0, 0])
 
 
+def test_oracle_weighs():
+    w, reach = cache_oracle.weights([[0.0, math.log(3.0), 7.0], [1.0, 2.0, 3.0]], [2, 1], 1.0)
+    np.testing.assert_allclose(w, [[0.25, 0.75, 0.0], [1.0, 0.0, 0.0]])
+    np.testing.assert_allclose(reach, [math.log(3.0), 1.0])
+
+
+def nearest_bf16(x):
+    """float32 to bf16 and back, ties to even."""
+    u = np.asarray(x, dtype=np.float32).view(np.uint32).astype(np.uint64)
+    return ((u + 0x7FFF + (u >> np.uint64(16) & np.uint64(1))) & np.uint64(0xFFFF0000)).astype(np.uint32).view(np.float32)
+
+
+def in_parts(x, n):
+    """x as the sum of its n nearest bf16 parts."""
+    rest, total = np.asarray(x, dtype=np.float32), np.zeros(np.shape(x))
+    for _ in range(n):
+        part = nearest_bf16(rest)
+        rest = (rest - part).astype(np.float32)
+        total += part
+    return total
+
+
+def weighed(q, n, scale, q_parts, p_parts):
+    """The steps of the attention kernels for those weights: float32 between them, q and the weights in bf16 parts."""
+    f = np.float32
+    s = in_parts(q, q_parts).astype(f)
+    c = f(f(scale) * f(1.44269504088896340736))
+    there = np.arange(q.shape[1]) < n[:, None]
+    top = np.where(there, s, f(-np.inf)).max(axis=1, keepdims=True)
+    x = (s.astype(np.float64) * c - (top * c).astype(np.float64)).astype(f)
+    p = np.where(there, np.exp2(x.astype(np.float64)).astype(f), f(0))
+    total = np.zeros(q.shape[0], dtype=f)
+    for j in range(q.shape[1]):
+        total += p[:, j]
+    return in_parts(p, p_parts).astype(f) * (f(1) / total)[:, None]
+
+
+@pytest.mark.parametrize("size", [0.5, 30.0])
+def test_the_bound_of_weights_tells_their_parts_apart(size):
+    """float32: three parts of queries and of weights are within it, two of the queries are not, nor are two of the weights
+    where logits are small.  bf16: two parts of the weights are, one is not."""
+    r = np.random.default_rng(7)
+    n, scale = r.integers(2, 33, 400), 0.125
+    q = (r.uniform(-1, 1, (400, 64)) * size / scale).astype(np.float32)
+    ref, reach = cache_oracle.weights(q, n, scale)
+
+    def off(q_parts, p_parts, q=q, ref=ref):
+        with np.errstate(divide="ignore", invalid="ignore"):
+            return np.where(ref > 0, np.abs(weighed(q, n, scale, q_parts, p_parts) / ref - 1), 0.0)
+    bound = cache_oracle.weights_off(reach)[:, None]
+    assert (off(3, 3) <= bound).all()
+    assert (off(2, 3) > bound).any()
+    if size < 1:
+        assert (off(3, 2) > bound).any()
+    q = nearest_bf16(q)
+    ref, reach = cache_oracle.weights(q, n, scale)
+    bound = cache_oracle.weights_off(reach, bf16=True)[:, None]
+    assert (off(1, 2, q, ref) <= bound).all() and (off(1, 1, q, ref) > bound).any()
+
+
 # ------------------------------------------------------------------ refusals of the quantiser and the products
 
 
