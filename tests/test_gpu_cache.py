@@ -592,6 +592,25 @@ def test_weights_are_held_to_their_bits(drafts, group, dh, dtype, size):
     assert ((host(low) <= got) & (got <= host(high))).all(), float(np.abs(got / np.where(ref > 0, ref, 1) - 1)[ref > 0].max())
 
 
+@pytest.mark.parametrize("batch,drafts,group,dh,length", [(512, 1, 4, 64, 35200), (256, 16, 8, 128, 8960), (256, 3, 8, 256, 17920)])
+def test_many_small_weights_beside_a_large_one(batch, drafts, group, dh, length):
+    """Copies of a sequence whose first place has the weight 1 and whose others have e^-16.661 = 0.4875 2^-23 each, which are
+    lost beside it one by one, in chunks of 140 steps to a wave.  Values are 1, so a result is the sum of the weights over itself.
+    At each step the numerator adds 32 places to 1, in eights (2^-24 off each), the sum of the first place's lane the 8 that it
+    holds (2^-24).  Lost one by one, these 8 were 7.8 2^-24.  2^-20: all other roundings."""
+    c = Fp8Cache.empty(-(-length // 64), 1, 64, dh)
+    c.k_scale.fill_(1.0), c.v_scale.fill_(1.0)
+    c.k[..., 0].view(torch.uint8).fill_(0x38), c.v.view(torch.uint8).fill_(0x38)  # 1
+    c.k.view(torch.uint8)[0, 0, 0, 0] = 0
+    q = torch.zeros(batch, drafts, group, dh, device="cuda")
+    q[..., 0] = -16.661
+    table = torch.arange(c.pages, dtype=torch.int32, device="cuda").expand(batch, -1).contiguous()
+    lengths = torch.full((batch,), length, dtype=torch.int32, device="cuda")
+    got = c.attend(q, table, lengths, scale=1.0)
+    off = float((got.double() - 1).abs().max())
+    assert off <= 140 * 5 * 2.0 ** -24 + 2.0 ** -20
+
+
 def test_queries_and_results_of_any_strides():
     c, q, table, lengths = setup((9,), 3, 4, 2, 3, 64, 16, [50, 9, 80])
     ref = c.attend(q, table, lengths)
