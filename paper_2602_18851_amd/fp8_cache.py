@@ -84,13 +84,13 @@ class Fp8Cache:
             refuse_autograd("a tensor of the cache")
 
     def _slots(self, slots: torch.Tensor, n: int) -> int:
-        if slots.dtype != torch.int64 or tuple(slots.shape) != (n,) or slots.device != self.device \
+        if slots.dtype != torch.int64 or slots.shape != (n,) or slots.device != self.device \
                 or not slots.is_contiguous():
             raise ValueError(f"slots must be a contiguous int64 tensor [{n}] on {self.device}")
         return slots.data_ptr()
 
     def _rows(self, x: torch.Tensor, name: str, dtype: torch.dtype, n: int) -> tuple[int, int, int]:
-        if x.dtype != dtype or dtype not in _DTYPES or x.device != self.device or x.dim() != 3 \
+        if x.dtype != dtype or dtype not in _DTYPES or x.device != self.device \
                 or x.shape != (n, self.heads, self.head_dim):
             raise ValueError(f"k and v must be float32 or bfloat16 tensors [tokens, {self.heads}, {self.head_dim}] of one "
                              f"type on {self.device}")
@@ -106,7 +106,8 @@ class Fp8Cache:
         row's scale is the smallest power of two, 2^-126 at least, with max|x| / scale <= 448 (e4m3) or 57344 (e5m2), a code x
         / scale rounded to nearest even; a row that holds an infinity or a NaN becomes NaN.  Tokens whose slot is not in
         [0, pages * page) are padding and not written; the other slots must differ."""
-        n = k.shape[0] if k.dim() == 3 else -1
+        shape = k.shape
+        n = shape[0] if len(shape) == 3 else -1
         self._no_gradients()
         on_stream_of(self.device, spectral_cache_write, self._c, _DTYPES.get(k.dtype, -1), n,
                      *self._rows(k, "k", k.dtype, n), *self._rows(v, "v", k.dtype, n), self._slots(slots, n))
@@ -115,7 +116,8 @@ class Fp8Cache:
         """(keys, values) of slots (int64 [tokens]), each [tokens, heads, head_dim]: code * scale rounded to dtype (float32 or
         bfloat16); zeros for slots outside.  out: a pair of tensors of one type, any token and head strides without
         overlaps; new ones of dtype if None."""
-        n = slots.shape[0] if slots.dim() == 1 else -1
+        shape = slots.shape
+        n = shape[0] if len(shape) == 1 else -1
         self._no_gradients()
         if out is None:
             if dtype not in _DTYPES:
@@ -141,12 +143,13 @@ class Fp8Cache:
         scale: head_dim ** -0.5 if None.  out: like q, without overlaps; workspace: uint8 scratch for callers that keep
         it (a new tensor where it is too small); calls that can run at the same time need their own."""
         dev, dtype, dh = self.device, q.dtype, self.head_dim
-        if q.dim() != 4 or dtype not in _DTYPES or q.device != dev or q.shape[3] != dh:
+        shape = q.shape
+        if len(shape) != 4 or dtype not in _DTYPES or q.device != dev or shape[3] != dh:
             raise ValueError(f"q must be a float32 or bfloat16 tensor [batch, tokens, query heads, {dh}] on {dev}")
         if q.requires_grad:
             refuse_autograd("q")
         self._no_gradients()
-        batch, n, hq, _ = q.shape
+        batch, n, hq, _ = shape
         if not 1 <= n <= 64 or hq == 0 or hq % self.heads:
             raise ValueError(f"q must have 1 to 64 tokens and a multiple of {self.heads} heads")
         if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.device != dev:
@@ -159,12 +162,12 @@ class Fp8Cache:
             table_ld = cols
         elif table_ld < cols:
             raise ValueError("table must be row-major")
-        if lengths.dtype != torch.int32 or tuple(lengths.shape) != (batch,) or lengths.device != dev \
+        if lengths.dtype != torch.int32 or lengths.shape != (batch,) or lengths.device != dev \
                 or not lengths.is_contiguous():
             raise ValueError(f"lengths must be a contiguous int32 tensor [{batch}] on {dev}")
         masks = mask_batch = 0
         if tree is not None:
-            if tree.dtype != torch.int64 or tuple(tree.shape) not in ((n,), (batch, n)) or tree.device != dev \
+            if tree.dtype != torch.int64 or tree.shape not in ((n,), (batch, n)) or tree.device != dev \
                     or (n > 1 and tree.stride(-1) != 1):
                 raise ValueError(f"tree must be an int64 tensor [{n}] or [{batch}, {n}] on {dev}, rows contiguous")
             masks, mask_batch = tree.data_ptr(), tree.stride(0) if tree.dim() == 2 else 0
@@ -172,10 +175,10 @@ class Fp8Cache:
         if q_strides[3] != 1:
             raise ValueError("heads must be contiguous")
         if out is None:
-            out = torch.empty(q.shape, dtype=dtype, device=dev)
+            out = torch.empty(shape, dtype=dtype, device=dev)
             o_strides = (n * hq * dh, hq * dh, dh)
         else:
-            if out.shape != q.shape or out.dtype != dtype or out.device != dev:
+            if out.shape != shape or out.dtype != dtype or out.device != dev:
                 raise ValueError("out must have the shape, type and device of q")
             o_strides = out.stride()
             if o_strides[3] != 1:
