@@ -492,8 +492,9 @@ SN_API int spectral_cache_read(const sn_cache* cache, int32_t dtype, int64_t tok
  * place holds that a token does not see, NaN and infinities too, does not
  * reach its result.  A NaN that it sees, as spectral_cache_write makes of a row that is
  * not finite, does: of a key it makes the whole result NaN, of a value its element.
- * Infinities are codes of SN_E5M2 that spectral_cache_write never stores.  Of a value that is seen
- * they make its element NaN or an infinity; of a key the whole result NaN or, where the
+ * Infinities are codes of SN_E5M2 that spectral_cache_write never stores, and elements that it
+ * rounds to 2^128 (|x| from 1.9375 2^127 on, with SN_E5M2 1.875).  Of a value that is seen they
+ * make its element NaN or an infinity; of a key the whole result NaN or, where the
  * logit is minus infinity, a weight of zero.
  *   q        device, element e of head h of drafted token i of sequence b at
  *            b * q_batch + i * q_draft + h * q_head + e; out the same.

@@ -113,6 +113,27 @@ def test_rows_of_extremes(fmt):
         np.testing.assert_array_equal(host(ss)[0, 0, :7], scale[:, 0])
 
 
+@pytest.mark.parametrize("fmt,first", [("e4m3", 1.9375), ("e5m2", 1.875)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_elements_that_round_to_an_infinity(fmt, first, dtype):
+    """The last element that is held as a finite one, the next, and the type's largest: 2^128 from `first` 2^127 on."""
+    last = torch.tensor(first * 2.0 ** 127).to(TORCH[dtype])
+    below = torch.nextafter(last, torch.zeros_like(last)) if dtype == "f32" else (last.view(torch.int16) - 1).view(torch.bfloat16)
+    x = torch.stack([below, last, torch.tensor(torch.finfo(TORCH[dtype]).max).to(TORCH[dtype])]).cuda()
+    x = torch.stack([x, -x]).reshape(6, 1, 1).repeat(1, 1, 16)
+    x[:, :, 1:] = 1.0
+    c = Fp8Cache.empty(1, 1, 16, 16, fmt)
+    c.write(x, x, torch.arange(6, device="cuda"))
+    for got in c.read(torch.arange(6, device="cuda"), dtype=torch.float32):
+        down = 2 * first - 2.0  # the mantissa below the midpoint
+        want = torch.tensor([down * 2.0 ** 127, float("inf"), float("inf")])
+        assert torch.equal(got[:3, 0, 0].cpu(), want) and torch.equal(got[3:, 0, 0].cpu(), -want)
+    q = torch.full((1, 1, 1, 16), 2.0 ** -120, device="cuda").to(TORCH[dtype])
+    table, lengths = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    assert torch.isfinite(c.attend(q, table, lengths)).all()
+    assert not torch.isfinite(c.attend(q, table, lengths + 1)[..., 0]).any()
+
+
 def test_rows_of_any_strides_and_pages_apart():
     """Keys and values as windows of one projection; a cache whose pages hold keys and values side by side."""
     r = rng(3)
