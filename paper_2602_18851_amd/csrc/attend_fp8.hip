@@ -256,9 +256,6 @@ __device__ __forceinline__ float quarters_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Weights join a lane's sum in eights, as the matrix cores add them to the result: one by one, thousands of small ones are lost
-// beside a large one (140 steps of 32 places, a weight of 1 and others just below 2^-24: 7.1e-5 off, in eights 4.9e-6).
-
 // A row's running maximum is raised, and its sums scaled, only when a logit is above it by a factor of 2^kSlack in weight: until
 // then weights are up to 2^kSlack, which float32 and bf16 hold as exactly.
 constexpr float kSlack = 8.f;
@@ -485,6 +482,8 @@ attend_kernel(AttendArgs a) {
         top[n] = m;
       }
       const float base = top[n] == kNone ? 0.f : top[n] * c_log2;
+      // Weights join the lane's sum in eights, as the matrix cores add their products to the result: one by one, thousands of
+      // small ones are lost beside a large one (140 steps, a weight of 1 and others just below 2^-24: 7.1e-5 off, now 4.9e-6).
       float p[8], sum = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -665,7 +664,7 @@ __device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, c
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, sum, 0, 0, 0);
 }
 
-// Many rows (trees of drafted tokens): the matrix cores and the exponentials bound the call.  8 waves of 32 rows share
+// Many rows of bf16 (trees of drafted tokens): the matrix cores and the exponentials bound the call.  8 waves of 32 rows share
 // tiles of 8192 / D places, which they widen to bf16 together, once: K to LDS place by place, V turned, so that a lane's eight
 // places of P^T are 16 bytes of a row of V^T.  With 128 rows or less, PARTS 2: pairs of waves have the same rows and half
 // of a tile's places each.  Products of 32 x 32: lane 32 hi + s holds
@@ -683,7 +682,7 @@ __device__ __forceinline__ f32x16 multiply32(const bf16x8& x, const bf16x8& y, c
 //   waves 0-3 write them in 2 i + 1, waves 4-7, a tile ahead, in 2 i.
 // Tiles past the last are loaded and written too, to no use, so that no load in flight meets a branch: the compiler would
 // wait for all of them there (with branches 677 us in the case below, without 483).
-// 16 sequences of 64 tokens, 8 key heads of 128 with 8 query heads each, over 8000-8192 places: 385-412 us by the chip.  The matrix
+// 16 sequences of 64 tokens, 8 key heads of 128 with 8 query heads each, over 8000-8192 places: 381-412 us by the chip.  The matrix
 // products alone take 263 (1.55 PFLOP/s with P in two parts, at the clock that power leaves, the rate of a large bf16
 // product); one part of P 335, with twice the rounding error of the result's type.  Addresses are scalar work that
 // goes beside the matrix products (420 us with the vector part), whose waves have the lower priority.
@@ -949,7 +948,7 @@ __global__ void __launch_bounds__(64 * kTreeWaves, 2) tree_kernel(AttendArgs a) 
     for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        float p[8], sum = 0.f;
+        float p[8], sum = 0.f;  // in eights, as in attend_kernel
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           p[e] = __builtin_amdgcn_exp2f(fmaf(st[n][8 * g + e], c_log2, -base));

@@ -37,7 +37,8 @@ __device__ __forceinline__ bool locate(const RowsArgs& a, uint32_t row, uint32_t
 }
 
 // LANES lanes of 16 elements take a row of keys and that of values together, so that enough is on its way: 8191
-// tokens of 8 heads of 128 in bf16 take 9.9 us (5.1 TB/s; 11.5 with 8 elements of one of the two a lane).
+// tokens of 8 heads of 128 in bf16 take 9.9 us (11.5 with 8 elements of one of the two a lane) again and again, when the
+// 256 MB cache holds them, and 13.9 (3.7 TB/s) when it does not; in float32 10.8 again and again.
 template <typename T, bool E5M2, int LANES>
 __global__ void __launch_bounds__(256) write_kernel(RowsArgs a) {
   const int t = threadIdx.x, c = 16 * (t % LANES);
@@ -92,8 +93,9 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&f)[4]) {
 }
 
 // A lane takes the elements of one 16-byte store of keys and of values, and two rows at a time.  The results are more
-// than the caches hold where it counts, so their stores pass them by: 32768 tokens of 8 heads of 128 to bf16 33.6 us (6.0 TB/s),
-// 41.5 with ordinary stores, 47.5 with 8 elements of one of the two a lane.
+// than the caches hold where it counts, so their stores pass them by: 32768 tokens of 8 heads of 128 to bf16 33.6 us, 41.5 with
+// ordinary stores, 47.5 with 8 elements of one of the two a lane, all again and again; 41.6 (4.9 TB/s) of inputs that no
+// cache holds.
 template <typename T, bool E5M2, int LANES>
 __global__ void __launch_bounds__(256) read_kernel(RowsArgs a) {
   constexpr int PER = 16 / sizeof(T), WORDS = PER / 4, ROWS = 2;

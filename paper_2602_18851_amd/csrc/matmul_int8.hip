@@ -168,7 +168,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) tile_kernel(IntArgs a) {
 
 // Products of few tiles: tiles of 64 x 64 by 4 waves of 32 x 32, so that four times as many workgroups share the product, with a
 // ring of kSStages blocks of columns in LDS: a workgroup alone on its compute unit hides its loads' latency itself.
-// 1001 x 999 x 3001: 12 us, of which the host's part of a call is 9 (tiles of 128 x 128 in four parts: 20).
+// 1001 x 999 x 3001: 10.7-12 us for 24 blocks one after the other, bound by their latency (a call with tiles of 128 x 128 in
+// four parts: 20); 1000^3, 8 blocks, 7-7.5.
 constexpr int kST = 64, kSStages = 4;
 constexpr int kSStage = 2 * kST * 128;
 
@@ -468,6 +469,8 @@ __device__ __forceinline__ void stage_plain(const IntArgs& a, uint8_t* codes, fl
 }
 
 // The same for one row of up to kHeldRow columns, held in registers; its barriers wait for no load, so that those of B go on.
+// Longer ones do not fit there and are quantised before B is requested: bf16 against 8192 x 14336 29.7 us, from codes 21.8, and
+// against 8192 x 28672 50.6 and 37.8.
 constexpr int kHeldRow = 2 * 8 * 64 * kFewWaves;
 template <typename T>
 struct HeldRow {

@@ -16,7 +16,8 @@ using sn::QuantInt8Args;
 
 // LANES lanes take a row, which they hold in registers, 8 values of every 8 LANES in HELD groups, so x is
 // read once; rows that are too long for that (HELD 0) are read a second time for their codes.  Bound by memory: 8192 x 8192
-// bf16 36 us (5.6 TB/s; 42 with every quotient checked for ties), 4097 x 3001 float32 12.5 us (4.9).  Codes stored past the
+// bf16 34-38 us, of inputs that no cache holds 37 (5.4 TB/s; 42 with every quotient checked for ties), 4097 x 3001 float32 12-13.5 us
+// (4.6).  Codes stored past the
 // caches take 34, but the product that follows reads them.
 template <typename T, int LANES, int HELD>
 __global__ void __launch_bounds__(256) quantize_int8_kernel(QuantInt8Args a) {
