@@ -469,6 +469,17 @@ def test_more_sequences_than_are_scanned(batch, drafts, group, dh, page, dtype):
         assert torch.equal(got[some], c.attend(q[some], table[some, :256 // page], lengths[some]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_most_sequences(dtype):
+    """2^20 copies of 200, which have the bits of these."""
+    r = rng(20)
+    lens = r.integers(0, 65, 200)
+    c, q, table, lengths = setup((32,), 200, 1, 1, 2, 16, 16, [int(n) for n in lens], dtype=dtype)
+    ref = c.attend(q, table, lengths)
+    copy = torch.from_numpy(r.integers(0, 200, 1 << 20)).cuda()
+    assert torch.equal(c.attend(q[copy], table[copy], lengths[copy]), ref[copy])
+
+
 def test_the_time_of_many_sequences_grows_as_they_do():
     """Four times the sequences take about four times as long: 16 times when every workgroup looked at every sequence."""
     c, _, rows, _ = setup((19,), 1, 1, 1, 1, 16, 16, [64])
